@@ -49,7 +49,14 @@ typedef enum {
 } hq_status;
 
 typedef enum { HQ_E8 = 0, HQ_D4 = 1, HQ_A2 = 2, HQ_Z = 3 } hq_lattice;
-typedef enum { HQ_BF16 = 0, HQ_FP32 = 1, HQ_FP16 = 2, HQ_INT8 = 3 } hq_dtype;
+typedef enum {
+  HQ_BF16 = 0,
+  HQ_FP32 = 1,
+  HQ_FP16 = 2,
+  HQ_INT8 = 3,
+  HQ_E4M3 = 4, /* OCP FP8 (cache format) */
+  HQ_MXFP4 = 5 /* OCP Microscaling FP4 (cache format) */
+} hq_dtype;
 typedef enum { HQ_ROT_NONE = 0, HQ_ROT_SIGNS = 1, HQ_ROT_QJL = 2 } hq_rotation;
 
 /* Options beyond the five knobs of hq_plan; all-zero means the weight-path
@@ -425,6 +432,133 @@ hq_status hq_decode_attention(hq_plan_t k_plan, const hq_stream* k, hq_plan_t v_
                               const void* window_k, const void* window_v, int32_t wt,
                               int32_t window, void* out, int32_t ot, void* workspace,
                               size_t ws_bytes, void* stream);
+
+/* A key or value cache at a fixed rate: the cast path (Sec. 4.8) applied to head
+ * vectors of 128, as a store whose slots can be written in any order, freed and
+ * written again (a coded stream only grows).  A stored vector is the cast of
+ * y = H D x, D the plan's signs of the head's columns:
+ *   HQ_INT8   codes c = clamp(rint(y * 127 / max|y|), +-127), scale max|y| / 127;
+ *   HQ_E4M3   codes E4M3(y * 448 / max|y|), scale max|y| / 448;
+ *   HQ_MXFP4  E2M1 pairs (the even value in the low nibble) and one E8M0 byte
+ *             per 32 values, as hq_act_prep_mxfp4 casts.
+ * A vector whose transform holds an infinity or a NaN is stored as codes 0 with
+ * the scale NaN (E8M0 byte 255): it reads back as NaN and makes the outputs that
+ * attend to it NaN.  int8 and E4M3 vectors with max|y| below 2^-100 are stored as
+ * zeros with scale 0.
+ *   codes         device, 16-byte aligned, [blocks, heads, block_tokens, 128] bytes
+ *                 (HQ_MXFP4: 64): one head's tokens of a block are one run.
+ *   scales        device, 16-byte aligned: fp32 [blocks, heads, block_tokens]
+ *                 (HQ_MXFP4: bytes [blocks, heads, block_tokens, 4]).
+ *   block_tokens  a multiple of 16 (HQ_ERR_UNSUPPORTED otherwise); blocks *
+ *                 block_tokens below 2^31.
+ *   heads         KV heads; heads * 128 <= plan.cols (a plan's columns are a multiple
+ *                 of 512, so 1, 2 or 3 heads use the first of its columns).
+ *   stats         nullable device hq_stats.
+ * Slot i is token i % block_tokens of block i / block_tokens.  The library writes
+ * no slot that it is not given.  Plans: tile 128, no rotation, dither or fp16 norms
+ * (HQ_ERR_UNSUPPORTED otherwise), made on the current device
+ * (HQ_ERR_INVALID_ARG otherwise). */
+typedef struct {
+  void* codes;
+  void* scales;
+  int64_t blocks;
+  int32_t block_tokens;
+  int32_t heads;
+  int32_t format;    /* HQ_INT8, HQ_E4M3 or HQ_MXFP4 */
+  int32_t reserved0;
+  hq_stats* stats;
+} hq_cache;
+
+/* hq_cache_write -- cast row r of k (and of v) into slot slots[r] of its cache.
+ *   k, v    device, rows x heads * 128, element type xt (HQ_BF16 or HQ_FP32),
+ *           row strides ldk, ldv elements; 16-byte aligned, strides a multiple
+ *           of 16 bytes.  One launch writes both; v, v_plan and v_cache may be
+ *           null together to write k alone.
+ *   slots   device int64 [rows]; a negative slot skips its row (padding).  The
+ *           other slots of a call are distinct: of rows that share one, its
+ *           contents are unspecified.
+ * The caches have one format, heads and block_tokens (plans and block counts may
+ * differ) and share no memory.  Device-side, in each cache's stats: a slot past the
+ * cache is skipped (HQ_ERR_INVALID_ARG); a vector with a non-finite transform
+ * counts in overflow_tiles (HQ_ERR_OVERFLOW).  Host errors: HQ_ERR_INVALID_ARG,
+ * HQ_ERR_UNSUPPORTED (rows * heads >= 2^31), HQ_ERR_HIP. */
+hq_status hq_cache_write(hq_plan_t k_plan, const void* k, int64_t ldk, const hq_cache* k_cache,
+                         hq_plan_t v_plan, const void* v, int64_t ldv, const hq_cache* v_cache,
+                         int32_t xt, int64_t rows, const int64_t* slots, void* stream);
+
+/* hq_cache_read -- row r of y = the values slot slots[r] stands for, D H (s c) / 128.
+ *   y       device, rows x heads * 128, HQ_BF16 (round to nearest even) or
+ *           HQ_FP32, row stride ld; aligned as for hq_cache_write.
+ *   slots   device int64 [rows]; any order, a slot may repeat.  A negative slot
+ *           gives a row of zeros, a slot past the cache too (HQ_ERR_INVALID_ARG
+ *           in c->stats).
+ * Host errors as hq_cache_write. */
+hq_status hq_cache_read(hq_plan_t plan, const hq_cache* c, const int64_t* slots, int64_t rows,
+                        void* y, int32_t yt, int64_t ld, void* stream);
+
+/* Workspace bytes for hq_cache_attention over a key cache (its heads and
+ * block_tokens count), 0 for invalid arguments.  Never less for a larger batch,
+ * heads_q or max_blocks: a workspace for the largest call serves every smaller one. */
+size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int32_t heads_q,
+                                          int32_t max_blocks);
+
+/* hq_cache_attention -- one query token per sequence attending over a fixed-rate
+ * cache: out[b, h] = sum_t softmax_t(scale q[b, h] . k^_t) v^_t, k^ and v^ the rows
+ * hq_cache_read would return in fp32.  The query is moved into the stored
+ * coordinates once and the value sum back once; nothing is materialized.
+ *   k, v         caches of one format, heads, block_tokens and blocks.
+ *   q            device [batch, heads_q, 128], HQ_BF16 or HQ_FP32, 16-byte
+ *                aligned; head h reads KV head h / (heads_q / heads), a group of
+ *                1 .. 16 (HQ_ERR_UNSUPPORTED above).
+ *   scale        softmax scale (1 / sqrt(128) for standard attention), finite.
+ *   block_table  device int32 [batch, max_blocks]: token t of sequence b is token
+ *                t % block_tokens of block block_table[b, t / block_tokens].
+ *                Entries behind a sequence's last block are not read.
+ *   seq_lens     device int32 [batch] token counts; an empty sequence gives zeros.
+ *                What lies in the cache behind a sequence's last token does not
+ *                matter (stale codes, NaN scales).
+ *   out          device [batch, heads_q, 128], HQ_FP32 or HQ_BF16 (round to
+ *                nearest even), 16-byte aligned.
+ *   workspace    device, 16-byte aligned, >= hq_cache_attention_workspace_bytes(
+ *                k, batch, heads_q, max_blocks); not read or written, and may be
+ *                null, where that call's tokens are not split.  Calls that may
+ *                overlap (on two streams, or two captured graphs that may) need
+ *                one each.
+ * Scores, maxima and sums are fp32, in an order fixed by the call's shape and the
+ * sequence's length, so results repeat bit for bit.  Device-side, in k->stats: a
+ * length outside 0 .. max_blocks * block_tokens is clamped, tokens of a block id
+ * outside the cache are left out (both HQ_ERR_INVALID_ARG).  Host errors:
+ * HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (max_blocks * block_tokens above 2^30),
+ * HQ_ERR_HIP. */
+hq_status hq_cache_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan_t v_plan, const hq_cache* v,
+                             const void* q, int32_t qt, int64_t batch, int32_t heads_q, float scale,
+                             const int32_t* block_table, int32_t max_blocks, const int32_t* seq_lens,
+                             void* out, int32_t ot, void* workspace, size_t ws_bytes, void* stream);
+
+/* hq_rmsnorm_act_prep -- the residual's addition, an RMS norm and hq_act_prep in
+ * one pass: h = bf16(x + residual), y = H D (h * weight) / rms(h) per tile with
+ * rms(h) = sqrt(mean(h^2) + eps), then x_q and s_x of y as hq_act_prep defines them
+ * (any tile), for hq_gemm_int8_blockscaled.  The codes do not depend on rms(h), one
+ * factor of the whole row: it enters s_x alone.
+ *   x         device bf16 M x cols, row stride ldx
+ *   residual  nullable device bf16 M x cols, row stride ldr; null: h = x
+ *   weight    device [cols], wt = HQ_BF16 or HQ_FP32
+ *   eps       finite, > 0
+ *   h         nullable device bf16 M x cols, row stride ldh: receives h; may be x
+ *             or residual themselves (same pointer and stride)
+ *   xq, sx    as hq_act_prep: device int8 M x cols (contiguous, 8-byte aligned),
+ *             fp32 [M]
+ * x, residual, weight and h are 16-byte aligned, their strides multiples of 8.  A row
+ * with an infinity or a NaN, or with a sum of squares past fp32, gets s_x = NaN; a row
+ * of zeros (max|y rms(h)| below 2^-100) zeros (E4M3: of either sign) and s_x = 0.  Host
+ * errors: HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (cols above 16384), HQ_ERR_HIP.
+ * hq_rmsnorm_act_prep_fp8 -- the same with x_q and s_x of hq_act_prep_fp8. */
+hq_status hq_rmsnorm_act_prep(hq_plan_t plan, const void* x, int64_t ldx, const void* residual,
+                              int64_t ldr, const void* weight, int32_t wt, float eps, int64_t M,
+                              void* h, int64_t ldh, int8_t* xq, float* sx, void* stream);
+hq_status hq_rmsnorm_act_prep_fp8(hq_plan_t plan, const void* x, int64_t ldx, const void* residual,
+                                  int64_t ldr, const void* weight, int32_t wt, float eps, int64_t M,
+                                  void* h, int64_t ldh, uint8_t* xq, float* sx, void* stream);
 
 /* The library's automatic Rice-k rule for `count` symbols summing to `sum`
  * (the geometric optimum k* of Sec. 3.3), as the kernels evaluate it. */

@@ -238,7 +238,84 @@ struct hq_gemm_args {
   int32_t tile;       // RHT tile: the weight factors' K span (128 .. 2048)
 };
 
+// One tensor of a cache write or read.
+struct hq_cache_side {
+  const void* x;          // write: rows of heads * 128 values, stride ld
+  int64_t ld;
+  uint8_t* codes;
+  void* scales;
+  int64_t slots;          // blocks * block_tokens
+  const uint32_t* dmask;  // RHT sign bit per column
+  hq_stats* stats;
+};
+struct hq_cache_io_args {
+  hq_cache_side side[2];  // write: keys, values; read: the first only
+  const int64_t* slots;   // one per row
+  uint32_t tiles;         // rows * heads
+  int32_t heads, block_tokens;
+  int32_t x_bf16;
+  void* y;                // read: output rows, stride ldy
+  int64_t ldy;
+  int32_t y_bf16;
+};
+
+// One-token attention over a fixed-rate cache.  Workspace (splits > 1): per
+// (sequence, query head, split) the sum of 128 values, its maximum and its weight.
+struct hq_cache_attn_args {
+  const uint8_t* k_codes;
+  const void* k_scales;
+  const uint8_t* v_codes;
+  const void* v_scales;
+  const uint32_t* k_dmask;
+  const uint32_t* v_dmask;
+  const void* q;
+  void* out;
+  const int32_t* table;     // batch x max_blocks block ids
+  const int32_t* seq_lens;  // batch token counts
+  float* part_acc;
+  float* part_m;
+  float* part_l;
+  hq_stats* stats;
+  int64_t batch, blocks;
+  int32_t heads_q, heads_kv, group;
+  int32_t max_blocks, block_tokens;
+  int32_t splits;
+  int32_t q_bf16, out_bf16;
+  float qscale;             // softmax scale times log2(e) / 128
+};
+
+#define HQ_CACHE_WG_TARGET 512  // workgroups a cache attention call aims at
+
+// Splits of each sequence's tokens: enough workgroups (one per KV head and
+// split) to fill the chip, of at least 128 tokens each.
+static inline int64_t hq_cache_splits(int64_t heads, int64_t max_tokens) {
+  const int64_t most = (max_tokens + 127) / 128;
+  const int64_t want = (HQ_CACHE_WG_TARGET + heads - 1) / heads;
+  return want < most ? want : most;
+}
+
+// RMS norm fused with the 8-bit activation prep.
+struct hq_norm_args {
+  const void* x;          // bf16 rows, stride ldx
+  const void* residual;   // bf16 rows, stride ldr, or null
+  const void* weight;     // K values
+  void* h;                // bf16 rows x + residual, stride ldh, or null
+  int64_t ldx, ldr, ldh;
+  int64_t M, K;
+  int8_t* xq;
+  float* sx;
+  const uint32_t* dmask;
+  float eps;
+  int32_t w_bf16;
+  int32_t fp8;
+  int32_t tile;
+};
+
 // Kernel launchers; return a hipError_t as int.
+int hq_launch_cache_write(const hq_cache_io_args& a, int format, int sides, void* stream);
+int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream);
+int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* stream);
+int hq_launch_norm_prep(const hq_norm_args& a, void* stream);
 int hq_launch_encode(const hq_plan_s* p, const hq_encode_args& a, const hq_rice_thr& t, int xt,
                      void* stream);
 int hq_launch_decode(const hq_plan_s* p, const hq_decode_args& a, int yt, void* stream);

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libhq.so")
 
 HQ_OK = 0
 HQ_E8, HQ_D4, HQ_A2, HQ_Z = 0, 1, 2, 3
-HQ_BF16, HQ_FP32, HQ_FP16, HQ_INT8 = 0, 1, 2, 3
+HQ_BF16, HQ_FP32, HQ_FP16, HQ_INT8, HQ_E4M3, HQ_MXFP4 = 0, 1, 2, 3, 4, 5
 HQ_ROT_NONE, HQ_ROT_SIGNS, HQ_ROT_QJL = 0, 1, 2
 LATTICES = {"E8": HQ_E8, "D4": HQ_D4, "A2": HQ_A2, "Z": HQ_Z}
 STATUS = {0: "HQ_OK", -1: "HQ_ERR_INVALID_ARG", -2: "HQ_ERR_UNSUPPORTED", -3: "HQ_ERR_CAPACITY",
@@ -58,6 +58,12 @@ class StreamStruct(C.Structure):
                 ("kparam", C.c_void_p), ("norms", C.c_void_p), ("rows_capacity", C.c_int64),
                 ("rows", C.c_int64), ("scan", C.c_void_p), ("scan_bytes", C.c_int64),
                 ("stats", C.c_void_p)]
+
+
+class CacheStruct(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("blocks", C.c_int64),
+                ("block_tokens", C.c_int32), ("heads", C.c_int32), ("format", C.c_int32),
+                ("reserved0", C.c_int32), ("stats", C.c_void_p)]
 
 
 _lib = None
@@ -122,6 +128,18 @@ def lib():
     L.hq_decode_attention.restype = i32
     L.hq_decode_attention.argtypes = [p, p, p, p, p, i32, i64, i32, C.c_float, p, i32, i32, p, p,
                                       p, i32, i32, p, i32, p, C.c_size_t, p]
+    L.hq_cache_write.restype = i32
+    L.hq_cache_write.argtypes = [p, p, i64, p, p, p, i64, p, i32, i64, p, p]
+    L.hq_cache_read.restype = i32
+    L.hq_cache_read.argtypes = [p, p, p, i64, p, i32, i64, p]
+    L.hq_cache_attention_workspace_bytes.restype = C.c_size_t
+    L.hq_cache_attention_workspace_bytes.argtypes = [p, i64, i32, i32]
+    L.hq_cache_attention.restype = i32
+    L.hq_cache_attention.argtypes = [p, p, p, p, p, i32, i64, i32, f32, p, i32, p, p, i32, p,
+                                     C.c_size_t, p]
+    for fn in (L.hq_rmsnorm_act_prep, L.hq_rmsnorm_act_prep_fp8):
+        fn.restype = i32
+        fn.argtypes = [p, p, i64, p, i64, p, i32, f32, i64, p, i64, p, p, p]
     L.hq_rice_kstar.restype = i32
     L.hq_rice_kstar.argtypes = [i64, i64]
     L.hq_calibrated_snr.restype = i32
@@ -501,6 +519,196 @@ def hq_decode_attention(k_plan: Plan, k: EncodedStream, v_plan: Plan, v: Encoded
     return out
 
 
+def _on_device(*tensors):
+    """The tensors lie on the current device, whose stream the call goes to."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor on {t.device} in a call on cuda:{dev}")
+
+
+def _rows(t, width, name):
+    """A 2-D tensor of `width` contiguous values a row: its row stride."""
+    if t.dim() != 2 or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [rows, {width}] with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+
+
+class Cache:
+    """A fixed-rate key or value cache (hq_cache) of `blocks` blocks of
+    `block_tokens` slots in HQ_INT8, HQ_E4M3 or HQ_MXFP4.  heads: KV heads (the
+    plan's cols / 128 by default).  codes / scales: tensors to use instead of
+    new, zeroed ones (one byte a code, [blocks, heads, block_tokens, 128], and
+    fp32 [blocks, heads, block_tokens]; MXFP4 [..., 64] and bytes [..., 4])."""
+
+    def __init__(self, plan: Plan, blocks, block_tokens, format=HQ_INT8, heads=None, device="cuda",
+                 codes=None, scales=None, stats=True):
+        self.plan = plan
+        self.heads = plan.cols // 128 if heads is None else heads
+        self.blocks, self.block_tokens, self.format = blocks, block_tokens, format
+        if format not in (HQ_INT8, HQ_E4M3, HQ_MXFP4):
+            raise ValueError(f"unsupported cache format {format}")
+        mx = format == HQ_MXFP4
+        shape = (blocks, self.heads, block_tokens)
+        cshape, sshape = shape + (64 if mx else 128,), shape + ((4,) if mx else ())
+        sdt = torch.uint8 if mx else torch.float32
+        if codes is None:
+            codes = torch.zeros(cshape, dtype=torch.int8 if format == HQ_INT8 else torch.uint8, device=device)
+        if scales is None:
+            scales = torch.zeros(sshape, dtype=sdt, device=codes.device)
+        for t, want, what in ((codes, cshape, "codes"), (scales, sshape, "scales")):
+            if tuple(t.shape) != want or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError(f"{what} must be a contiguous device tensor of shape {want}")
+        if codes.element_size() != 1 or scales.dtype != sdt or scales.device != codes.device:
+            raise ValueError(f"codes of one byte and scales of {sdt} on one device")
+        self.codes, self.scales, self.device = codes, scales, codes.device
+        self.stats = torch.zeros(STATS_BYTES // 4, dtype=torch.int32, device=codes.device) if stats else None
+        self.c = CacheStruct(codes.data_ptr(), scales.data_ptr(), blocks, block_tokens, self.heads,
+                             format, 0, self.stats.data_ptr() if stats else None)
+
+    def read_stats(self):
+        if self.stats is None:
+            return None
+        s = Stats.from_buffer_copy(self.stats.cpu().numpy().tobytes())
+        return {f: getattr(s, f) for f, _ in Stats._fields_}
+
+    def reset_stats(self):
+        if self.stats is not None:
+            self.stats.zero_()
+
+
+def _slots(slots, rows):
+    if slots.dtype != torch.int64 or slots.dim() != 1 or slots.numel() != rows or not slots.is_contiguous():
+        raise ValueError("slots must be a contiguous int64 tensor, one per row")
+    return slots.data_ptr()
+
+
+def hq_cache_write(k_plan: Plan, k: torch.Tensor, k_cache: Cache, v_plan, v, v_cache,
+                   slots: torch.Tensor, stream=None):
+    """hq_cache_write: k and v [rows, heads * 128] (bf16 or fp32) into the slots
+    (int64 [rows], negative: skipped) of their caches; v_plan, v and v_cache
+    None: k alone."""
+    rows, width = k.shape[0], k_cache.heads * 128
+    if (v is None) != (v_cache is None) or (v is None) != (v_plan is None):
+        raise ValueError("v_plan, v and v_cache come together")
+    ldk, ldv = _rows(k, width, "k"), 0
+    if v is not None:
+        ldv = _rows(v, width, "v")
+        if v.dtype != k.dtype or v.shape[0] != rows:
+            raise ValueError("k and v must have one dtype and the same rows")
+    _on_device(k, v, slots, k_cache.codes, None if v is None else v_cache.codes)
+    st = lib().hq_cache_write(k_plan.handle, k.data_ptr(), ldk, C.byref(k_cache.c),
+                              None if v is None else v_plan.handle, None if v is None else v.data_ptr(),
+                              ldv, None if v is None else C.byref(v_cache.c), _dtype_code(k.dtype),
+                              rows, _slots(slots, rows), _stream_handle(stream))
+    _check("hq_cache_write", st)
+
+
+def hq_cache_read(plan: Plan, cache: Cache, slots: torch.Tensor, out_dtype=torch.bfloat16, out=None,
+                  stream=None):
+    """hq_cache_read: the rows of the slots (int64, negative: zeros), [rows, heads * 128]."""
+    rows, width = slots.shape[0], cache.heads * 128
+    if out is None:
+        out = torch.empty((rows, width), dtype=out_dtype, device=cache.device)
+    ld = _rows(out, width, "out")
+    if out.shape[0] != rows:
+        raise ValueError("out must have one row per slot")
+    _on_device(slots, out, cache.codes)
+    st = lib().hq_cache_read(plan.handle, C.byref(cache.c), _slots(slots, rows), rows, out.data_ptr(),
+                             _dtype_code(out.dtype), ld, _stream_handle(stream))
+    _check("hq_cache_read", st)
+    return out
+
+
+def hq_cache_attention_workspace_bytes(k_cache: Cache, batch, heads_q, max_blocks):
+    return lib().hq_cache_attention_workspace_bytes(C.byref(k_cache.c), batch, heads_q, max_blocks)
+
+
+def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor,
+                       block_table: torch.Tensor, seq_lens: torch.Tensor, scale=None,
+                       out_dtype=torch.float32, workspace=None, out=None, stream=None):
+    """hq_cache_attention: q [batch, heads_q, 128] (bf16 or fp32) attends over
+    the caches' blocks block_table int32 [batch, max_blocks], seq_lens int32
+    [batch] tokens each.  Returns [batch, heads_q, 128]."""
+    if q.dim() != 3 or q.shape[2] != 128 or not q.is_contiguous():
+        raise ValueError("q must be a contiguous [batch, heads_q, 128]")
+    batch, heads_q = q.shape[0], q.shape[1]
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != batch or \
+            not block_table.is_contiguous():
+        raise ValueError("block_table must be a contiguous int32 [batch, max_blocks]")
+    if seq_lens.dtype != torch.int32 or tuple(seq_lens.shape) != (batch,) or not seq_lens.is_contiguous():
+        raise ValueError("seq_lens must be a contiguous int32 [batch]")
+    max_blocks = block_table.shape[1]
+    if out is None:
+        out = torch.empty((batch, heads_q, 128), dtype=out_dtype, device=q.device)
+    elif out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("out must be a contiguous [batch, heads_q, 128]")
+    if workspace is None:
+        nb = hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)
+        workspace = torch.empty(max(nb, 16), dtype=torch.uint8, device=q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _on_device(q, block_table, seq_lens, out, workspace, k.codes, v.codes)
+    st = lib().hq_cache_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), q.data_ptr(),
+                                  _dtype_code(q.dtype), batch, heads_q,
+                                  128 ** -0.5 if scale is None else scale, block_table.data_ptr(),
+                                  max_blocks, seq_lens.data_ptr(), out.data_ptr(),
+                                  _dtype_code(out.dtype), workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(), _stream_handle(stream))
+    _check("hq_cache_attention", st)
+    return out
+
+
+def _rmsnorm_act_prep(fn, code, plan, x, weight, eps, residual, h, xq, sx, stream):
+    M, K = x.shape[0], plan.cols
+    ldx, ldr, ldh = _rows(x, K, "x"), 0, 0
+    if x.dtype != torch.bfloat16:
+        raise ValueError("x must be bf16")
+    if weight.numel() != K or not weight.is_contiguous():
+        raise ValueError("weight must hold one contiguous value per column")
+    if residual is not None:
+        ldr = _rows(residual, K, "residual")
+        if residual.dtype != torch.bfloat16 or residual.shape[0] != M:
+            raise ValueError("residual must be bf16 with the rows of x")
+        if h is None:
+            h = torch.empty((M, K), dtype=torch.bfloat16, device=x.device)
+    if h is not None:
+        ldh = _rows(h, K, "h")
+        if h.dtype != torch.bfloat16 or h.shape[0] != M:
+            raise ValueError("h must be bf16 with the rows of x")
+    if xq is None:
+        xq = torch.empty((M, K), dtype=code, device=x.device)
+    elif xq.shape != (M, K) or xq.dtype != code or not xq.is_contiguous():
+        raise ValueError(f"xq must be a contiguous {code} [rows, {K}]")
+    if sx is None:
+        sx = torch.empty((M,), dtype=torch.float32, device=x.device)
+    elif sx.shape != (M,) or sx.dtype != torch.float32 or not sx.is_contiguous():
+        raise ValueError("sx must be a contiguous fp32 [rows]")
+    _on_device(x, weight, residual, h, xq, sx)
+    st = getattr(lib(), fn)(plan.handle, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(),
+                            ldr, weight.data_ptr(), _dtype_code(weight.dtype), eps, M,
+                            None if h is None else h.data_ptr(), ldh, xq.data_ptr(), sx.data_ptr(),
+                            _stream_handle(stream))
+    _check(fn, st)
+    return (xq, sx) if residual is None else (xq, sx, h)
+
+
+def hq_rmsnorm_act_prep(plan: Plan, x: torch.Tensor, weight: torch.Tensor, eps=1e-5, residual=None,
+                        h=None, xq=None, sx=None, stream=None):
+    """hq_rmsnorm_act_prep: h = x + residual, then the int8 activation prep of
+    its RMS norm.  Returns (xq, sx), with a residual (xq, sx, h); h may be
+    residual or x itself."""
+    return _rmsnorm_act_prep("hq_rmsnorm_act_prep", torch.int8, plan, x, weight, eps, residual, h, xq,
+                             sx, stream)
+
+
+def hq_rmsnorm_act_prep_fp8(plan: Plan, x: torch.Tensor, weight: torch.Tensor, eps=1e-5,
+                            residual=None, h=None, xq=None, sx=None, stream=None):
+    """hq_rmsnorm_act_prep_fp8: the same in E4M3 (bytes)."""
+    return _rmsnorm_act_prep("hq_rmsnorm_act_prep_fp8", torch.uint8, plan, x, weight, eps, residual, h,
+                             xq, sx, stream)
+
+
 def hq_rice_kstar(count, total):
     return lib().hq_rice_kstar(int(count), int(total))
 
@@ -519,5 +727,7 @@ EXPORTED = ["hq_plan", "hq_plan_destroy", "hq_plan_get_info", "hq_scan_bytes", "
             "hq_decode_gemv", "hq_attention_workspace_bytes", "hq_decode_attention",
             "hq_decode_fp8", "hq_act_prep_fp8", "hq_gemm_fp8_blockscaled",
             "hq_decode_mxfp4", "hq_act_prep_mxfp4", "hq_gemm_mxfp4_blockscaled",
+            "hq_cache_write", "hq_cache_read", "hq_cache_attention_workspace_bytes",
+            "hq_cache_attention", "hq_rmsnorm_act_prep", "hq_rmsnorm_act_prep_fp8",
             "hq_rice_kstar",
             "hq_calibrated_snr", "hq_status_string"]
