@@ -506,7 +506,7 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
  * cache: out[b, h] = sum_t softmax_t(scale q[b, h] . k^_t) v^_t, k^ and v^ the rows
  * hq_cache_read would return in fp32.  The query is moved into the stored
  * coordinates once and the value sum back once; nothing is materialized.
- *   k, v         caches of one format, heads, block_tokens and blocks.
+ *   k, v         caches of one format, heads, block_tokens and blocks (one at least).
  *   q            device [batch, heads_q, 128], HQ_BF16 or HQ_FP32, 16-byte
  *                aligned; head h reads KV head h / (heads_q / heads), a group of
  *                1 .. 16 (HQ_ERR_UNSUPPORTED above).
@@ -520,12 +520,11 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
  *   out          device [batch, heads_q, 128], HQ_FP32 or HQ_BF16 (round to
  *                nearest even), 16-byte aligned.
  *   workspace    device, 16-byte aligned, >= hq_cache_attention_workspace_bytes(
- *                k, batch, heads_q, max_blocks); not read or written, and may be
- *                null, where that call's tokens are not split.  Calls that may
- *                overlap (on two streams, or two captured graphs that may) need
- *                one each.
- * Scores, maxima and sums are fp32, in an order fixed by the call's shape and the
- * sequence's length, so results repeat bit for bit.  Device-side, in k->stats: a
+ *                k, batch, heads_q, max_blocks); may be null where max_blocks *
+ *                block_tokens is at most 512.  Calls that may overlap (on two
+ *                streams, or two captured graphs that may) need one each.
+ * Scores, maxima and sums are fp32, in an order fixed by the call's shape and its
+ * lengths, so results repeat bit for bit.  Device-side, in k->stats: a
  * length outside 0 .. max_blocks * block_tokens is clamped, tokens of a block id
  * outside the cache are left out (both HQ_ERR_INVALID_ARG).  Host errors:
  * HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (max_blocks * block_tokens above 2^30),

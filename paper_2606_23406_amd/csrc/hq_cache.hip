@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include "hq_device.h"
+#include "hq_lds.h"
 
 #pragma clang fp contract(off)
 
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
 
 // ----------------------------------------------------------------- attention
 // One workgroup takes one KV head of one sequence and a run of its tokens (a
-// split), each wave 32 tokens at a time.  Both products run on the matrix cores in
+// chunk), each wave 32 tokens at a time.  Both products run on the matrix cores in
 // bf16, which holds every code of the three formats exactly; the query and the
 // weights enter as three bf16 terms each (8 + 8 + 8 bits, by truncation: their sum is
 // the fp32 value itself), so the sums are fp32 sums.
@@ -265,117 +266,384 @@ __device__ __forceinline__ void pairs_of(uint32_t w, float f, uint32_t* o) {
   }
 }
 
-// What a wave loads for 32 tokens.
+// ---- who does what
+// The tokens of a call are cut into chunks, about HQ_CACHE_WG_TARGET workgroups'
+// worth over all sequences and KV heads, so that a batch of uneven lengths keeps the
+// chip as busy as an even one.  Item j of the list is chunk j - first of sequence b.
+// Every wave finds its item by itself: 64 lengths a step, one per lane.
+struct CacheItem {
+  int32_t b;       // -1: behind the last item
+  int32_t n;       // chunks of this sequence (an empty one has one, which writes its zeros)
+  int64_t first;   // the sequence's first item
+  int32_t len, chunk;
+};
+
+__device__ __forceinline__ int32_t cache_len(const hq_cache_attn_args& A, int64_t b, bool tell) {
+  const int64_t cap = (int64_t)A.max_blocks * A.block_tokens;
+  const int64_t len = A.seq_lens[b];
+  if (len >= 0 && len <= cap) return (int32_t)len;
+  if (tell) report(A.stats, HQ_ERR_INVALID_ARG);
+  return len < 0 ? 0 : (int32_t)cap;
+}
+
+// Chunks hold whole steps of four waves: multiples of 128 tokens, HQ_CACHE_LEAST at
+// least, one of 2^30 for any sequence.
+__device__ __forceinline__ int32_t cache_chunk(const hq_cache_attn_args& A, int lane, bool tell) {
+  int64_t total = 0;
+  for (int64_t i = lane; i < A.batch; i += 64) total += cache_len(A, i, tell);
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
+  const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
+  const int64_t chunk = min((even + 127) & ~(int64_t)127, (int64_t)1 << 30);
+  return (int32_t)readfirst((uint32_t)(chunk < HQ_CACHE_LEAST ? HQ_CACHE_LEAST : chunk));
+}
+
+// By item (j >= 0) or by sequence (j < 0).
+__device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int64_t j, int64_t b, int lane,
+                                                bool tell) {
+  CacheItem it;
+  it.chunk = cache_chunk(A, lane, tell);
+  it.b = -1;
+  int64_t base = 0;
+  for (int64_t i0 = 0; i0 < A.batch; i0 += 64) {
+    const bool in = i0 + lane < A.batch;
+    const int32_t len = in ? cache_len(A, i0 + lane, false) : 0;
+    const uint32_t n = !in ? 0u : len == 0 ? 1u : ((uint32_t)len + it.chunk - 1) / (uint32_t)it.chunk;
+    const uint32_t incl = wave_scan_incl(n), all = __builtin_amdgcn_readlane(incl, 63);
+    if (j >= 0 ? j < base + all : b < i0 + 64) {
+      const int at = j >= 0 ? __popcll(__ballot(base + incl <= j)) : (int)(b - i0);
+      it.b = (int32_t)i0 + at;
+      it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
+      it.first = base + (uint32_t)__builtin_amdgcn_readlane(incl, at) - it.n;
+      it.len = __builtin_amdgcn_readlane(len, at);
+      break;
+    }
+    base += all;
+  }
+  return it;
+}
+
+// ---- a wave's tokens
+// A wave's tokens come through LDS, loaded there straight from memory (no register
+// waits for them) in a ring of two steps of 32 tokens, each two halves of 16: the key
+// codes, the value codes, and the 64 bytes of scales of each.  A row's 16-byte chunks are
+// permuted by its index, which the loads' source addresses do, so that the reads
+// below meet no bank twice.
+template <int FMT>
+struct CacheRing {
+  static constexpr int RB = row_bytes<FMT>();
+  static constexpr int V = 16 * RB, SCALES = 32 * RB;      // places in a half
+  static constexpr int HALF = SCALES + 512, STEP = 2 * HALF, WAVE = 2 * STEP;
+  static constexpr int LOADS = 2 * (2 * (16 * RB / 1024) + 2);  // of a step
+  // 16-byte chunk c of row r lies at chunk c ^ swizzle(r)
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t r) { return FMT == kMx ? (r >> 1) & 3 : r & 7; }
+};
+
+// One step's codes and scales in registers.
 template <int FMT>
 struct CacheStep {
   static constexpr int KW = FMT == kMx ? 4 : 8;  // words of 32 codes
   static constexpr int VW = FMT == kMx ? 1 : 2;  // words of 8 codes
-  uint32_t k[2][KW];     // token 16 h + l % 16, dims 32 (l / 16) ..
-  uint32_t v[2][4][VW];  // token 16 h + 4 (l / 16) + r, dims 8 (l % 16) ..
+  uint32_t k[2][KW];         // token 16 h + l % 16, dims 32 (l / 16) ..
+  uint32_t v[2][4][VW];      // token 16 h + 4 (l / 16) + r, dims 8 (l % 16) ..
   float ks[2][4], vs[2][4];  // fp32 scales of those four tokens
   uint32_t kx[2], vx[2][4];  // MXFP4: the scale byte of k, the four bytes of v's tokens
-  int32_t live[2];           // tokens of each half to attend to
 };
 
+typedef __attribute__((address_space(3))) void lds_void;
+
+// A run of `bytes` from p on as a buffer resource (p the same in every lane).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t run_of(const uint8_t* p, uint32_t bytes) {
+  const uint64_t a = (uint64_t)p;
+  const uint64_t u = (uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)u, 0, bytes, 0x00020000);
+}
+
+// Where a wave stands in its sequence: block blk of the table row, token off of it.
+// The ids of 64 blocks ahead are one per lane, so that following the table costs a
+// lane read and not a load that the next loads' addresses wait for.
 struct CacheWalk {
-  int32_t blk, off;  // block of the table and token inside it
-  __device__ __forceinline__ void advance(int32_t by, int32_t bt) {
-    off += by;
-    while (off >= bt) {
-      off -= bt;
+  const int32_t* table;
+  int32_t last;  // the sequence's last block
+  int32_t blk, off;
+  int32_t first, ids;  // lane l: block first + l
+  __device__ __forceinline__ void fetch(int lane) {
+    first = blk;
+    ids = table[min(blk + lane, last)];
+  }
+  __device__ __forceinline__ int32_t id(int lane) {
+    if (blk - first >= 64) fetch(lane);
+    return __builtin_amdgcn_readlane(ids, blk - first);
+  }
+  __device__ __forceinline__ void advance(int32_t bt) {  // by 16 tokens, which divide a block
+    off += 16;
+    if (off == bt) {
+      off = 0;
       ++blk;
     }
   }
 };
 
+// Starts the loads of the 32 tokens from t on into `step` (LDS) and moves the walk
+// past them; live[h]: tokens of each half to attend to.
 template <int FMT>
-__device__ __forceinline__ void cache_load(const hq_cache_attn_args& A, const int32_t* table, int32_t head,
-                                           CacheWalk w, int32_t t, int32_t end, int lane, CacheStep<FMT>& s) {
-  const int n = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void cache_fetch(const hq_cache_attn_args& A, int32_t head, CacheWalk& w, int32_t t,
+                                            int32_t end, int lane, uint8_t* step, int32_t (&live)[2]) {
+  using R = CacheRing<FMT>;
+  constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
+  const uint32_t row_in = lane / CPR, chunk = lane % CPR;
+  const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    int32_t live = end - t - 16 * h;
-    live = live < 0 ? 0 : live > 16 ? 16 : live;
-    int32_t b = 0;
-    if (live > 0) {
-      b = table[w.blk];
+    // dead halves (behind the end, or of a block outside the cache) load the cache's
+    // first tokens, so that a step is always the same loads; nothing reads them
+    int32_t b = 0, off = 0;
+    live[h] = min(max(end - t - 16 * h, 0), 16);
+    if (live[h] > 0) {
+      b = w.id(lane);
+      off = w.off;
       if (b < 0 || b >= A.blocks) {
-        live = 0;
+        live[h] = b = off = 0;
         if (head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
       }
+      w.advance(A.block_tokens);
     }
-    s.live[h] = live;
-    if (live > 0) {
-      const int64_t row = ((int64_t)b * A.heads_kv + head) * A.block_tokens + w.off;
-      const uint8_t* kp = A.k_codes + (row + n) * row_bytes<FMT>() + g * (row_bytes<FMT>() / 4);
-      const uint8_t* vp = A.v_codes + (row + 4 * g) * row_bytes<FMT>() + n * (row_bytes<FMT>() / 16);
+    const int64_t row = ((int64_t)b * A.heads_kv + head) * A.block_tokens + off;
+    const __amdgpu_buffer_rsrc_t kr = run_of(A.k_codes + row * R::RB, 16 * R::RB);
+    const __amdgpu_buffer_rsrc_t vr = run_of(A.v_codes + row * R::RB, 16 * R::RB);
+    const __amdgpu_buffer_rsrc_t ksr = run_of((const uint8_t*)A.k_scales + row * 4, 64);
+    const __amdgpu_buffer_rsrc_t vsr = run_of((const uint8_t*)A.v_scales + row * 4, 64);
+    uint8_t* to = step + h * R::HALF;
 #pragma unroll
-      for (int i = 0; i < CacheStep<FMT>::KW; i += 4) {
-        const uint4 x = *(const uint4*)(kp + 4 * i);
-        s.k[h][i] = x.x; s.k[h][i + 1] = x.y; s.k[h][i + 2] = x.z; s.k[h][i + 3] = x.w;
+    for (uint32_t i = 0; i < 16 / RPL; ++i) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(to + i * 1024), 16, from, i * 1024, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(to + R::V + i * 1024), 16, from, i * 1024, 0, 0);
+    }
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(ksr, (lds_void*)(to + R::SCALES), 4, lane * 4, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(vsr, (lds_void*)(to + R::SCALES + 256), 4, lane * 4, 0, 0, 0);
+  }
+}
+
+// A step's codes and scales out of LDS.
+template <int FMT>
+__device__ __forceinline__ void cache_take(const uint8_t* step, int lane, CacheStep<FMT>& s) {
+  using R = CacheRing<FMT>;
+  const uint32_t n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint8_t* half = step + h * R::HALF;
+#pragma unroll
+    for (int i = 0; i < CacheStep<FMT>::KW; i += 4) {
+      const uint32_t chunk = (FMT == kMx ? g : 2 * g + i / 4) ^ R::swizzle(n);
+      const uint4 x = *(const uint4*)(half + n * R::RB + chunk * 16);
+      s.k[h][i] = x.x; s.k[h][i + 1] = x.y; s.k[h][i + 2] = x.z; s.k[h][i + 3] = x.w;
+    }
+    const uint8_t* sc = half + R::SCALES;
+    if constexpr (FMT == kMx) {
+      s.kx[h] = sc[4 * n + g];
+      const uint4 x = *(const uint4*)(sc + 256 + 16 * g);
+      s.vx[h][0] = x.x; s.vx[h][1] = x.y; s.vx[h][2] = x.z; s.vx[h][3] = x.w;
+    } else {
+      const float4 x = *(const float4*)(sc + 16 * g);
+      const float4 y = *(const float4*)(sc + 256 + 16 * g);
+      s.ks[h][0] = x.x; s.ks[h][1] = x.y; s.ks[h][2] = x.z; s.ks[h][3] = x.w;
+      s.vs[h][0] = y.x; s.vs[h][1] = y.y; s.vs[h][2] = y.z; s.vs[h][3] = y.w;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t row = 4 * g + r;
+      if constexpr (FMT == kMx) {
+        s.v[h][r][0] = *(const uint32_t*)(half + R::V + row * R::RB + ((n >> 2) ^ R::swizzle(row)) * 16 + (n & 3) * 4);
+      } else {
+        const uint2 x = *(const uint2*)(half + R::V + row * R::RB + ((n >> 1) ^ R::swizzle(row)) * 16 + (n & 1) * 8);
+        s.v[h][r][0] = x.x; s.v[h][r][1] = x.y;
+      }
+    }
+  }
+}
+
+// The state that a wave carries over its tokens: per lane the maximum and sum of
+// its column's scores, and the values' sum, acc[j][r] dim 8 (4 (l / 16) + r) + j.
+struct CacheState {
+  float m, l;
+  v4_t acc[8];
+};
+
+// One step: 32 tokens' scores, the running maximum and sum, their values' sum.
+// PACK: column l % 16 is term l % 4 of head (l / 4) % 4.  Otherwise it is a head, and the
+// terms are three products.
+template <int FMT, bool PACK>
+__device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&live)[2],
+                                           const uint32_t (&q)[PACK ? 1 : 3][4][4], int lane, CacheState& z) {
+  constexpr int T = PACK ? 1 : 3;
+  const int n = lane & 15, g = lane >> 4;
+  if (live[0] + live[1] < 32) {
+    // stale or absent tokens: their value codes count as zeros (their weight is
+    // zero, but a stale code or scale may be a NaN)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (4 * g + r >= live[h]) {
+#pragma unroll
+          for (int i = 0; i < CacheStep<FMT>::VW; ++i) cur.v[h][r][i] = 0u;
+          cur.ks[h][r] = cur.vs[h][r] = 0.0f;
+          cur.vx[h][r] = 0x7F7F7F7Fu;
+        }
+  }
+  float p[2][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float f = FMT == kMx ? __uint_as_float(cur.kx[h] << 23) : 1.0f;
+    v4_t c[T];
+#pragma unroll
+    for (int i = 0; i < T; ++i) c[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      uint32_t a[4];
+      if constexpr (FMT == kMx) {
+        pairs_of<FMT>(cur.k[h][s], f, a);
+      } else {
+        pairs_of<FMT>(cur.k[h][2 * s], f, a);
+        pairs_of<FMT>(cur.k[h][2 * s + 1], f, a + 2);
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if constexpr (FMT == kMx) {
-          s.v[h][r][0] = *(const uint32_t*)(vp + r * row_bytes<FMT>());
-        } else {
-          const uint2 x = *(const uint2*)(vp + r * row_bytes<FMT>());
-          s.v[h][r][0] = x.x; s.v[h][r][1] = x.y;
+      for (int i = 0; i < T; ++i) c[i] = mfma_bf16(a, q[i][s], c[i]);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float x = PACK ? c[0][r] : c[0][r] + (c[T / 2][r] + c[T - 1][r]);
+      if constexpr (PACK) {  // the terms' sum, in each lane of the head's four
+        x += dpp_xor<1>(x);
+        x += dpp_xor<2>(x);
+      }
+      p[h][r] = FMT == kMx ? x : x * cur.ks[h][r];
+    }
+  }
+  if (live[0] + live[1] < 32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (4 * g + r >= live[h]) p[h][r] = -__builtin_inff();
+  }
+  float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(p[0][0], p[0][1]), __builtin_fmaxf(p[0][2], p[0][3])),
+                              __builtin_fmaxf(__builtin_fmaxf(p[1][0], p[1][1]), __builtin_fmaxf(p[1][2], p[1][3])));
+  top = __builtin_fmaxf(top, swz_xor16(top));
+  top = __builtin_fmaxf(top, lane_xor32(top));
+  if (__ballot(top > z.m)) {  // some column has a new maximum: all sums move to theirs
+    const float mn = __builtin_fmaxf(z.m, top);
+    const float alpha = __builtin_amdgcn_exp2f(z.m - (mn == -__builtin_inff() ? 0.0f : mn));
+    z.m = mn;
+    z.l *= alpha;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z.acc[j] *= alpha;
+  }
+  const float ref = z.m == -__builtin_inff() ? 0.0f : z.m;  // nothing seen yet
+  uint32_t pt[T][4];  // the weights' terms: k index 4 h + r
+  const uint32_t cut1 = PACK && (n & 3) < 1 ? 0u : 0xFFFF0000u, cut2 = PACK && (n & 3) < 2 ? 0u : 0xFFFF0000u;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t tt[4][T];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float e = __builtin_amdgcn_exp2f(p[h][r] - ref);
+      z.l += e;
+      const float x = FMT == kMx ? e : e * cur.vs[h][r];
+      if constexpr (PACK) {  // the column's own term
+        const float y = x - __uint_as_float(__float_as_uint(x) & cut1);
+        tt[r][0] = __float_as_uint(y - __uint_as_float(__float_as_uint(y) & cut2));
+      } else {
+        three_terms(x, tt[r]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      pt[i][2 * h] = high_pair(tt[0][i], tt[1][i]);
+      pt[i][2 * h + 1] = high_pair(tt[2][i], tt[3][i]);
+    }
+  }
+  // value codes: per token words of two dims, then per dim the tokens' pairs
+#pragma unroll
+  for (int w = 0; w < CacheStep<FMT>::VW; ++w) {
+    constexpr int D = 4 / CacheStep<FMT>::VW;  // pairs of dims in a word
+    uint32_t vf[2 * D][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        uint32_t x[2][D];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          pairs_of<FMT>(cur.v[h][r + e][w],
+                        FMT == kMx ? __uint_as_float(((cur.vx[h][r + e] >> (8 * (n >> 2))) & 0xFFu) << 23) : 1.0f, x[e]);
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+          vf[2 * d][2 * h + r / 2] = __builtin_amdgcn_perm(x[1][d], x[0][d], 0x05040100u);
+          vf[2 * d + 1][2 * h + r / 2] = high_pair(x[0][d], x[1][d]);
         }
       }
-      if constexpr (FMT == kMx) {
-        s.kx[h] = ((const uint8_t*)A.k_scales)[(row + n) * 4 + g];
-        const uint4 x = *(const uint4*)((const uint8_t*)A.v_scales + (row + 4 * g) * 4);
-        s.vx[h][0] = x.x; s.vx[h][1] = x.y; s.vx[h][2] = x.z; s.vx[h][3] = x.w;
-      } else {
-        const float4 x = *(const float4*)((const float*)A.k_scales + row + 4 * g);
-        const float4 y = *(const float4*)((const float*)A.v_scales + row + 4 * g);
-        s.ks[h][0] = x.x; s.ks[h][1] = x.y; s.ks[h][2] = x.z; s.ks[h][3] = x.w;
-        s.vs[h][0] = y.x; s.vs[h][1] = y.y; s.vs[h][2] = y.z; s.vs[h][3] = y.w;
-      }
-    }
-    w.advance(16, A.block_tokens);
+#pragma unroll
+    for (int i = T - 1; i >= 0; --i)
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) z.acc[2 * D * w + j] = mfma_bf16(vf[j], pt[i], z.acc[2 * D * w + j]);
   }
 }
 
 constexpr int kQPitch = HQ_TILE + 8;  // bf16 of a query row in LDS
 constexpr int kOPitch = HQ_TILE + 4;  // floats of an output row in LDS
 
-template <int FMT>
+// v * 1 / (128 sum) moved back to the head's own coordinates.
+__device__ __forceinline__ void cache_finish(const hq_cache_attn_args& A, float L, float* v, int32_t head, int lane) {
+  const float inv = L == 0.0f ? 0.0f : 1.0f / (L * 128.0f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= inv;
+  const XSigns sg(lane);
+  fwht128(v, sg);
+  const uint32_t dbits = sign_bits8(A.v_dmask, (int64_t)head * HQ_TILE + (lane & 15) * 8);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = flip(v[i], dbits, i);
+}
+
+template <int FMT, bool PACK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_attn_kernel(
     hq_cache_attn_args A) {
-  __shared__ __attribute__((aligned(16))) float s_o[HQ_WAVES_PER_WG][16][kOPitch];
-  __shared__ float s_m[HQ_WAVES_PER_WG][16], s_l[HQ_WAVES_PER_WG][16];
-  uint16_t* s_q = (uint16_t*)&s_o[0][0][0];  // the query's terms, before the sums
-  static_assert(3 * 16 * kQPitch * sizeof(uint16_t) <= sizeof(s_o), "the query fits the sums' place");
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  using R = CacheRing<FMT>;
+  constexpr int HEADS = PACK ? 4 : 16, T = PACK ? 1 : 3;
+  extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];  // a wave's ring after the other
+  __shared__ float s_m[HQ_WAVES_PER_WG][HEADS], s_l[HQ_WAVES_PER_WG][HEADS];
+  // term i of the query lies in the second step of wave i's ring until that is first
+  // loaded, a wave's sums in its own ring at the end
+  static_assert(16 * kQPitch * sizeof(uint16_t) <= R::STEP && HEADS * kOPitch * sizeof(float) <= R::WAVE, "");
+  auto q_row = [&](int term, int row) { return (uint16_t*)(s_ring + term * R::WAVE + R::STEP) + row * kQPitch; };
+  auto o_row = [&](int w, int row) { return (float*)(s_ring + w * R::WAVE) + row * kOPitch; };
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4, grp = tid >> 4;
   const int wave = (int)readfirst((uint32_t)(tid >> 6));
-  const uint32_t bh = blockIdx.x / (uint32_t)A.splits;
-  const int32_t split = (int32_t)(blockIdx.x - bh * (uint32_t)A.splits);
-  const int64_t b = bh / (uint32_t)A.heads_kv;
-  const int32_t head = (int32_t)(bh - (uint32_t)b * (uint32_t)A.heads_kv);
-  const int32_t G = A.group;
-  const int64_t cap = (int64_t)A.max_blocks * A.block_tokens;
-  int64_t len64 = A.seq_lens[b];
-  if (len64 < 0 || len64 > cap) {
-    if (split == 0 && head == 0 && tid == 0) report(A.stats, HQ_ERR_INVALID_ARG);
-    len64 = len64 < 0 ? 0 : cap;
-  }
-  const int32_t len = (int32_t)len64;
-  // the sequence's own tokens are shared out evenly, 128 (32 a wave) at least
-  int32_t chunk = (int32_t)(((len64 + A.splits - 1) / A.splits + 127) & ~(int64_t)127);
-  const int64_t begin64 = (int64_t)split * chunk;
-  const int64_t pair0 = b * A.heads_q + (int64_t)head * G;
-  if (begin64 >= len) {  // nothing here; the first split of an empty sequence still answers
-    if (A.splits > 1) return;  // the join knows how many splits a length has
-    const int grp = tid >> 4;
-    const float z[8] = {};
-    if (grp < G) store8(A.out, (pair0 + grp) * HQ_TILE + n * 8, A.out_bf16, z);
+  const uint32_t j = blockIdx.x / (uint32_t)A.heads_kv;
+  const int32_t head = (int32_t)(blockIdx.x - j * (uint32_t)A.heads_kv);
+  const CacheItem it = cache_item(A, j, 0, lane, blockIdx.x == 0 && wave == 0);
+  if (it.b < 0) return;
+  const int32_t G = A.group, c0 = n * 8;
+  const int64_t pair0 = (int64_t)it.b * A.heads_q + (int64_t)head * G;
+  if (it.len == 0) {
+    const float zero[8] = {};
+    if (grp < G) store8(A.out, (pair0 + grp) * HQ_TILE + c0, A.out_bf16, zero);
     return;
   }
+  const int32_t per = it.chunk / HQ_WAVES_PER_WG;
+  const int64_t begin64 = (j - it.first) * it.chunk + wave * per;
+  const int32_t begin = (int32_t)min(begin64, (int64_t)it.len), end = min(it.len, begin + per);
+  CacheWalk w;
+  w.table = A.table + (int64_t)it.b * A.max_blocks;
+  w.last = (it.len - 1) / A.block_tokens;
+  w.blk = begin / A.block_tokens;
+  w.off = begin - w.blk * A.block_tokens;
+  w.fetch(lane);
+  uint8_t* ring = s_ring + wave * R::WAVE;
+  int32_t live[2], next[2] = {0, 0};
+  if (begin < end) cache_fetch<FMT>(A, head, w, begin, end, lane, ring, live);
   // ---- the query into the cache's coordinates, as three bf16 terms
-  {
-    const int grp = tid >> 4, c0 = n * 8;
+  if (grp < HEADS || !PACK) {
     float v[8] = {};
     if (grp < G) {
       load8(A.q, (pair0 + grp) * HQ_TILE + c0, A.q_bf16, v);
@@ -395,150 +663,87 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       o.y = high_pair(t[2][i], t[3][i]);
       o.z = high_pair(t[4][i], t[5][i]);
       o.w = high_pair(t[6][i], t[7][i]);
-      *(uint4*)(s_q + (i * 16 + grp) * kQPitch + c0) = o;
+      *(uint4*)((PACK ? q_row(0, grp * 4 + i) : q_row(i, grp)) + c0) = o;
     }
+    if (PACK) *(uint4*)(q_row(0, grp * 4 + 3) + c0) = make_uint4(0u, 0u, 0u, 0u);
   }
   __syncthreads();
   // step s of the contraction takes dims 32 (l / 16) + 8 s + j in lane l (the codes
   // that the lane's one run of 32 holds)
-  uint32_t q[3][4][4];
+  uint32_t q[T][4][4];
 #pragma unroll
-  for (int i = 0; i < 3; ++i)
+  for (int i = 0; i < T; ++i)
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const uint4 x = *(const uint4*)(s_q + (i * 16 + n) * kQPitch + 32 * g + 8 * s);
+      const uint4 x = *(const uint4*)(q_row(i, n) + 32 * g + 8 * s);
       q[i][s][0] = x.x; q[i][s][1] = x.y; q[i][s][2] = x.z; q[i][s][3] = x.w;
     }
-  __syncthreads();  // s_o takes the query's place
+  __syncthreads();  // the query's place is loaded over
 
-  v4_t acc[8];
+  CacheState z;
+  z.m = -__builtin_inff();
+  z.l = 0.0f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  float m = -__builtin_inff(), l = 0.0f;
-  const int32_t per = chunk / HQ_WAVES_PER_WG;
-  const int32_t begin = (int32_t)begin64 + wave * per;
-  const int32_t end = min(len, begin + per);
-  const int32_t* table = A.table + b * A.max_blocks;
-  CacheWalk w;
-  w.blk = begin / A.block_tokens;
-  w.off = begin - w.blk * A.block_tokens;
-  CacheStep<FMT> cur;
-  if (begin < end) cache_load<FMT>(A, table, head, w, begin, end, lane, cur);
+  for (int i = 0; i < 8; ++i) z.acc[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
+  if (begin + 32 < end) cache_fetch<FMT>(A, head, w, begin + 32, end, lane, ring + R::STEP, next);
+  int32_t slot = 0;
   for (int32_t t = begin; t < end; t += 32) {
-    CacheStep<FMT> nxt;
-    w.advance(32, A.block_tokens);
-    if (t + 32 < end) cache_load<FMT>(A, table, head, w, t + 32, end, lane, nxt);
-    if (cur.live[0] + cur.live[1] < 32) {
-      // stale or absent tokens: their value codes count as zeros (their weight is
-      // zero, but a stale code or scale may be a NaN)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (4 * g + r >= cur.live[h]) {
-#pragma unroll
-            for (int i = 0; i < CacheStep<FMT>::VW; ++i) cur.v[h][r][i] = 0u;
-            cur.ks[h][r] = cur.vs[h][r] = 0.0f;
-            cur.vx[h][r] = 0x7F7F7F7Fu;
-          }
+    // the loads of this step are done when at most the next step's are not
+    if (t + 32 < end)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    CacheStep<FMT> cur;
+    cache_take<FMT>(ring + slot * R::STEP, lane, cur);
+    const int32_t here[2] = {live[0], live[1]};
+    live[0] = next[0];
+    live[1] = next[1];
+    if (t + 64 < end) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
+      cache_fetch<FMT>(A, head, w, t + 64, end, lane, ring + slot * R::STEP, next);
     }
-    float p[2][4];
-    float top = -__builtin_inff();
+    slot ^= 1;
+    cache_step<FMT, PACK>(cur, here, q, lane, z);
+  }
+  z.l += swz_xor16(z.l);
+  z.l += lane_xor32(z.l);
+  // ---- the four waves' sums under one maximum, one head per 16 lanes
+  if constexpr (PACK) {
+    // the terms' sums: in the fourth lane of a head the weights' columns were a term over again
+    const float keep = (n & 3) == 3 ? 0.0f : 1.0f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float f = FMT == kMx ? e8m0(cur.kx[h]) : 1.0f;
-      v4_t c = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-      uint32_t a[4][4];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        if constexpr (FMT == kMx) {
-          pairs_of<FMT>(cur.k[h][s], f, a[s]);
-        } else {
-          pairs_of<FMT>(cur.k[h][2 * s], f, a[s]);
-          pairs_of<FMT>(cur.k[h][2 * s + 1], f, a[s] + 2);
-        }
-      }
-#pragma unroll
-      for (int i = 2; i >= 0; --i)  // the small terms first
-#pragma unroll
-        for (int s = 0; s < 4; ++s) c = mfma_bf16(a[s], q[i][s], c);
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float x = FMT == kMx ? c[r] : c[r] * cur.ks[h][r];
-        if (4 * g + r >= cur.live[h]) x = -__builtin_inff();
-        p[h][r] = x;
-        top = __builtin_fmaxf(top, x);
+        float x = keep == 0.0f ? 0.0f : z.acc[i][r];
+        x += dpp_xor<1>(x);
+        z.acc[i][r] = x + dpp_xor<2>(x);
       }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if ((n & 3) == r) {
+        float* o = o_row(wave, n >> 2) + (4 * g + r) * 8;
+        *(float4*)o = make_float4(z.acc[0][r], z.acc[1][r], z.acc[2][r], z.acc[3][r]);
+        *(float4*)(o + 4) = make_float4(z.acc[4][r], z.acc[5][r], z.acc[6][r], z.acc[7][r]);
+      }
+    if (g == 0 && (n & 3) == 0) {
+      s_m[wave][n >> 2] = z.m;
+      s_l[wave][n >> 2] = z.l;
     }
-    top = __builtin_fmaxf(top, swz_xor16(top));
-    top = __builtin_fmaxf(top, lane_xor32(top));
-    const float mn = __builtin_fmaxf(m, top);
-    const float ref = mn == -__builtin_inff() ? 0.0f : mn;  // nothing seen yet
-    const float alpha = __builtin_amdgcn_exp2f(m - ref);
-    m = mn;
-    l *= alpha;
+  } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] *= alpha;
-    uint32_t pt[3][4];  // the weights' terms: k index 4 h + r
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t tt[4][3];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float e = __builtin_amdgcn_exp2f(p[h][r] - ref);
-        l += e;
-        three_terms(FMT == kMx ? e : e * cur.vs[h][r], tt[r]);
-      }
-#pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        pt[i][2 * h] = high_pair(tt[0][i], tt[1][i]);
-        pt[i][2 * h + 1] = high_pair(tt[2][i], tt[3][i]);
-      }
+    for (int r = 0; r < 4; ++r) {
+      float* o = o_row(wave, n) + (4 * g + r) * 8;
+      *(float4*)o = make_float4(z.acc[0][r], z.acc[1][r], z.acc[2][r], z.acc[3][r]);
+      *(float4*)(o + 4) = make_float4(z.acc[4][r], z.acc[5][r], z.acc[6][r], z.acc[7][r]);
     }
-    // value codes: per token four words of two dims each, then per dim the tokens' pairs
-    uint32_t vf[8][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        uint32_t x[2][4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if constexpr (FMT == kMx) {
-            pairs_of<FMT>(cur.v[h][r + e][0], e8m0((cur.vx[h][r + e] >> (8 * (n >> 2))) & 0xFFu), x[e]);
-          } else {
-            pairs_of<FMT>(cur.v[h][r + e][0], 1.0f, x[e]);
-            pairs_of<FMT>(cur.v[h][r + e][1], 1.0f, x[e] + 2);
-          }
-        }
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          vf[2 * d][2 * h + r / 2] = __builtin_amdgcn_perm(x[1][d], x[0][d], 0x05040100u);
-          vf[2 * d + 1][2 * h + r / 2] = high_pair(x[0][d], x[1][d]);
-        }
-      }
-#pragma unroll
-    for (int i = 2; i >= 0; --i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = mfma_bf16(vf[j], pt[i], acc[j]);
-    cur = nxt;
-  }
-  l += swz_xor16(l);
-  l += lane_xor32(l);
-  // acc[j][r] is dim 8 (4 g + r) + j of head n
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    float* o = &s_o[wave][n][(4 * g + r) * 8];
-    *(float4*)o = make_float4(acc[0][r], acc[1][r], acc[2][r], acc[3][r]);
-    *(float4*)(o + 4) = make_float4(acc[4][r], acc[5][r], acc[6][r], acc[7][r]);
-  }
-  if (g == 0) {
-    s_m[wave][n] = m;
-    s_l[wave][n] = l;
+    if (g == 0) {
+      s_m[wave][n] = z.m;
+      s_l[wave][n] = z.l;
+    }
   }
   __syncthreads();
-  // ---- the four waves' sums under one maximum, one head per 16 lanes
-  const int grp = tid >> 4, c0 = n * 8;
+  if (grp >= G) return;
   float M = s_m[0][grp], L = 0.0f, v[8] = {};
 #pragma unroll
   for (int x = 1; x < HQ_WAVES_PER_WG; ++x) M = __builtin_fmaxf(M, s_m[x][grp]);
@@ -548,11 +753,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     const float f = __builtin_amdgcn_exp2f(s_m[x][grp] - ref);
     L = __builtin_fmaf(f, s_l[x][grp], L);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(f, s_o[x][grp][c0 + i], v[i]);
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(f, o_row(x, grp)[c0 + i], v[i]);
   }
-  if (A.splits > 1) {
-    if (grp >= G) return;
-    const int64_t part = (pair0 + grp) * A.splits + split;
+  if (it.n > 1) {
+    const int64_t part = ((int64_t)j * A.heads_kv + head) * G + grp;
     store8(A.part_acc, part * HQ_TILE + c0, false, v);
     if (n == 0) {
       A.part_m[part] = M;
@@ -560,47 +764,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     }
     return;
   }
-  const float inv = L == 0.0f ? 0.0f : 1.0f / (L * 128.0f);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] *= inv;
-  const XSigns sg(lane);
-  fwht128(v, sg);
-  if (grp >= G) return;
-  const uint32_t dbits = sign_bits8(A.v_dmask, (int64_t)head * HQ_TILE + c0);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = flip(v[i], dbits, i);
+  cache_finish(A, L, v, head, lane);
   store8(A.out, (pair0 + grp) * HQ_TILE + c0, A.out_bf16, v);
 }
 
-// Joins a query head's splits under one maximum, in order, and moves the result
-// back: one workgroup per query head, 16 lanes per split.
+// Joins a query head's chunks under one maximum, in order, and moves the result
+// back: one workgroup per query head, 16 lanes per chunk.
 __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A) {
   __shared__ float s_red[16];
   __shared__ float4 s_acc[16][32];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4, c0 = n * 8;
   const int64_t pair = blockIdx.x;
   const int64_t b = pair / A.heads_q;
-  const int32_t head = (int32_t)(pair - b * A.heads_q) / A.group;
-  const int64_t cap = (int64_t)A.max_blocks * A.block_tokens;
-  int64_t len = A.seq_lens[b];
-  len = len < 0 ? 0 : len > cap ? cap : len;
-  const int64_t chunk = ((len + A.splits - 1) / A.splits + 127) & ~(int64_t)127;
-  const int32_t live = len > 0 ? (int32_t)((len + chunk - 1) / chunk) : 0;
-  const float* pm = A.part_m + pair * A.splits;
-  const float* pl = A.part_l + pair * A.splits;
+  const int32_t hq = (int32_t)(pair - b * A.heads_q), head = hq / A.group;
+  const CacheItem it = cache_item(A, -1, b, lane, false);
+  if (it.n == 1) return;  // already whole
+  const int64_t part0 = (it.first * A.heads_kv + head) * A.group + (hq - head * A.group);
   float M = -__builtin_inff();
-  for (int32_t x = grp; x < live; x += 16) M = __builtin_fmaxf(M, pm[x]);
+  for (int32_t x = grp; x < it.n; x += 16) M = __builtin_fmaxf(M, A.part_m[part0 + (int64_t)x * A.heads_q]);
   if (n == 0) s_red[grp] = M;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 16; ++k) M = __builtin_fmaxf(M, s_red[k]);
   const float ref = M == -__builtin_inff() ? 0.0f : M;
   float L = 0.0f, v[8] = {};
-  for (int32_t x = grp; x < live; x += 16) {
-    const float f = __builtin_amdgcn_exp2f(pm[x] - ref);
-    L = __builtin_fmaf(f, pl[x], L);
+  for (int32_t x = grp; x < it.n; x += 16) {
+    const int64_t part = part0 + (int64_t)x * A.heads_q;
+    const float f = __builtin_amdgcn_exp2f(A.part_m[part] - ref);
+    L = __builtin_fmaf(f, A.part_l[part], L);
     float a[8];
-    load8(A.part_acc, (pair * A.splits + x) * HQ_TILE + c0, false, a);
+    load8(A.part_acc, part * HQ_TILE + c0, false, a);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(f, a[i], v[i]);
   }
@@ -620,14 +813,7 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
     v[4] += a1.x; v[5] += a1.y; v[6] += a1.z; v[7] += a1.w;
     L += s_red[k];
   }
-  const float inv = L == 0.0f ? 0.0f : 1.0f / (L * 128.0f);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] *= inv;
-  const XSigns sg(lane);
-  fwht128(v, sg);
-  const uint32_t dbits = sign_bits8(A.v_dmask, (int64_t)head * HQ_TILE + c0);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = flip(v[i], dbits, i);
+  cache_finish(A, L, v, head, lane);
   store8(A.out, pair * HQ_TILE + c0, A.out_bf16, v);
 }
 
@@ -652,11 +838,30 @@ int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream) {
   return (int)hipGetLastError();
 }
 
+template <int FMT, bool PACK>
+static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
+  static hq_lds_granted granted;
+  constexpr size_t lds = (size_t)HQ_WAVES_PER_WG * CacheRing<FMT>::WAVE;
+  if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, PACK>, lds, granted)) return e;
+  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, PACK>), grid, dim3(256), lds, st, a);
+  return 0;
+}
+
+template <int FMT>
+static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
+  return a.group <= 4 ? launch_attn<FMT, true>(a, grid, st) : launch_attn<FMT, false>(a, grid, st);
+}
+
 int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* stream) {
-  const dim3 grid((uint32_t)(a.batch * a.heads_kv * a.splits));
-  HQ_CACHE_FORMATS(hq_cache_attn_kernel, format, grid, (hipStream_t)stream, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL(hq_cache_join_kernel, dim3((uint32_t)(a.batch * a.heads_q)), dim3(256), 0,
-                       (hipStream_t)stream, a);
+  const hipStream_t st = (hipStream_t)stream;
+  const dim3 grid((uint32_t)(a.items * a.heads_kv)), wg(256);
+  int e = 0;
+  switch (format) {
+    case HQ_INT8: e = launch_attn<kInt8>(a, grid, st); break;
+    case HQ_E4M3: e = launch_attn<kE4M3>(a, grid, st); break;
+    default: e = launch_attn<kMx>(a, grid, st);
+  }
+  if (e) return e;
+  if (a.join) hipLaunchKernelGGL(hq_cache_join_kernel, dim3((uint32_t)(a.batch * a.heads_q)), wg, 0, st, a);
   return (int)hipGetLastError();
 }

@@ -52,16 +52,6 @@ void fill_side(const hq_plan_s* p, const hq_cache* c, const void* x, int64_t ld,
   s->stats = c->stats;
 }
 
-// Partial sums of a call: per KV head and split one set for each of its query
-// heads.  heads * splits <= heads + HQ_CACHE_WG_TARGET, and never more than one
-// split per 128 tokens, both growing with every argument: a workspace for the
-// largest call serves every smaller one.
-int64_t partials(int64_t heads, int64_t group, int64_t max_tokens) {
-  const int64_t by_tokens = heads * ((max_tokens + 127) / 128);
-  const int64_t by_target = heads + HQ_CACHE_WG_TARGET;
-  return (by_tokens < by_target ? by_tokens : by_target) * group;
-}
-
 hq_status norm_prep(hq_plan_t p, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
                     int32_t wt, float eps, int64_t M, void* h, int64_t ldh, int8_t* xq, float* sx, int fp8,
                     void* stream) {
@@ -158,7 +148,7 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
   if (!k || batch <= 0 || heads_q <= 0 || max_blocks <= 0 || k->heads <= 0 || k->block_tokens <= 0 ||
       heads_q % k->heads != 0)
     return 0;
-  const int64_t n = partials(batch * k->heads, heads_q / k->heads, (int64_t)max_blocks * k->block_tokens);
+  const int64_t n = hq_cache_items(batch, k->heads, (int64_t)max_blocks * k->block_tokens) * heads_q;
   return (size_t)n * (HQ_TILE + 2) * sizeof(float);
 }
 
@@ -168,12 +158,13 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
                              size_t ws_bytes, void* stream) {
   hq_status st = check_cache(kp, k);
   if (st != HQ_OK || (st = check_cache(vp, v)) != HQ_OK) return st;
-  if (v->format != k->format || v->heads != k->heads || v->block_tokens != k->block_tokens || v->blocks != k->blocks)
+  if (v->format != k->format || v->heads != k->heads || v->block_tokens != k->block_tokens || v->blocks != k->blocks ||
+      k->blocks == 0)
     return HQ_ERR_INVALID_ARG;
   if (!float_type(qt) || !float_type(ot) || batch < 0 || heads_q <= 0 || heads_q % k->heads != 0 ||
       max_blocks <= 0 || !std::isfinite(scale))
     return HQ_ERR_INVALID_ARG;
-  const int64_t group = heads_q / k->heads, heads = batch * k->heads;
+  const int64_t group = heads_q / k->heads;
   if (group > 16) return HQ_ERR_UNSUPPORTED;
   const int64_t max_tokens = (int64_t)max_blocks * k->block_tokens;
   if (max_tokens > (int64_t)1 << 30 || batch > 0x7FFFFFFF / heads_q) return HQ_ERR_UNSUPPORTED;
@@ -181,10 +172,11 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
   if (!q || !out || !block_table || !seq_lens || !aligned(q, 16) || !aligned(out, 16) || !aligned(block_table, 4) ||
       !aligned(seq_lens, 4))
     return HQ_ERR_INVALID_ARG;
-  const int64_t splits = hq_cache_splits(heads, max_tokens);
-  if (heads * splits > 0x7FFFFFFF) return HQ_ERR_UNSUPPORTED;
-  if (splits > 1 && (!workspace || !aligned(workspace, 16) ||
-                     ws_bytes < hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)))
+  const int64_t items = hq_cache_items(batch, k->heads, max_tokens);
+  const bool join = max_tokens > HQ_CACHE_LEAST;
+  if (items * heads_q > 0x7FFFFFFF) return HQ_ERR_UNSUPPORTED;
+  if (join && (!workspace || !aligned(workspace, 16) ||
+               ws_bytes < hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)))
     return HQ_ERR_INVALID_ARG;
   if ((st = check_device(kp)) != HQ_OK || (st = check_device(vp)) != HQ_OK) return st;
   hq_cache_attn_args a;
@@ -199,8 +191,8 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
   a.out = out;
   a.table = block_table;
   a.seq_lens = seq_lens;
-  if (splits > 1) {
-    const int64_t n = batch * heads_q * splits;
+  if (join) {
+    const int64_t n = items * heads_q;
     a.part_acc = (float*)workspace;
     a.part_m = a.part_acc + n * HQ_TILE;
     a.part_l = a.part_m + n;
@@ -213,7 +205,8 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
   a.group = (int32_t)group;
   a.max_blocks = max_blocks;
   a.block_tokens = k->block_tokens;
-  a.splits = (int32_t)splits;
+  a.items = items;
+  a.join = join;
   a.q_bf16 = qt == HQ_BF16;
   a.out_bf16 = ot == HQ_BF16;
   a.qscale = scale * (1.4426950408889634f / 128.0f);  // log2(e): the softmax runs in base 2

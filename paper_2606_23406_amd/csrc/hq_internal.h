@@ -259,8 +259,9 @@ struct hq_cache_io_args {
   int32_t y_bf16;
 };
 
-// One-token attention over a fixed-rate cache.  Workspace (splits > 1): per
-// (sequence, query head, split) the sum of 128 values, its maximum and its weight.
+// One-token attention over a fixed-rate cache.  Workspace (where a sequence may
+// be split): per (item, query head of its KV heads) the sum of 128 values, its
+// maximum and its weight.
 struct hq_cache_attn_args {
   const uint8_t* k_codes;
   const void* k_scales;
@@ -277,21 +278,25 @@ struct hq_cache_attn_args {
   float* part_l;
   hq_stats* stats;
   int64_t batch, blocks;
+  int64_t items;            // bound on the chunks of all sequences
   int32_t heads_q, heads_kv, group;
   int32_t max_blocks, block_tokens;
-  int32_t splits;
+  int32_t join;             // a sequence may have several chunks
   int32_t q_bf16, out_bf16;
   float qscale;             // softmax scale times log2(e) / 128
 };
 
 #define HQ_CACHE_WG_TARGET 512  // workgroups a cache attention call aims at
+#define HQ_CACHE_LEAST 512      // tokens of the smallest chunk
 
-// Splits of each sequence's tokens: enough workgroups (one per KV head and
-// split) to fill the chip, of at least 128 tokens each.
-static inline int64_t hq_cache_splits(int64_t heads, int64_t max_tokens) {
-  const int64_t most = (max_tokens + 127) / 128;
-  const int64_t want = (HQ_CACHE_WG_TARGET + heads - 1) / heads;
-  return want < most ? want : most;
+// Bound on the chunks of a call's sequences: a chunk is at least HQ_CACHE_LEAST
+// tokens and total * heads_kv / HQ_CACHE_WG_TARGET, so all sequences together have
+// at most HQ_CACHE_WG_TARGET / heads_kv beside the one each that rounding adds.
+// Grows with every argument but heads_kv; times heads_kv it grows with that too.
+static inline int64_t hq_cache_items(int64_t batch, int64_t heads_kv, int64_t max_tokens) {
+  const int64_t most = (max_tokens + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST;
+  const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
+  return batch * most < batch + even ? batch * most : batch + even;
 }
 
 // RMS norm fused with the 8-bit activation prep.

@@ -45,24 +45,29 @@ def test_workspace_bytes(hq):
     assert n(C.byref(c), 1, 16, 100) >= n(C.byref(c), 1, 8, 100) > last
 
 
-def test_split_rule(hq, tmp_path):
-    """Each sequence gets at least one split, and the partial sums fit what the
-    workspace bound allows, over many shapes."""
+def test_chunks_fit_the_workspace(hq, tmp_path):
+    """The chunks that the kernel cuts a batch into (its arithmetic, here in Python) are never more
+    than the bound that the grid and the workspace go by, whatever the lengths."""
     src = tmp_path / "rule.cpp"
-    src.write_text('#include "hq_internal.h"\n#include <cstdio>\n#include <initializer_list>\n'
-                   'int main() {\n  for (long h : {1L, 2L, 7L, 8L, 100L, 511L, 512L, 513L, 4000L, 100000L})\n'
-                   '    for (long t : {1L, 16L, 127L, 128L, 129L, 1000L, 8192L, 131072L, 1L << 30})\n'
-                   '      printf("%ld %ld %ld\\n", h, t, (long)hq_cache_splits(h, t));\n}\n')
+    src.write_text('#include "hq_internal.h"\n#include <cstdio>\n#include <cstdlib>\n'
+                   'int main(int, char** a) {\n  printf("%d %d %ld\\n", HQ_CACHE_WG_TARGET, HQ_CACHE_LEAST,\n'
+                   '         (long)hq_cache_items(atol(a[1]), atol(a[2]), atol(a[3])));\n}\n')
     exe = tmp_path / "rule"
     subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2606_23406_amd", "csrc"), "-o", str(exe),
                     str(src)], check=True)
     L = hq.lib()
-    for line in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines():
-        heads, tokens, splits = map(int, line.split())
-        assert 1 <= splits <= (tokens + 127) // 128
+    rng = np.random.default_rng(0)
+    for batch, heads, blocks in [(1, 1, 1), (1, 8, 8192), (3, 3, 400), (64, 8, 33), (65, 2, 700), (300, 1, 1000),
+                                 (2000, 16, 64), (1, 512, 100), (7, 600, 90)]:
+        target, least, items = map(int, subprocess.run([str(exe), str(batch), str(heads), str(16 * blocks)],
+                                                       capture_output=True, text=True, check=True).stdout.split())
+        for lens in (np.full(batch, 16 * blocks), rng.integers(0, 16 * blocks + 1, batch),
+                     np.where(np.arange(batch) == 0, 16 * blocks, 1), np.zeros(batch, np.int64)):
+            chunk = max(least, (-(-int(lens.sum()) * heads // target) + 127) // 128 * 128)
+            n = np.where(lens == 0, 1, -(-lens // chunk))
+            assert batch <= n.sum() <= items, (batch, heads, blocks)
         c = hq.CacheStruct(None, None, 1, 16, heads, 3, 0, None)
-        blocks = (tokens + 15) // 16
-        assert heads * splits * 130 * 4 <= L.hq_cache_attention_workspace_bytes(C.byref(c), 1, heads, blocks)
+        assert items * heads * 2 * 130 * 4 == L.hq_cache_attention_workspace_bytes(C.byref(c), batch, 2 * heads, blocks)
 
 
 def test_the_oracle_transforms_back():

@@ -367,6 +367,7 @@ def test_refusals(hq):
         assert call(c=cache(block_tokens=24)) == -2 and call(c=cache(block_tokens=0)) == -1
         assert call(c=cache(blocks=1 << 30)) == -2 and call(c=cache(blocks=-1)) == -1
         assert call(c=cache(codes=None)) == -1 and call(c=cache(scales=kc.scales.data_ptr() + 4)) == -1
+    assert attend(k=cache(blocks=0), v=cache(blocks=0)) == -1
     assert attend(v=cache(format=4)) == -1 and attend(v=cache(blocks=kc.blocks - 1)) == -1
     assert attend(heads_q=6) == -1 and attend(heads_q=0) == -1 and attend(heads_q=heads * 17) == -2
     assert attend(qt=2) == -1 and attend(ot=3) == -1 and attend(s=float("nan")) == -1 and attend(mb=0) == -1
