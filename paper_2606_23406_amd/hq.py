@@ -156,8 +156,10 @@ def _check(fn, status):
 
 
 def _stream_handle(stream=None):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return C.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return stream.cuda_stream
+    # the handle alone: building torch's Stream object around it takes 2.7 us
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dtype_code(dt):
@@ -523,15 +525,18 @@ def _on_device(*tensors):
     """The tensors lie on the current device, whose stream the call goes to."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.get_device() != dev:
+        if t.get_device() != dev:
             raise ValueError(f"a tensor on {t.device} in a call on cuda:{dev}")
 
 
-def _rows(t, width, name):
-    """A 2-D tensor of `width` contiguous values a row: its row stride."""
-    if t.dim() != 2 or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be [rows, {width}] with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+def _rows(t, rows, width, dtype, name):
+    """A [rows, width] tensor of `dtype` with contiguous rows: its row stride."""
+    if t.dtype != dtype or t.shape != (rows, width):
+        raise ValueError(f"{name} must be {dtype} [{rows}, {width}]")
+    ld, step = t.stride()
+    if step != 1 and width > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return ld if rows > 1 else max(ld, width)
 
 
 class Cache:
@@ -578,7 +583,7 @@ class Cache:
 
 
 def _slots(slots, rows):
-    if slots.dtype != torch.int64 or slots.dim() != 1 or slots.numel() != rows or not slots.is_contiguous():
+    if slots.dtype != torch.int64 or slots.shape != (rows,) or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int64 tensor, one per row")
     return slots.data_ptr()
 
@@ -588,19 +593,18 @@ def hq_cache_write(k_plan: Plan, k: torch.Tensor, k_cache: Cache, v_plan, v, v_c
     """hq_cache_write: k and v [rows, heads * 128] (bf16 or fp32) into the slots
     (int64 [rows], negative: skipped) of their caches; v_plan, v and v_cache
     None: k alone."""
-    rows, width = k.shape[0], k_cache.heads * 128
-    if (v is None) != (v_cache is None) or (v is None) != (v_plan is None):
-        raise ValueError("v_plan, v and v_cache come together")
-    ldk, ldv = _rows(k, width, "k"), 0
-    if v is not None:
-        ldv = _rows(v, width, "v")
-        if v.dtype != k.dtype or v.shape[0] != rows:
-            raise ValueError("k and v must have one dtype and the same rows")
-    _on_device(k, v, slots, k_cache.codes, None if v is None else v_cache.codes)
-    st = lib().hq_cache_write(k_plan.handle, k.data_ptr(), ldk, C.byref(k_cache.c),
-                              None if v is None else v_plan.handle, None if v is None else v.data_ptr(),
-                              ldv, None if v is None else C.byref(v_cache.c), _dtype_code(k.dtype),
-                              rows, _slots(slots, rows), _stream_handle(stream))
+    rows, width, dt = k.shape[0], k_cache.heads * 128, k.dtype
+    ldk = _rows(k, rows, width, dt, "k")
+    if v is None:
+        if v_plan is not None or v_cache is not None:
+            raise ValueError("v_plan, v and v_cache come together")
+        _on_device(k, slots, k_cache.codes)
+        vargs = (None, None, 0, None)
+    else:
+        _on_device(k, v, slots, k_cache.codes, v_cache.codes)
+        vargs = (v_plan.handle, v.data_ptr(), _rows(v, rows, width, dt, "v"), C.byref(v_cache.c))
+    st = lib().hq_cache_write(k_plan.handle, k.data_ptr(), ldk, C.byref(k_cache.c), *vargs,
+                              _dtype_code(dt), rows, _slots(slots, rows), _stream_handle(stream))
     _check("hq_cache_write", st)
 
 
@@ -610,12 +614,11 @@ def hq_cache_read(plan: Plan, cache: Cache, slots: torch.Tensor, out_dtype=torch
     rows, width = slots.shape[0], cache.heads * 128
     if out is None:
         out = torch.empty((rows, width), dtype=out_dtype, device=cache.device)
-    ld = _rows(out, width, "out")
-    if out.shape[0] != rows:
-        raise ValueError("out must have one row per slot")
+    dt = out.dtype
+    ld = _rows(out, rows, width, dt, "out")
     _on_device(slots, out, cache.codes)
     st = lib().hq_cache_read(plan.handle, C.byref(cache.c), _slots(slots, rows), rows, out.data_ptr(),
-                             _dtype_code(out.dtype), ld, _stream_handle(stream))
+                             _dtype_code(dt), ld, _stream_handle(stream))
     _check("hq_cache_read", st)
     return out
 
@@ -632,16 +635,16 @@ def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.
     [batch] tokens each.  Returns [batch, heads_q, 128]."""
     if q.dim() != 3 or q.shape[2] != 128 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [batch, heads_q, 128]")
-    batch, heads_q = q.shape[0], q.shape[1]
+    batch, heads_q, _ = shape = q.shape
     if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != batch or \
             not block_table.is_contiguous():
         raise ValueError("block_table must be a contiguous int32 [batch, max_blocks]")
-    if seq_lens.dtype != torch.int32 or tuple(seq_lens.shape) != (batch,) or not seq_lens.is_contiguous():
+    if seq_lens.dtype != torch.int32 or seq_lens.shape != (batch,) or not seq_lens.is_contiguous():
         raise ValueError("seq_lens must be a contiguous int32 [batch]")
     max_blocks = block_table.shape[1]
     if out is None:
-        out = torch.empty((batch, heads_q, 128), dtype=out_dtype, device=q.device)
-    elif out.shape != q.shape or not out.is_contiguous():
+        out = torch.empty(shape, dtype=out_dtype, device=q.device)
+    elif out.shape != shape or not out.is_contiguous():
         raise ValueError("out must be a contiguous [batch, heads_q, 128]")
     if workspace is None:
         nb = hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)
@@ -654,40 +657,36 @@ def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.
                                   128 ** -0.5 if scale is None else scale, block_table.data_ptr(),
                                   max_blocks, seq_lens.data_ptr(), out.data_ptr(),
                                   _dtype_code(out.dtype), workspace.data_ptr(),
-                                  workspace.numel() * workspace.element_size(), _stream_handle(stream))
+                                  workspace.nbytes, _stream_handle(stream))
     _check("hq_cache_attention", st)
     return out
 
 
 def _rmsnorm_act_prep(fn, code, plan, x, weight, eps, residual, h, xq, sx, stream):
-    M, K = x.shape[0], plan.cols
-    ldx, ldr, ldh = _rows(x, K, "x"), 0, 0
-    if x.dtype != torch.bfloat16:
-        raise ValueError("x must be bf16")
-    if weight.numel() != K or not weight.is_contiguous():
+    M, K = x.shape[0], plan.info.cols
+    bf16 = torch.bfloat16
+    ldx, ldr, ldh, rp, hp = _rows(x, M, K, bf16, "x"), 0, 0, None, None
+    if weight.shape != (K,) or not weight.is_contiguous():
         raise ValueError("weight must hold one contiguous value per column")
-    if residual is not None:
-        ldr = _rows(residual, K, "residual")
-        if residual.dtype != torch.bfloat16 or residual.shape[0] != M:
-            raise ValueError("residual must be bf16 with the rows of x")
-        if h is None:
-            h = torch.empty((M, K), dtype=torch.bfloat16, device=x.device)
-    if h is not None:
-        ldh = _rows(h, K, "h")
-        if h.dtype != torch.bfloat16 or h.shape[0] != M:
-            raise ValueError("h must be bf16 with the rows of x")
     if xq is None:
         xq = torch.empty((M, K), dtype=code, device=x.device)
     elif xq.shape != (M, K) or xq.dtype != code or not xq.is_contiguous():
-        raise ValueError(f"xq must be a contiguous {code} [rows, {K}]")
+        raise ValueError(f"xq must be a contiguous {code} [{M}, {K}]")
     if sx is None:
         sx = torch.empty((M,), dtype=torch.float32, device=x.device)
     elif sx.shape != (M,) or sx.dtype != torch.float32 or not sx.is_contiguous():
-        raise ValueError("sx must be a contiguous fp32 [rows]")
-    _on_device(x, weight, residual, h, xq, sx)
-    st = getattr(lib(), fn)(plan.handle, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(),
-                            ldr, weight.data_ptr(), _dtype_code(weight.dtype), eps, M,
-                            None if h is None else h.data_ptr(), ldh, xq.data_ptr(), sx.data_ptr(),
+        raise ValueError(f"sx must be a contiguous fp32 [{M}]")
+    _on_device(x, weight, xq, sx)
+    if residual is not None:
+        if h is None:
+            h = torch.empty((M, K), dtype=bf16, device=x.device)
+        _on_device(residual)
+        ldr, rp = _rows(residual, M, K, bf16, "residual"), residual.data_ptr()
+    if h is not None:
+        _on_device(h)
+        ldh, hp = _rows(h, M, K, bf16, "h"), h.data_ptr()
+    st = getattr(lib(), fn)(plan.handle, x.data_ptr(), ldx, rp, ldr, weight.data_ptr(),
+                            _dtype_code(weight.dtype), eps, M, hp, ldh, xq.data_ptr(), sx.data_ptr(),
                             _stream_handle(stream))
     _check(fn, st)
     return (xq, sx) if residual is None else (xq, sx, h)
