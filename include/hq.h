@@ -449,8 +449,8 @@ hq_status hq_decode_attention(hq_plan_t k_plan, const hq_stream* k, hq_plan_t v_
  *                 (HQ_MXFP4: 64): one head's tokens of a block are one run.
  *   scales        device, 16-byte aligned: fp32 [blocks, heads, block_tokens]
  *                 (HQ_MXFP4: bytes [blocks, heads, block_tokens, 4]).
- *   block_tokens  a multiple of 16 (HQ_ERR_UNSUPPORTED otherwise); blocks *
- *                 block_tokens below 2^31.
+ *   block_tokens  a multiple of 16 (HQ_ERR_UNSUPPORTED otherwise); one block at
+ *                 least, blocks * block_tokens below 2^31.
  *   heads         KV heads; heads * 128 <= plan.cols (a plan's columns are a multiple
  *                 of 512, so 1, 2 or 3 heads use the first of its columns).
  *   stats         nullable device hq_stats.
@@ -506,7 +506,7 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
  * cache: out[b, h] = sum_t softmax_t(scale q[b, h] . k^_t) v^_t, k^ and v^ the rows
  * hq_cache_read would return in fp32.  The query is moved into the stored
  * coordinates once and the value sum back once; nothing is materialized.
- *   k, v         caches of one format, heads, block_tokens and blocks (one at least).
+ *   k, v         caches of one format, heads, block_tokens and blocks.
  *   q            device [batch, heads_q, 128], HQ_BF16 or HQ_FP32, 16-byte
  *                aligned; head h reads KV head h / (heads_q / heads), a group of
  *                1 .. 16 (HQ_ERR_UNSUPPORTED above).

@@ -58,6 +58,27 @@ __device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const floa
   }
 }
 
+// D of the 8 columns from col on, as bf16 sign bits per pair of columns.
+__device__ __forceinline__ uint4 sign_words(const uint32_t* dsign16, int64_t col) {
+  return *(const uint4*)(dsign16 + (col >> 1));
+}
+
+__device__ __forceinline__ void flip8(float* v, uint4 d) {
+  const uint32_t w[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = xor_sign(v[2 * i], w[i] << 16);
+    v[2 * i + 1] = xor_sign(v[2 * i + 1], w[i] & 0xFFFF0000u);
+  }
+}
+
+// a / b for a constant b, correctly rounded where nothing underflows: the quotient
+// by the rounded reciprocal, corrected by its exact remainder.
+__device__ __forceinline__ float over(float a, float b) {
+  const float r = 1.0f / b, q = a * r;
+  return __builtin_fmaf(__builtin_fmaf(-b, q, a), r, q);
+}
+
 __device__ __forceinline__ void report(hq_stats* s, int32_t err) {
   if (s) atomicCAS(&s->status, 0u, (uint32_t)err);
 }
@@ -66,94 +87,100 @@ __device__ __forceinline__ void report(hq_stats* s, int32_t err) {
 // 16 lanes take one head vector, 8 values each; a wave four of them, neighbouring
 // heads of one token where there are four.
 
-struct CacheTile {
-  int64_t row;   // token row of the call
-  int32_t head;
-  int64_t at;    // index of the stored head vector, or -1
-};
+// A lane group takes two vectors, whose slots and rows are loaded together: with one
+// a wave waits for a slot and then for what it points to with little else in flight.
+// (65536 rows of 8 heads in int8: written in 78 us with two, 85 with one, read in 44 and
+// 56; up to 4096 rows the same.  Four write 8192 rows in 15.1 us, two in 13.4.)
+// Both kernels are bound by memory and by VALU issue at once, about 350 instructions
+// per pair: 8192 rows of 8 heads from bf16 to E4M3 take 13.4 us (3.8 TB/s), 32768 rows of
+// int8 to bf16 23.2 us (4.4 TB/s), where a large copy moves 5.2 TB/s.
+constexpr int U = 2;
+constexpr uint32_t kIoTiles = 16 * U;  // of a workgroup
 
-__device__ __forceinline__ CacheTile cache_tile(const hq_cache_io_args& A, const hq_cache_side& S, int lane,
-                                                bool first) {
-  const uint32_t tile = blockIdx.x * 16u + (threadIdx.x >> 4);
-  CacheTile t;
-  t.row = tile / (uint32_t)A.heads;
-  t.head = (int32_t)(tile - (uint32_t)t.row * (uint32_t)A.heads);
-  t.at = -1;
-  if (tile >= A.tiles) {
-    t.row = -1;
-    return t;
+struct CacheTiles {
+  uint32_t row[U], head[U];  // of the call; past its end the last tile's
+  bool in[U];                // not past the end
+  int64_t slot[U];
+  __device__ __forceinline__ explicit CacheTiles(const hq_cache_io_args& A) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const uint32_t t = (blockIdx.x * U + i) * 16u + (threadIdx.x >> 4), tile = min(t, A.tiles - 1);
+      in[i] = t < A.tiles;
+      row[i] = A.by_heads.of(tile);
+      head[i] = tile - row[i] * (uint32_t)A.heads;
+      slot[i] = A.slots[row[i]];
+    }
   }
-  const int64_t slot = A.slots[t.row];
-  if (slot >= 0 && slot < S.slots) {
-    const uint32_t blk = (uint32_t)slot / (uint32_t)A.block_tokens;
-    const uint32_t off = (uint32_t)slot - blk * (uint32_t)A.block_tokens;
-    t.at = ((int64_t)blk * A.heads + t.head) * A.block_tokens + off;
-  } else if (slot >= 0 && first && t.head == 0 && (lane & 15) == 0) {
-    report(S.stats, HQ_ERR_INVALID_ARG);
+  // Whether tile i has a slot in the cache, and where its vector lies.
+  __device__ __forceinline__ bool at(const hq_cache_io_args& A, const hq_cache_side& S, int lane, int i,
+                                     int64_t& vec) const {
+    const bool ok = slot[i] >= 0 && slot[i] < S.slots;
+    if (slot[i] >= S.slots && head[i] == 0 && (lane & 15) == 0) report(S.stats, HQ_ERR_INVALID_ARG);
+    const uint32_t s = ok ? (uint32_t)slot[i] : 0u, blk = A.by_block.of(s);
+    vec = (int64_t)(blk * (uint64_t)(uint32_t)A.heads + head[i]) * A.block_tokens + (s - blk * (uint32_t)A.block_tokens);
+    return ok && in[i];
   }
-  return t;
-}
+};
 
 template <int FMT>
 __global__ __launch_bounds__(256) void hq_cache_write_kernel(hq_cache_io_args A) {
   const hq_cache_side& S = A.side[blockIdx.y];
-  const int lane = threadIdx.x & 63;
-  const CacheTile t = cache_tile(A, S, lane, true);
-  const int c0 = (lane & 15) * 8;
-  float v[8] = {};
-  // every lane of a wave stays for the transform's lane moves
-  if (t.at >= 0) {
-    load8(S.x, t.row * S.ld + (int64_t)t.head * HQ_TILE + c0, A.x_bf16, v);
-    const uint32_t dbits = sign_bits8(S.dmask, (int64_t)t.head * HQ_TILE + c0);
+  const int lane = threadIdx.x & 63, c0 = (lane & 15) * 8;
+  const CacheTiles t(A);
+  float v[U][8];
+  uint4 d[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = flip(v[i], dbits, i);
+  for (int i = 0; i < U; ++i) {
+    load8(S.x, (int64_t)t.row[i] * S.ld + (t.head[i] * HQ_TILE + c0), A.x_bf16, v[i]);
+    d[i] = sign_words(S.dsign16, t.head[i] * HQ_TILE + c0);
   }
-  const XSigns sg(lane);
-  fwht128(v, sg);
-  float am = amax_or_nan<8>(v);
-  am = __builtin_elementwise_maximum(am, xor_lane_f<1>(am));
-  am = __builtin_elementwise_maximum(am, xor_lane_f<2>(am));
-  am = __builtin_elementwise_maximum(am, xor_lane_f<4>(am));
-  am = __builtin_elementwise_maximum(am, xor_lane_f<8>(am));
-  // a vector with an infinite or NaN value has no scale: codes 0, scale NaN
-  const bool bad = !(am <= 3.4028234663852886e38f);
-  if (bad) {
+  const TwSigns sg(lane);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    if (t.at >= 0 && (lane & 15) == 0 && S.stats) {
-      atomicAdd(&S.stats->overflow_tiles, 1u);
-      report(S.stats, HQ_ERR_OVERFLOW);
-    }
-  }
-  if constexpr (FMT == kMx) {
-    int32_t X;
-    const uint32_t packed = mxfp4_x8(v, X);
-    if (t.at < 0) return;
-    *(uint32_t*)(S.codes + t.at * row_bytes<FMT>() + c0 / 2) = packed;
-    if ((lane & 3) == 0) ((uint8_t*)S.scales)[t.at * 4 + ((lane & 15) >> 2)] = bad ? 0xFFu : (uint8_t)(X + 127);
-  } else {
-    const float top = FMT == kE4M3 ? 448.0f : 127.0f;
-    // below 2^-100 the reciprocal could overflow: such a vector is stored as zeros
-    const bool zero = bad || am < 0x1p-100f;
-    const float inv = zero ? 0.0f : top / am;
-    uint32_t packed[2] = {0u, 0u};
-    float q[8];
+  for (int i = 0; i < U; ++i) {
+    // every lane of a wave stays for the transform's lane moves, which leave sigma
+    // times the values
+    int64_t vec;
+    const bool live = t.at(A, S, lane, i, vec);
+    flip8(v[i], d[i]);
+    fwht128_tw(v[i], sg);
+    float am = amax_or_nan<8>(v[i]);
+    am = __builtin_elementwise_maximum(am, dpp_xor<1>(am));
+    am = __builtin_elementwise_maximum(am, dpp_xor<2>(am));
+    am = __builtin_elementwise_maximum(am, swz_xor4(am));
+    am = __builtin_elementwise_maximum(am, dpp_xor<8>(am));
+    // a vector with an infinite or NaN value has no scale: codes 0, scale NaN
+    const bool bad = !(am <= 3.4028234663852886e38f);
+    if (__builtin_expect(bad, 0)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      q[i] = v[i] * inv;
-      if (FMT == kInt8) q[i] = __builtin_rintf(q[i]);
-      q[i] = __builtin_fminf(__builtin_fmaxf(q[i], -top), top);
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+      if (live && (lane & 15) == 0 && S.stats) {
+        atomicAdd(&S.stats->overflow_tiles, 1u);
+        report(S.stats, HQ_ERR_OVERFLOW);
+      }
     }
-    if constexpr (FMT == kE4M3) {
-      packed[0] = e4m3x4(q[0], q[1], q[2], q[3]);
-      packed[1] = e4m3x4(q[4], q[5], q[6], q[7]);
+    if constexpr (FMT == kMx) {
+      int32_t X;
+      const uint32_t packed = mxfp4_x8(v[i], X) ^ (sg.sigma ? 0x88888888u : 0u);
+      if (!live) continue;
+      *(uint32_t*)(S.codes + vec * row_bytes<FMT>() + c0 / 2) = packed;
+      if ((lane & 3) == 0) ((uint8_t*)S.scales)[vec * 4 + ((lane & 15) >> 2)] = bad ? 0xFFu : (uint8_t)(X + 127);
     } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) packed[i >> 2] |= ((uint32_t)(int32_t)q[i] & 0xFFu) << (8 * (i & 3));
+      constexpr float top = FMT == kE4M3 ? 448.0f : 127.0f;
+      // below 2^-100 the reciprocal could overflow: such a vector is stored as zeros
+      const bool zero = bad || am < 0x1p-100f;
+      const float inv = zero ? 0.0f : xor_sign(top / am, sg.sigma);
+      // |q| is top (1 + 2^-23) at most, which rounds to top in both formats: no clamp
+      uint2 packed;
+      if constexpr (FMT == kE4M3) {
+        packed.x = e4m3x4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
+        packed.y = e4m3x4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+      } else {
+        packed = int8x8(v[i], inv);
+      }
+      if (!live) continue;
+      *(uint2*)(S.codes + vec * row_bytes<FMT>() + c0) = packed;
+      if ((lane & 15) == 0) ((float*)S.scales)[vec] = bad ? __builtin_nanf("") : zero ? 0.0f : over(am, top);
     }
-    if (t.at < 0) return;
-    *(uint2*)(S.codes + t.at * row_bytes<FMT>() + c0) = make_uint2(packed[0], packed[1]);
-    if ((lane & 15) == 0) ((float*)S.scales)[t.at] = bad ? __builtin_nanf("") : zero ? 0.0f : am / top;
   }
 }
 
@@ -165,25 +192,40 @@ __device__ __forceinline__ float e8m0(uint32_t byte) {
 template <int FMT>
 __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) {
   const hq_cache_side& S = A.side[0];
-  const int lane = threadIdx.x & 63;
-  const CacheTile t = cache_tile(A, S, lane, true);
-  const int c0 = (lane & 15) * 8;
-  float v[8] = {}, scale = 0.0f;
-  if (t.at >= 0) {
+  const int lane = threadIdx.x & 63, c0 = (lane & 15) * 8;
+  const CacheTiles t(A);
+  uint2 w[U];
+  uint4 d[U];
+  float scale[U];
+  bool live[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    int64_t vec;  // a vector of the cache also where the tile has none
+    live[i] = t.at(A, S, lane, i, vec);
     if constexpr (FMT == kMx) {
-      const uint32_t w = *(const uint32_t*)(S.codes + t.at * row_bytes<FMT>() + c0 / 2);
-      const float f = e8m0(((const uint8_t*)S.scales)[t.at * 4 + ((lane & 15) >> 2)]);
-      scale = 1.0f;
-      const v2f_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
-      const v2f_t b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-      const v2f_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
-      const v2f_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+      w[i].x = *(const uint32_t*)(S.codes + vec * row_bytes<FMT>() + c0 / 2);
+      w[i].y = ((const uint8_t*)S.scales)[vec * 4 + ((lane & 15) >> 2)];
+      scale[i] = 1.0f;
+    } else {
+      w[i] = *(const uint2*)(S.codes + vec * row_bytes<FMT>() + c0);
+      scale[i] = ((const float*)S.scales)[vec];
+    }
+    d[i] = sign_words(S.dsign16, t.head[i] * HQ_TILE + c0);
+  }
+  const TwSigns sg(lane);
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    float v[8];
+    if constexpr (FMT == kMx) {
+      const float f = e8m0(w[i].y);
+      const v2f_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i].x, 1.0f, 0);
+      const v2f_t b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i].x, 1.0f, 1);
+      const v2f_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i].x, 1.0f, 2);
+      const v2f_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i].x, 1.0f, 3);
       v[0] = a[0] * f; v[1] = a[1] * f; v[2] = b[0] * f; v[3] = b[1] * f;
       v[4] = c[0] * f; v[5] = c[1] * f; v[6] = d[0] * f; v[7] = d[1] * f;
     } else {
-      const uint2 w = *(const uint2*)(S.codes + t.at * row_bytes<FMT>() + c0);
-      scale = ((const float*)S.scales)[t.at];
-      const uint32_t w2[2] = {w.x, w.y};
+      const uint32_t w2[2] = {w[i].x, w[i].y};
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if constexpr (FMT == kE4M3) {
@@ -192,20 +234,18 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
           v[4 * h] = a[0]; v[4 * h + 1] = a[1]; v[4 * h + 2] = b[0]; v[4 * h + 3] = b[1];
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[4 * h + i] = (float)(int8_t)(w2[h] >> (8 * i));
+          for (int e = 0; e < 4; ++e) v[4 * h + e] = (float)(int8_t)(w2[h] >> (8 * e));
         }
       }
     }
-  }
-  const XSigns sg(lane);
-  fwht128(v, sg);
-  if (t.row < 0) return;
-  // H of the codes first, then the scale: integer codes sum exactly
-  const uint32_t dbits = sign_bits8(S.dmask, (int64_t)t.head * HQ_TILE + c0);
-  const float f = scale * 0.0078125f;
+    fwht128_tw(v, sg);
+    // H of the codes first, then the scale: integer codes sum exactly
+    const float f = xor_sign(scale[i] * 0.0078125f, sg.sigma);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = t.at < 0 ? 0.0f : flip(v[i] * f, dbits, i);
-  store8(A.y, t.row * A.ldy + (int64_t)t.head * HQ_TILE + c0, A.y_bf16, v);
+    for (int e = 0; e < 8; ++e) v[e] = live[i] ? v[e] * f : 0.0f;
+    flip8(v, d[i]);
+    if (t.in[i]) store8(A.y, (int64_t)t.row[i] * A.ldy + (t.head[i] * HQ_TILE + c0), A.y_bf16, v);
+  }
 }
 
 // ----------------------------------------------------------------- attention
@@ -827,13 +867,13 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
   }
 
 int hq_launch_cache_write(const hq_cache_io_args& a, int format, int sides, void* stream) {
-  const dim3 grid((a.tiles + 15) / 16, (uint32_t)sides);
+  const dim3 grid((a.tiles + kIoTiles - 1) / kIoTiles, (uint32_t)sides);
   HQ_CACHE_FORMATS(hq_cache_write_kernel, format, grid, (hipStream_t)stream, a);
   return (int)hipGetLastError();
 }
 
 int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream) {
-  const dim3 grid((a.tiles + 15) / 16);
+  const dim3 grid((a.tiles + kIoTiles - 1) / kIoTiles);
   HQ_CACHE_FORMATS(hq_cache_read_kernel, format, grid, (hipStream_t)stream, a);
   return (int)hipGetLastError();
 }

@@ -20,12 +20,11 @@ hq_status check_cache(const hq_plan_s* p, const hq_cache* c) {
   if (!p || !c) return HQ_ERR_INVALID_ARG;
   if (p->tile != HQ_TILE || p->rotation != HQ_ROT_NONE || p->dither || p->norm_fp16) return HQ_ERR_UNSUPPORTED;
   if (c->format != HQ_INT8 && c->format != HQ_E4M3 && c->format != HQ_MXFP4) return HQ_ERR_INVALID_ARG;
-  if (c->heads <= 0 || (int64_t)c->heads * HQ_TILE > p->cols || c->blocks < 0 || c->block_tokens <= 0)
+  if (c->heads <= 0 || (int64_t)c->heads * HQ_TILE > p->cols || c->blocks <= 0 || c->block_tokens <= 0)
     return HQ_ERR_INVALID_ARG;
   if (c->block_tokens % 16 != 0) return HQ_ERR_UNSUPPORTED;
   if (c->blocks > 0x7FFFFFFF / c->block_tokens) return HQ_ERR_UNSUPPORTED;  // slots are 31-bit
-  if (c->blocks > 0 && (!c->codes || !c->scales || !aligned(c->codes, 16) || !aligned(c->scales, 16)))
-    return HQ_ERR_INVALID_ARG;
+  if (!c->codes || !c->scales || !aligned(c->codes, 16) || !aligned(c->scales, 16)) return HQ_ERR_INVALID_ARG;
   return HQ_OK;
 }
 
@@ -48,7 +47,7 @@ void fill_side(const hq_plan_s* p, const hq_cache* c, const void* x, int64_t ld,
   s->codes = (uint8_t*)c->codes;
   s->scales = c->scales;
   s->slots = c->blocks * c->block_tokens;
-  s->dmask = p->d_dmask;
+  s->dsign16 = p->d_dsign16;
   s->stats = c->stats;
 }
 
@@ -77,7 +76,7 @@ hq_status norm_prep(hq_plan_t p, const void* x, int64_t ldx, const void* residua
   a.K = p->cols;
   a.xq = xq;
   a.sx = sx;
-  a.dmask = p->d_dmask;
+  a.dsign16 = p->d_dsign16;
   a.eps = eps;
   a.w_bf16 = wt == HQ_BF16;
   a.fp8 = fp8;
@@ -99,7 +98,7 @@ hq_status hq_cache_write(hq_plan_t kp, const void* k, int64_t ldk, const hq_cach
     if ((st = check_cache(vp, vc)) != HQ_OK) return st;
     if (vc->format != kc->format || vc->heads != kc->heads || vc->block_tokens != kc->block_tokens)
       return HQ_ERR_INVALID_ARG;
-    if (kc->blocks > 0 && (vc->codes == kc->codes || vc->scales == kc->scales)) return HQ_ERR_INVALID_ARG;
+    if (vc->codes == kc->codes || vc->scales == kc->scales) return HQ_ERR_INVALID_ARG;
   } else if (v) {
     return HQ_ERR_INVALID_ARG;
   }
@@ -118,6 +117,8 @@ hq_status hq_cache_write(hq_plan_t kp, const void* k, int64_t ldk, const hq_cach
   a.tiles = (uint32_t)(rows * kc->heads);
   a.heads = kc->heads;
   a.block_tokens = kc->block_tokens;
+  a.by_heads = hq_divide_by((uint32_t)kc->heads);
+  a.by_block = hq_divide_by((uint32_t)kc->block_tokens);
   a.x_bf16 = xt == HQ_BF16;
   return hip_status(hq_launch_cache_write(a, kc->format, both ? 2 : 1, stream));
 }
@@ -138,6 +139,8 @@ hq_status hq_cache_read(hq_plan_t p, const hq_cache* c, const int64_t* slots, in
   a.tiles = (uint32_t)(rows * c->heads);
   a.heads = c->heads;
   a.block_tokens = c->block_tokens;
+  a.by_heads = hq_divide_by((uint32_t)c->heads);
+  a.by_block = hq_divide_by((uint32_t)c->block_tokens);
   a.y = y;
   a.ldy = ld;
   a.y_bf16 = yt == HQ_BF16;
@@ -158,8 +161,7 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
                              size_t ws_bytes, void* stream) {
   hq_status st = check_cache(kp, k);
   if (st != HQ_OK || (st = check_cache(vp, v)) != HQ_OK) return st;
-  if (v->format != k->format || v->heads != k->heads || v->block_tokens != k->block_tokens || v->blocks != k->blocks ||
-      k->blocks == 0)
+  if (v->format != k->format || v->heads != k->heads || v->block_tokens != k->block_tokens || v->blocks != k->blocks)
     return HQ_ERR_INVALID_ARG;
   if (!float_type(qt) || !float_type(ot) || batch < 0 || heads_q <= 0 || heads_q % k->heads != 0 ||
       max_blocks <= 0 || !std::isfinite(scale))

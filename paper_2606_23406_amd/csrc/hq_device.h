@@ -637,6 +637,20 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
 }
 
+// rint(v inv) of eight values as int8 bytes, |v inv| below 2^22: adding 1.5 2^23
+// rounds to the integer (to nearest even), whose low byte is the sum's.
+__device__ __forceinline__ uint2 int8x8(const float* v, float inv) {
+  uint32_t t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = __float_as_uint(v[i] * inv + 12582912.0f);
+  uint32_t r[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    r[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[4 * i + 3], t[4 * i + 2], 0x0C0C0400u),
+                                 __builtin_amdgcn_perm(t[4 * i + 1], t[4 * i], 0x0C0C0400u), 0x05040100u);
+  return make_uint2(r[0], r[1]);
+}
+
 // Two values as OCP FP4 E2M1 codes of v / 2^X (magnitudes 0, .5, 1, 1.5, 2, 3,
 // 4, 6 as codes 0 .. 7 with the sign in bit 3) in byte SEL of r, the first in
 // the low nibble: the nearest value, ties to the even code, saturating at 6,

@@ -238,6 +238,24 @@ struct hq_gemm_args {
   int32_t tile;       // RHT tile: the weight factors' K span (128 .. 2048)
 };
 
+// Division of 31-bit numbers by a divisor known on the host: n / d = (n mul) >>
+// (32 + shift) with mul = floor(2^(32 + shift) / d) + 1, shift = ceil(log2 d) - 1 (d >=
+// 2): the error n (mul - 2^(32 + shift) / d) / 2^(32 + shift) is at most n / 2^(32 + shift)
+// < 1 / d for n < 2^31.
+struct hq_divisor {
+  uint32_t mul, shift;  // mul 0: by 1
+#ifdef __HIPCC__
+  __device__ __forceinline__ uint32_t of(uint32_t n) const { return mul ? __umulhi(n, mul) >> shift : n; }
+#endif
+};
+static inline hq_divisor hq_divide_by(uint32_t d) {
+  hq_divisor r = {0, 0};
+  if (d < 2) return r;
+  while ((2u << r.shift) < d) ++r.shift;  // ceil(log2 d) - 1
+  r.mul = (uint32_t)((((uint64_t)1 << (32 + r.shift)) / d) + 1);
+  return r;
+}
+
 // One tensor of a cache write or read.
 struct hq_cache_side {
   const void* x;          // write: rows of heads * 128 values, stride ld
@@ -245,7 +263,7 @@ struct hq_cache_side {
   uint8_t* codes;
   void* scales;
   int64_t slots;          // blocks * block_tokens
-  const uint32_t* dmask;  // RHT sign bit per column
+  const uint32_t* dsign16;  // RHT signs as bf16 XOR words, one per column pair
   hq_stats* stats;
 };
 struct hq_cache_io_args {
@@ -253,6 +271,7 @@ struct hq_cache_io_args {
   const int64_t* slots;   // one per row
   uint32_t tiles;         // rows * heads
   int32_t heads, block_tokens;
+  hq_divisor by_heads, by_block;
   int32_t x_bf16;
   void* y;                // read: output rows, stride ldy
   int64_t ldy;
@@ -309,7 +328,7 @@ struct hq_norm_args {
   int64_t M, K;
   int8_t* xq;
   float* sx;
-  const uint32_t* dmask;
+  const uint32_t* dsign16;  // RHT signs as bf16 XOR words, one per column pair
   float eps;
   int32_t w_bf16;
   int32_t fp8;

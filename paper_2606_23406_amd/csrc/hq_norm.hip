@@ -13,12 +13,12 @@ namespace {
 // max|y|) do not depend on it: y is formed from h * w alone, and the factor enters
 // s_x = max|y| / (top rms).  So the sum of squares and the maximum meet at one
 // barrier, and a row is read once and written once.
-// Blocks of 512 columns: up to tile 512 wave w takes the blocks 4 i + w; LONG (tiles of
-// 1024 and 2048, two or four blocks) groups of four, 16 (i / 4) + 4 w + i % 4, so that a
-// tile lies inside one wave.
-template <int NIT, bool FP8, bool LONG>
-__global__ __launch_bounds__(256) void hq_norm_prep_kernel(hq_norm_args A) {
-  __shared__ float s_max[4], s_sum[4];
+// Blocks of 512 columns: up to tile 512 wave w of W takes the blocks W i + w; LONG (tiles
+// of 1024 and 2048, two or four blocks) groups of four, 4 W (i / 4) + 4 w + i % 4, so that
+// a tile lies inside one wave.
+template <int W, int NIT, bool FP8, bool LONG>
+__global__ __launch_bounds__(64 * W) void hq_norm_prep_kernel(hq_norm_args A) {
+  __shared__ float s_max[W], s_sum[W];
   const int tid = threadIdx.x, lane = tid & 63;
   const uint32_t wave = readfirst((uint32_t)(tid >> 6));
   const int64_t row = blockIdx.x;
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256) void hq_norm_prep_kernel(hq_norm_args A) {
   const uint16_t* rrow = A.residual ? (const uint16_t*)A.residual + row * A.ldr + 8 * lane : nullptr;
   uint16_t* hrow = A.h ? (uint16_t*)A.h + row * A.ldh + 8 * lane : nullptr;
   auto base_of = [&](int i) -> uint32_t {
-    return HQ_SUB * (LONG ? 16u * (i / 4) + 4u * wave + (i & 3) : 4u * i + wave);
+    return HQ_SUB * (LONG ? 4u * W * (i / 4) + 4u * wave + (i & 3) : (uint32_t)W * i + wave);
   };
   uint4 raw[NIT], res[NIT];
 #pragma unroll
@@ -38,7 +38,8 @@ __global__ __launch_bounds__(256) void hq_norm_prep_kernel(hq_norm_args A) {
       if (rrow) res[i] = *(const uint4*)(rrow + base);
     }
   }
-  const XSigns sg(lane);
+  const TwSigns sg(lane);  // the transform leaves sigma times the values
+  const float s16 = (lane & 16) ? -1.0f : 1.0f, s32 = (lane & 32) ? -1.0f : 1.0f;
   float v[NIT][8], amax = 0.0f, sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < NIT; ++i) {
@@ -71,25 +72,25 @@ __global__ __launch_bounds__(256) void hq_norm_prep_kernel(hq_norm_args A) {
       wt[0] = a.x; wt[1] = a.y; wt[2] = a.z; wt[3] = a.w;
       wt[4] = b.x; wt[5] = b.y; wt[6] = b.z; wt[7] = b.w;
     }
-    const uint32_t dbits = sign_bits8(A.dmask, col);
+    const uint4 dw = *(const uint4*)(A.dsign16 + (col >> 1));
+    const uint32_t d4[4] = {dw.x, dw.y, dw.z, dw.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float a = __uint_as_float(w4[e] << 16), b = __uint_as_float(w4[e] & 0xFFFF0000u);
+      const uint32_t x = w4[e] ^ d4[e];
+      const float a = __uint_as_float(x << 16), b = __uint_as_float(x & 0xFFFF0000u);
       sum = __builtin_fmaf(a, a, sum);
       sum = __builtin_fmaf(b, b, sum);
-      v[i][2 * e] = flip(a * wt[2 * e], dbits, 2 * e);
-      v[i][2 * e + 1] = flip(b * wt[2 * e + 1], dbits, 2 * e + 1);
+      v[i][2 * e] = a * wt[2 * e];
+      v[i][2 * e + 1] = b * wt[2 * e + 1];
     }
-    fwht128(v[i], sg);
+    fwht128_tw(v[i], sg);
     if (LONG || A.tile >= 256) {
-      const float s = (lane & 16) ? -1.0f : 1.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e], s, swz_xor16(v[i][e]));
+      for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e], s16, swz_xor16(v[i][e]));
     }
     if (LONG || A.tile >= 512) {
-      const float s = (lane & 32) ? -1.0f : 1.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e], s, lane_xor32(v[i][e]));
+      for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e], s32, lane_xor32(v[i][e]));
     }
   }
   if constexpr (LONG) {
@@ -111,44 +112,50 @@ __global__ __launch_bounds__(256) void hq_norm_prep_kernel(hq_norm_args A) {
   for (int i = 0; i < NIT; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) amax = __builtin_fmaxf(amax, __builtin_fabsf(v[i][e]));
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    amax = __builtin_fmaxf(amax, __shfl_xor(amax, m, 64));
-    sum += __shfl_xor(sum, m, 64);
-  }
+  amax = __builtin_fmaxf(amax, dpp_xor<1>(amax));
+  sum += dpp_xor<1>(sum);
+  amax = __builtin_fmaxf(amax, dpp_xor<2>(amax));
+  sum += dpp_xor<2>(sum);
+  amax = __builtin_fmaxf(amax, swz_xor4(amax));
+  sum += swz_xor4(sum);
+  amax = __builtin_fmaxf(amax, dpp_xor<8>(amax));
+  sum += dpp_xor<8>(sum);
+  amax = __builtin_fmaxf(amax, swz_xor16(amax));
+  sum += swz_xor16(sum);
+  amax = __builtin_fmaxf(amax, lane_xor32(amax));
+  sum += lane_xor32(sum);
   if (lane == 0) {
     s_max[wave] = amax;
     s_sum[wave] = sum;
   }
   __syncthreads();
-  amax = __builtin_fmaxf(__builtin_fmaxf(s_max[0], s_max[1]), __builtin_fmaxf(s_max[2], s_max[3]));
+  amax = s_max[0];
+  sum = s_sum[0];
+#pragma unroll
+  for (int x = 1; x < W; ++x) {
+    amax = __builtin_fmaxf(amax, s_max[x]);
+    sum += s_sum[x];
+  }
   const float top = FP8 ? 448.0f : 127.0f;  // E4M3's largest magnitude, or int8's
   // below 2^-100 the reciprocal could overflow: such a row counts as zeros
-  const float inv = amax < 0x1p-100f ? 0.0f : top / amax;
+  const float inv = amax < 0x1p-100f ? 0.0f : xor_sign(top / amax, sg.sigma);
+  // |v inv| is top (1 + 2^-23) at most, which rounds to top in both formats: no clamp.
+  // (A row with a NaN has the scale NaN, whatever its codes.)
 #pragma unroll
   for (int i = 0; i < NIT; ++i) {
     const uint32_t base = base_of(i);
     if (base >= K) continue;
-    uint32_t packed[2] = {0u, 0u};
-    float q[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      q[e] = v[i][e] * inv;
-      if (!FP8) q[e] = __builtin_rintf(q[e]);
-      q[e] = __builtin_fminf(__builtin_fmaxf(q[e], -top), top);
-    }
+    uint2 packed;
     if constexpr (FP8) {
-      packed[0] = e4m3x4(q[0], q[1], q[2], q[3]);
-      packed[1] = e4m3x4(q[4], q[5], q[6], q[7]);
+      packed.x = e4m3x4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
+      packed.y = e4m3x4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) packed[e >> 2] |= ((uint32_t)(int32_t)q[e] & 0xFFu) << (8 * (e & 3));
+      packed = int8x8(v[i], inv);
     }
-    *(uint2*)(A.xq + row * A.K + base + 8 * lane) = make_uint2(packed[0], packed[1]);
+    *(uint2*)(A.xq + row * A.K + base + 8 * lane) = packed;
   }
   if (tid == 0) {
-    const float mean = ((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])) / (float)A.K;
-    const float rms = __builtin_sqrtf(mean + A.eps);
+    const float rms = __builtin_sqrtf(sum / (float)A.K + A.eps);
     // a NaN or an infinity anywhere in the row makes its scale NaN
     A.sx[row] = rms <= 3.4028234663852886e38f ? amax < 0x1p-100f ? 0.0f : amax / top / rms : __builtin_nanf("");
   }
@@ -156,22 +163,31 @@ __global__ __launch_bounds__(256) void hq_norm_prep_kernel(hq_norm_args A) {
 
 }  // namespace
 
+template <int W, int NIT, bool FP8, bool LONG>
+static void launch(const hq_norm_args& a, hipStream_t st) {
+  hipLaunchKernelGGL((hq_norm_prep_kernel<W, NIT, FP8, LONG>), dim3((uint32_t)a.M), dim3(64 * W), 0, st, a);
+}
+
+// Two blocks a wave, as many waves as that takes.  More blocks a wave leave less
+// in flight (1000 x 14336 at tile 512 without a residual: 16.4 us with 8 blocks on
+// four waves, 14.7 with 4 on eight, 14.2 with 2 on sixteen; 4000 x 8192 with one
+// 49.4, 46.7 and -), fewer make the barrier's share larger (8192 x 4096: 46.8 us with
+// 2 on four, 48.2 with 1 on eight).
 template <bool FP8>
 static void launch(const hq_norm_args& a, hipStream_t st) {
-  const dim3 grid((uint32_t)a.M), wg(256);
   if (a.tile > HQ_SUB) {
     if (a.K <= 8192)
-      hipLaunchKernelGGL((hq_norm_prep_kernel<4, FP8, true>), grid, wg, 0, st, a);
+      launch<4, 4, FP8, true>(a, st);
     else
-      hipLaunchKernelGGL((hq_norm_prep_kernel<8, FP8, true>), grid, wg, 0, st, a);
+      launch<8, 4, FP8, true>(a, st);
   } else if (a.K <= 2048) {
-    hipLaunchKernelGGL((hq_norm_prep_kernel<1, FP8, false>), grid, wg, 0, st, a);
+    launch<4, 1, FP8, false>(a, st);
   } else if (a.K <= 4096) {
-    hipLaunchKernelGGL((hq_norm_prep_kernel<2, FP8, false>), grid, wg, 0, st, a);
+    launch<4, 2, FP8, false>(a, st);
   } else if (a.K <= 8192) {
-    hipLaunchKernelGGL((hq_norm_prep_kernel<4, FP8, false>), grid, wg, 0, st, a);
+    launch<8, 2, FP8, false>(a, st);
   } else {
-    hipLaunchKernelGGL((hq_norm_prep_kernel<8, FP8, false>), grid, wg, 0, st, a);
+    launch<16, 2, FP8, false>(a, st);
   }
 }
 

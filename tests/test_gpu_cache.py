@@ -365,7 +365,7 @@ def test_refusals(hq):
         assert call(plan=kv) == -2 and call(plan=long) == -2
         assert call(c=cache(format=2)) == -1 and call(c=cache(heads=0)) == -1 and call(c=cache(heads=5)) == -1
         assert call(c=cache(block_tokens=24)) == -2 and call(c=cache(block_tokens=0)) == -1
-        assert call(c=cache(blocks=1 << 30)) == -2 and call(c=cache(blocks=-1)) == -1
+        assert call(c=cache(blocks=1 << 30)) == -2 and call(c=cache(blocks=0)) == -1
         assert call(c=cache(codes=None)) == -1 and call(c=cache(scales=kc.scales.data_ptr() + 4)) == -1
     assert attend(k=cache(blocks=0), v=cache(blocks=0)) == -1
     assert attend(v=cache(format=4)) == -1 and attend(v=cache(blocks=kc.blocks - 1)) == -1
