@@ -449,7 +449,7 @@ hq_status hq_decode_attention(hq_plan_t k_plan, const hq_stream* k, hq_plan_t v_
  *                 (HQ_MXFP4: 64): one head's tokens of a block are one run.
  *   scales        device, 16-byte aligned: fp32 [blocks, heads, block_tokens]
  *                 (HQ_MXFP4: bytes [blocks, heads, block_tokens, 4]).
- *   block_tokens  a multiple of 16 (HQ_ERR_UNSUPPORTED otherwise); one block at
+ *   block_tokens  a multiple of 16, 2^24 at most (HQ_ERR_UNSUPPORTED otherwise); one block at
  *                 least, blocks * block_tokens below 2^31.
  *   heads         KV heads; heads * 128 <= plan.cols (a plan's columns are a multiple
  *                 of 512, so 1, 2 or 3 heads use the first of its columns).

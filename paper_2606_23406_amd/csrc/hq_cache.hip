@@ -242,8 +242,10 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
     // H of the codes first, then the scale: integer codes sum exactly
     const float f = xor_sign(scale[i] * 0.0078125f, sg.sigma);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = live[i] ? v[e] * f : 0.0f;
+    for (int e = 0; e < 8; ++e) v[e] *= f;
     flip8(v, d[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = live[i] ? v[e] : 0.0f;
     if (t.in[i]) store8(A.y, (int64_t)t.row[i] * A.ldy + (t.head[i] * HQ_TILE + c0), A.y_bf16, v);
   }
 }
@@ -306,11 +308,28 @@ __device__ __forceinline__ void pairs_of(uint32_t w, float f, uint32_t* o) {
   }
 }
 
+// Maximum and sum over the four lane groups (lanes l, l ^ 16, l ^ 32, l ^ 48): a swap
+// of a value with itself leaves the two halves (or row pairs) side by side.
+typedef uint32_t v2u_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float groups_max(float x) {
+  const v2u_t a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const v2u_t b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float groups_sum(float x) {
+  const v2u_t a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const v2u_t b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 // ---- who does what
 // The tokens of a call are cut into chunks, about HQ_CACHE_WG_TARGET workgroups'
 // worth over all sequences and KV heads, so that a batch of uneven lengths keeps the
 // chip as busy as an even one.  Item j of the list is chunk j - first of sequence b.
 // Every wave finds its item by itself: 64 lengths a step, one per lane.
+constexpr int32_t kStep = 32 * HQ_CACHE_WAVES;
 struct CacheItem {
   int32_t b;       // -1: behind the last item
   int32_t n;       // chunks of this sequence (an empty one has one, which writes its zeros)
@@ -326,15 +345,15 @@ __device__ __forceinline__ int32_t cache_len(const hq_cache_attn_args& A, int64_
   return len < 0 ? 0 : (int32_t)cap;
 }
 
-// Chunks hold whole steps of four waves: multiples of 128 tokens, HQ_CACHE_LEAST at
-// least, one of 2^30 for any sequence.
+// Chunks hold whole steps of all waves, HQ_CACHE_LEAST tokens at least; one of 2^30
+// holds any sequence.
 __device__ __forceinline__ int32_t cache_chunk(const hq_cache_attn_args& A, int lane, bool tell) {
   int64_t total = 0;
   for (int64_t i = lane; i < A.batch; i += 64) total += cache_len(A, i, tell);
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
   const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
-  const int64_t chunk = min((even + 127) & ~(int64_t)127, (int64_t)1 << 30);
+  const int64_t chunk = min((even + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
   return (int32_t)readfirst((uint32_t)(chunk < HQ_CACHE_LEAST ? HQ_CACHE_LEAST : chunk));
 }
 
@@ -342,6 +361,14 @@ __device__ __forceinline__ int32_t cache_chunk(const hq_cache_attn_args& A, int 
 __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int64_t j, int64_t b, int lane,
                                                 bool tell) {
   CacheItem it;
+  if (!A.join) {  // one chunk each
+    it.b = (int32_t)(j >= 0 ? j : b);
+    it.n = 1;
+    it.first = it.b;
+    it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, true));
+    it.chunk = HQ_CACHE_LEAST;
+    return it;
+  }
   it.chunk = cache_chunk(A, lane, tell);
   it.b = -1;
   int64_t base = 0;
@@ -356,6 +383,8 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
       it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
       it.first = base + (uint32_t)__builtin_amdgcn_readlane(incl, at) - it.n;
       it.len = __builtin_amdgcn_readlane(len, at);
+      // even chunks: whole steps of all waves
+      it.chunk = (it.len + it.n * kStep - 1) / (it.n * kStep) * kStep;
       break;
     }
     base += all;
@@ -393,76 +422,78 @@ struct CacheStep {
 typedef __attribute__((address_space(3))) void lds_void;
 
 // A run of `bytes` from p on as a buffer resource (p the same in every lane).
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t run_of(const uint8_t* p, uint32_t bytes) {
-  const uint64_t a = (uint64_t)p;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t run_of(const void* p, int64_t at, uint32_t bytes) {
+  const uint64_t a = (uint64_t)p + at;
   const uint64_t u = (uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a);
   return __builtin_amdgcn_make_buffer_rsrc((void*)u, 0, bytes, 0x00020000);
 }
 
-// Where a wave stands in its sequence: block blk of the table row, token off of it.
-// The ids of 64 blocks ahead are one per lane, so that following the table costs a
-// lane read and not a load that the next loads' addresses wait for.
+// Where a wave stands in its sequence: token off of block blk of the table row, and
+// that block's head as buffers.  The ids of 64 blocks ahead are one per lane, so that
+// following the table costs a lane read and not a load that the next loads' addresses
+// wait for.
 struct CacheWalk {
   const int32_t* table;
   int32_t last;  // the sequence's last block
-  int32_t blk, off;
+  int32_t head, blk, off;
   int32_t first, ids;  // lane l: block first + l
-  __device__ __forceinline__ void fetch(int lane) {
+  __amdgpu_buffer_rsrc_t k, v, ks, vs;
+  bool bad;  // the block lies outside the cache: its buffers are empty
+  __device__ __forceinline__ void look_up(int lane) {
     first = blk;
     ids = table[min(blk + lane, last)];
+    // the wait for it stands here: at its uses it would wait for the tokens in flight
+    asm volatile("" : "+v"(ids));
   }
-  __device__ __forceinline__ int32_t id(int lane) {
-    if (blk - first >= 64) fetch(lane);
-    return __builtin_amdgcn_readlane(ids, blk - first);
+  template <int FMT>
+  __device__ __forceinline__ void enter(const hq_cache_attn_args& A, int lane) {
+    if (blk - first >= 64) look_up(lane);
+    const int32_t id = __builtin_amdgcn_readlane(ids, blk - first);
+    bad = (uint32_t)id >= (uint32_t)A.blocks;
+    if (bad && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
+    const uint32_t n = bad ? 0u : (uint32_t)A.block_tokens;
+    const int64_t row = bad ? 0 : ((int64_t)id * A.heads_kv + head) * A.block_tokens;
+    k = run_of(A.k_codes, row * row_bytes<FMT>(), n * row_bytes<FMT>());
+    v = run_of(A.v_codes, row * row_bytes<FMT>(), n * row_bytes<FMT>());
+    ks = run_of(A.k_scales, row * 4, n * 4);
+    vs = run_of(A.v_scales, row * 4, n * 4);
   }
-  __device__ __forceinline__ void advance(int32_t bt) {  // by 16 tokens, which divide a block
-    off += 16;
-    if (off == bt) {
-      off = 0;
-      ++blk;
+  // Starts the loads of the 32 tokens from t on into `step` (LDS) and moves the walk
+  // past them; live[h]: tokens of each half to attend to.
+  template <int FMT>
+  __device__ __forceinline__ void fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step,
+                                        int32_t (&live)[2]) {
+    using R = CacheRing<FMT>;
+    constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
+    const uint32_t row_in = lane / CPR, chunk = lane % CPR;
+    const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (t + 16 * h < end && off == A.block_tokens) {  // 16 divides a block
+        off = 0;
+        ++blk;
+        enter<FMT>(A, lane);
+      }
+      // a half behind the end loads its block's first tokens, one of a block outside the
+      // cache nothing, so that a step is always the same loads; nothing reads them
+      const int32_t some = min(max(end - t - 16 * h, 0), 16);
+      live[h] = bad ? 0 : some;
+      const uint32_t at = some ? off : 0;
+      off += 16;
+      uint8_t* to = step + h * R::HALF;
+#pragma unroll
+      for (uint32_t i = 0; i < 16 / RPL; ++i) {
+        const uint32_t rows = at * R::RB + i * 1024;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(k, (lds_void*)(to + i * 1024), 16, from, rows, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(v, (lds_void*)(to + R::V + i * 1024), 16, from, rows, 0, 0);
+      }
+      // lanes 16 and up load what nobody reads (the next tokens' scales, or nothing behind the block)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_void*)(to + R::SCALES), 4, lane * 4, at * 4, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_void*)(to + R::SCALES + 256), 4, lane * 4, at * 4, 0, 0);
     }
   }
 };
 
-// Starts the loads of the 32 tokens from t on into `step` (LDS) and moves the walk
-// past them; live[h]: tokens of each half to attend to.
-template <int FMT>
-__device__ __forceinline__ void cache_fetch(const hq_cache_attn_args& A, int32_t head, CacheWalk& w, int32_t t,
-                                            int32_t end, int lane, uint8_t* step, int32_t (&live)[2]) {
-  using R = CacheRing<FMT>;
-  constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
-  const uint32_t row_in = lane / CPR, chunk = lane % CPR;
-  const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    // dead halves (behind the end, or of a block outside the cache) load the cache's
-    // first tokens, so that a step is always the same loads; nothing reads them
-    int32_t b = 0, off = 0;
-    live[h] = min(max(end - t - 16 * h, 0), 16);
-    if (live[h] > 0) {
-      b = w.id(lane);
-      off = w.off;
-      if (b < 0 || b >= A.blocks) {
-        live[h] = b = off = 0;
-        if (head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
-      }
-      w.advance(A.block_tokens);
-    }
-    const int64_t row = ((int64_t)b * A.heads_kv + head) * A.block_tokens + off;
-    const __amdgpu_buffer_rsrc_t kr = run_of(A.k_codes + row * R::RB, 16 * R::RB);
-    const __amdgpu_buffer_rsrc_t vr = run_of(A.v_codes + row * R::RB, 16 * R::RB);
-    const __amdgpu_buffer_rsrc_t ksr = run_of((const uint8_t*)A.k_scales + row * 4, 64);
-    const __amdgpu_buffer_rsrc_t vsr = run_of((const uint8_t*)A.v_scales + row * 4, 64);
-    uint8_t* to = step + h * R::HALF;
-#pragma unroll
-    for (uint32_t i = 0; i < 16 / RPL; ++i) {
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(to + i * 1024), 16, from, i * 1024, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(to + R::V + i * 1024), 16, from, i * 1024, 0, 0);
-    }
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(ksr, (lds_void*)(to + R::SCALES), 4, lane * 4, 0, 0, 0);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(vsr, (lds_void*)(to + R::SCALES + 256), 4, lane * 4, 0, 0, 0);
-  }
-}
 
 // A step's codes and scales out of LDS.
 template <int FMT>
@@ -567,10 +598,11 @@ __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&
       for (int r = 0; r < 4; ++r)
         if (4 * g + r >= live[h]) p[h][r] = -__builtin_inff();
   }
-  float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(p[0][0], p[0][1]), __builtin_fmaxf(p[0][2], p[0][3])),
-                              __builtin_fmaxf(__builtin_fmaxf(p[1][0], p[1][1]), __builtin_fmaxf(p[1][2], p[1][3])));
-  top = __builtin_fmaxf(top, swz_xor16(top));
-  top = __builtin_fmaxf(top, lane_xor32(top));
+  // a NaN stays one: it makes the head's outputs NaN
+  float top = p[0][0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) top = __builtin_elementwise_maximum(top, p[i >> 2][i & 3]);
+  top = groups_max(top);
   if (__ballot(top > z.m)) {  // some column has a new maximum: all sums move to theirs
     const float mn = __builtin_fmaxf(z.m, top);
     const float alpha = __builtin_amdgcn_exp2f(z.m - (mn == -__builtin_inff() ? 0.0f : mn));
@@ -640,18 +672,16 @@ __device__ __forceinline__ void cache_finish(const hq_cache_attn_args& A, float 
   for (int i = 0; i < 8; ++i) v[i] *= inv;
   const XSigns sg(lane);
   fwht128(v, sg);
-  const uint32_t dbits = sign_bits8(A.v_dmask, (int64_t)head * HQ_TILE + (lane & 15) * 8);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = flip(v[i], dbits, i);
+  flip8(v, sign_words(A.v_dsign16, head * HQ_TILE + (lane & 15) * 8));
 }
 
 template <int FMT, bool PACK>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_attn_kernel(
+__global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_attn_kernel(
     hq_cache_attn_args A) {
   using R = CacheRing<FMT>;
   constexpr int HEADS = PACK ? 4 : 16, T = PACK ? 1 : 3;
   extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];  // a wave's ring after the other
-  __shared__ float s_m[HQ_WAVES_PER_WG][HEADS], s_l[HQ_WAVES_PER_WG][HEADS];
+  __shared__ float s_m[HQ_CACHE_WAVES][HEADS], s_l[HQ_CACHE_WAVES][HEADS];
   // term i of the query lies in the second step of wave i's ring until that is first
   // loaded, a wave's sums in its own ring at the end
   static_assert(16 * kQPitch * sizeof(uint16_t) <= R::STEP && HEADS * kOPitch * sizeof(float) <= R::WAVE, "");
@@ -670,32 +700,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     if (grp < G) store8(A.out, (pair0 + grp) * HQ_TILE + c0, A.out_bf16, zero);
     return;
   }
-  const int32_t per = it.chunk / HQ_WAVES_PER_WG;
-  const int64_t begin64 = (j - it.first) * it.chunk + wave * per;
-  const int32_t begin = (int32_t)min(begin64, (int64_t)it.len), end = min(it.len, begin + per);
+  // the query's loads, then the table's, then the tokens': each is waited for once
+  float qv[8] = {};
+  uint4 qd = {};
+  if (grp < G) {
+    load8(A.q, (pair0 + grp) * HQ_TILE + c0, A.q_bf16, qv);
+    qd = sign_words(A.k_dsign16, head * HQ_TILE + c0);
+  }
+  // the chunk's steps of 32 tokens shared out over the waves
+  const int32_t begin0 = (int32_t)((j - it.first) * it.chunk), tokens = min(it.chunk, it.len - begin0);
+  const int32_t per = (tokens + 32 * HQ_CACHE_WAVES - 1) / (32 * HQ_CACHE_WAVES) * 32;
+  const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
   CacheWalk w;
   w.table = A.table + (int64_t)it.b * A.max_blocks;
   w.last = (it.len - 1) / A.block_tokens;
-  w.blk = begin / A.block_tokens;
+  w.head = head;
+  w.blk = min(begin / A.block_tokens, w.last);
   w.off = begin - w.blk * A.block_tokens;
-  w.fetch(lane);
+  w.look_up(lane);
+  w.enter<FMT>(A, lane);
   uint8_t* ring = s_ring + wave * R::WAVE;
   int32_t live[2], next[2] = {0, 0};
-  if (begin < end) cache_fetch<FMT>(A, head, w, begin, end, lane, ring, live);
+  if (begin < end) w.fetch<FMT>(A, begin, end, lane, ring, live);
   // ---- the query into the cache's coordinates, as three bf16 terms
-  if (grp < HEADS || !PACK) {
-    float v[8] = {};
-    if (grp < G) {
-      load8(A.q, (pair0 + grp) * HQ_TILE + c0, A.q_bf16, v);
-      const uint32_t dbits = sign_bits8(A.k_dmask, (int64_t)head * HQ_TILE + c0);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = flip(v[i], dbits, i);
-    }
+  if (grp < HEADS) {
+    flip8(qv, qd);
     const XSigns sg(lane);
-    fwht128(v, sg);
+    fwht128(qv, sg);
     uint32_t t[8][3];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) three_terms(v[i] * A.qscale, t[i]);
+    for (int i = 0; i < 8; ++i) three_terms(qv[i] * A.qscale, t[i]);
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       uint4 o;
@@ -725,7 +759,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   z.l = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) z.acc[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  if (begin + 32 < end) cache_fetch<FMT>(A, head, w, begin + 32, end, lane, ring + R::STEP, next);
+  if (begin + 32 < end) w.fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP, next);
   int32_t slot = 0;
   for (int32_t t = begin; t < end; t += 32) {
     // the loads of this step are done when at most the next step's are not
@@ -740,14 +774,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     live[1] = next[1];
     if (t + 64 < end) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
-      cache_fetch<FMT>(A, head, w, t + 64, end, lane, ring + slot * R::STEP, next);
+      w.fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next);
     }
     slot ^= 1;
     cache_step<FMT, PACK>(cur, here, q, lane, z);
   }
-  z.l += swz_xor16(z.l);
-  z.l += lane_xor32(z.l);
-  // ---- the four waves' sums under one maximum, one head per 16 lanes
+  z.l = groups_sum(z.l);
+  // ---- the waves' sums under one maximum, one head per 16 lanes
   if constexpr (PACK) {
     // the terms' sums: in the fourth lane of a head the weights' columns were a term over again
     const float keep = (n & 3) == 3 ? 0.0f : 1.0f;
@@ -786,10 +819,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   if (grp >= G) return;
   float M = s_m[0][grp], L = 0.0f, v[8] = {};
 #pragma unroll
-  for (int x = 1; x < HQ_WAVES_PER_WG; ++x) M = __builtin_fmaxf(M, s_m[x][grp]);
+  for (int x = 1; x < HQ_CACHE_WAVES; ++x) M = __builtin_fmaxf(M, s_m[x][grp]);
   const float ref = M == -__builtin_inff() ? 0.0f : M;
 #pragma unroll
-  for (int x = 0; x < HQ_WAVES_PER_WG; ++x) {
+  for (int x = 0; x < HQ_CACHE_WAVES; ++x) {
     const float f = __builtin_amdgcn_exp2f(s_m[x][grp] - ref);
     L = __builtin_fmaf(f, s_l[x][grp], L);
 #pragma unroll
@@ -820,22 +853,43 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
   const CacheItem it = cache_item(A, -1, b, lane, false);
   if (it.n == 1) return;  // already whole
   const int64_t part0 = (it.first * A.heads_kv + head) * A.group + (hq - head * A.group);
-  float M = -__builtin_inff();
-  for (int32_t x = grp; x < it.n; x += 16) M = __builtin_fmaxf(M, A.part_m[part0 + (int64_t)x * A.heads_q]);
+  // a group's first four chunks are loaded whole before the maxima meet
+  float M = -__builtin_inff(), m[4], l[4], a[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int32_t x = grp + 16 * i;
+    m[i] = M;
+    l[i] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[i][e] = 0.0f;
+    if (x >= it.n) continue;
+    const int64_t part = part0 + (int64_t)x * A.heads_q;
+    m[i] = A.part_m[part];
+    l[i] = A.part_l[part];
+    load8(A.part_acc, part * HQ_TILE + c0, false, a[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) M = __builtin_fmaxf(M, m[i]);
+  for (int32_t x = grp + 64; x < it.n; x += 16) M = __builtin_fmaxf(M, A.part_m[part0 + (int64_t)x * A.heads_q]);
   if (n == 0) s_red[grp] = M;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 16; ++k) M = __builtin_fmaxf(M, s_red[k]);
   const float ref = M == -__builtin_inff() ? 0.0f : M;
   float L = 0.0f, v[8] = {};
-  for (int32_t x = grp; x < it.n; x += 16) {
-    const int64_t part = part0 + (int64_t)x * A.heads_q;
-    const float f = __builtin_amdgcn_exp2f(A.part_m[part] - ref);
-    L = __builtin_fmaf(f, A.part_l[part], L);
-    float a[8];
-    load8(A.part_acc, part * HQ_TILE + c0, false, a);
+  auto add = [&](float mx, float lx, const float* ax) {
+    const float f = __builtin_amdgcn_exp2f(mx - ref);
+    L = __builtin_fmaf(f, lx, L);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(f, a[i], v[i]);
+    for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(f, ax[e], v[e]);
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) add(m[i], l[i], a[i]);
+  for (int32_t x = grp + 64; x < it.n; x += 16) {
+    const int64_t part = part0 + (int64_t)x * A.heads_q;
+    float ax[8];
+    load8(A.part_acc, part * HQ_TILE + c0, false, ax);
+    add(A.part_m[part], A.part_l[part], ax);
   }
   __syncthreads();  // every group has read s_red
   s_acc[grp][2 * n] = make_float4(v[0], v[1], v[2], v[3]);
@@ -848,9 +902,9 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
   for (int i = 0; i < 8; ++i) v[i] = 0.0f;
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
-    const float4 a0 = s_acc[k][2 * n], a1 = s_acc[k][2 * n + 1];
-    v[0] += a0.x; v[1] += a0.y; v[2] += a0.z; v[3] += a0.w;
-    v[4] += a1.x; v[5] += a1.y; v[6] += a1.z; v[7] += a1.w;
+    const float4 x = s_acc[k][2 * n], y = s_acc[k][2 * n + 1];
+    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+    v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
     L += s_red[k];
   }
   cache_finish(A, L, v, head, lane);
@@ -881,9 +935,9 @@ int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream) {
 template <int FMT, bool PACK>
 static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
   static hq_lds_granted granted;
-  constexpr size_t lds = (size_t)HQ_WAVES_PER_WG * CacheRing<FMT>::WAVE;
+  constexpr size_t lds = (size_t)HQ_CACHE_WAVES * CacheRing<FMT>::WAVE;
   if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, PACK>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, PACK>), grid, dim3(256), lds, st, a);
+  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, PACK>), grid, dim3(64 * HQ_CACHE_WAVES), lds, st, a);
   return 0;
 }
 

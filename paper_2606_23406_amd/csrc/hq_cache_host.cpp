@@ -22,7 +22,7 @@ hq_status check_cache(const hq_plan_s* p, const hq_cache* c) {
   if (c->format != HQ_INT8 && c->format != HQ_E4M3 && c->format != HQ_MXFP4) return HQ_ERR_INVALID_ARG;
   if (c->heads <= 0 || (int64_t)c->heads * HQ_TILE > p->cols || c->blocks <= 0 || c->block_tokens <= 0)
     return HQ_ERR_INVALID_ARG;
-  if (c->block_tokens % 16 != 0) return HQ_ERR_UNSUPPORTED;
+  if (c->block_tokens % 16 != 0 || c->block_tokens > 1 << 24) return HQ_ERR_UNSUPPORTED;  // 32-bit bytes of a block
   if (c->blocks > 0x7FFFFFFF / c->block_tokens) return HQ_ERR_UNSUPPORTED;  // slots are 31-bit
   if (!c->codes || !c->scales || !aligned(c->codes, 16) || !aligned(c->scales, 16)) return HQ_ERR_INVALID_ARG;
   return HQ_OK;
@@ -187,8 +187,8 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
   a.k_scales = k->scales;
   a.v_codes = (const uint8_t*)v->codes;
   a.v_scales = v->scales;
-  a.k_dmask = kp->d_dmask;
-  a.v_dmask = vp->d_dmask;
+  a.k_dsign16 = kp->d_dsign16;
+  a.v_dsign16 = vp->d_dsign16;
   a.q = q;
   a.out = out;
   a.table = block_table;
@@ -201,7 +201,7 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
   }
   a.stats = k->stats;
   a.batch = batch;
-  a.blocks = k->blocks;
+  a.blocks = (int32_t)k->blocks;
   a.heads_q = heads_q;
   a.heads_kv = k->heads;
   a.group = (int32_t)group;

@@ -286,8 +286,8 @@ struct hq_cache_attn_args {
   const void* k_scales;
   const uint8_t* v_codes;
   const void* v_scales;
-  const uint32_t* k_dmask;
-  const uint32_t* v_dmask;
+  const uint32_t* k_dsign16;  // RHT signs as bf16 XOR words, one per column pair
+  const uint32_t* v_dsign16;
   const void* q;
   void* out;
   const int32_t* table;     // batch x max_blocks block ids
@@ -296,17 +296,25 @@ struct hq_cache_attn_args {
   float* part_m;
   float* part_l;
   hq_stats* stats;
-  int64_t batch, blocks;
+  int64_t batch;
   int64_t items;            // bound on the chunks of all sequences
   int32_t heads_q, heads_kv, group;
-  int32_t max_blocks, block_tokens;
+  int32_t max_blocks, blocks, block_tokens;
   int32_t join;             // a sequence may have several chunks
   int32_t q_bf16, out_bf16;
   float qscale;             // softmax scale times log2(e) / 128
 };
 
+// Workgroups of four waves; their rings take 70 KB of LDS each in the 8-bit formats, so
+// two fit a CU and 512 the chip: one round of them, and the chunks are cut for that.
+// 16 sequences of 8192 tokens take 59.2 us at 512, 64.7 at 1024 and 69.6 at 768 (a
+// part of a round more); with eight waves and 256 they take 59.8 and uneven lengths,
+// whose rounding then opens a second round, 29.9 instead of 20.5.
+#define HQ_CACHE_WAVES 4
 #define HQ_CACHE_WG_TARGET 512  // workgroups a cache attention call aims at
-#define HQ_CACHE_LEAST 512      // tokens of the smallest chunk
+// Tokens of the smallest chunk.  Four steps of a wave take 3 us more than one, and
+// joining chunks a launch of 4 to 5 us: 512 tokens of 8 KV heads take 8.5 us whole.
+#define HQ_CACHE_LEAST 512
 
 // Bound on the chunks of a call's sequences: a chunk is at least HQ_CACHE_LEAST
 // tokens and total * heads_kv / HQ_CACHE_WG_TARGET, so all sequences together have

@@ -531,12 +531,14 @@ def _on_device(*tensors):
 
 def _rows(t, rows, width, dtype, name):
     """A [rows, width] tensor of `dtype` with contiguous rows: its row stride."""
-    if t.dtype != dtype or t.shape != (rows, width):
+    if t.dtype is not dtype or t.shape != (rows, width):
         raise ValueError(f"{name} must be {dtype} [{rows}, {width}]")
+    if t.is_contiguous():
+        return width
     ld, step = t.stride()
-    if step != 1 and width > 1:
+    if step != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return ld if rows > 1 else max(ld, width)
+    return ld if rows > 1 else width
 
 
 class Cache:
