@@ -521,7 +521,7 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
  *                nearest even), 16-byte aligned.
  *   workspace    device, 16-byte aligned, >= hq_cache_attention_workspace_bytes(
  *                k, batch, heads_q, max_blocks); may be null where max_blocks *
- *                block_tokens is at most 512.  Calls that may overlap (on two
+ *                block_tokens is at most 1024.  Calls that may overlap (on two
  *                streams, or two captured graphs that may) need one each.
  * Scores, maxima and sums are fp32, in an order fixed by the call's shape and its
  * lengths, so results repeat bit for bit.  Device-side, in k->stats: a

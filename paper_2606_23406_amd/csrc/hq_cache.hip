@@ -325,15 +325,15 @@ __device__ __forceinline__ float groups_sum(float x) {
 }
 
 // ---- who does what
-// The tokens of a call are cut into chunks, about HQ_CACHE_WG_TARGET workgroups'
-// worth over all sequences and KV heads, so that a batch of uneven lengths keeps the
-// chip as busy as an even one.  Item j of the list is chunk j - first of sequence b.
-// Every wave finds its item by itself: 64 lengths a step, one per lane.
+// The tokens of a call are cut into chunks of about one length, as many workgroups
+// as the chip holds at once over all sequences and KV heads, so that a batch of uneven
+// lengths keeps it as busy as an even one.  Item j is chunk j - first of sequence b.
+// Every wave finds its item by itself, 64 lengths a step, one per lane.
 constexpr int32_t kStep = 32 * HQ_CACHE_WAVES;
 struct CacheItem {
   int32_t b;       // -1: behind the last item
   int32_t n;       // chunks of this sequence (an empty one has one, which writes its zeros)
-  int64_t first;   // the sequence's first item
+  int32_t first;   // the sequence's first item
   int32_t len, chunk;
 };
 
@@ -345,43 +345,60 @@ __device__ __forceinline__ int32_t cache_len(const hq_cache_attn_args& A, int64_
   return len < 0 ? 0 : (int32_t)cap;
 }
 
-// Chunks hold whole steps of all waves, HQ_CACHE_LEAST tokens at least; one of 2^30
-// holds any sequence.
-__device__ __forceinline__ int32_t cache_chunk(const hq_cache_attn_args& A, int lane, bool tell) {
-  int64_t total = 0;
-  for (int64_t i = lane; i < A.batch; i += 64) total += cache_len(A, i, tell);
+// The longest a chunk may be: whole steps of all waves, HQ_CACHE_LEAST tokens at
+// least; one of 2^30 holds any sequence.  An even share of the workgroups aimed at
+// would be right if every sequence were a multiple of it.  A sequence's last chunk is
+// not, and what that adds opens a second round of workgroups, so the share grows by
+// eighths until the chunks fit but for a few, to its double at most.  (24 sequences of
+// up to 6001 tokens, 8 KV heads in E4M3: 560 chunks of the even share take 51.7 us, 528 of
+// its 9 / 8 take 41.4.)  `mine`: the lane's own length, of the first 64 sequences.
+__device__ __forceinline__ int32_t cache_chunk(const hq_cache_attn_args& A, int lane, int32_t mine, bool tell) {
+  int64_t total = mine;
+  for (int64_t i = lane + 64; i < A.batch; i += 64) total += cache_len(A, i, tell);
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
   const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
-  const int64_t chunk = min((even + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
-  return (int32_t)readfirst((uint32_t)(chunk < HQ_CACHE_LEAST ? HQ_CACHE_LEAST : chunk));
+  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.heads_kv;
+  int32_t chunk = HQ_CACHE_LEAST;
+  for (int e = 8; e <= 16; ++e) {
+    const int64_t c = min(((even * e >> 3) + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
+    chunk = max(chunk, (int32_t)readfirst((uint32_t)c));
+    // about: a length a hair over a multiple may count as the multiple
+    const float per = __builtin_amdgcn_rcpf((float)chunk) * 0.999999f;
+    uint32_t n = lane < A.batch ? max(1u, (uint32_t)__builtin_ceilf((float)mine * per)) : 0u;
+    for (int64_t i = lane + 64; i < A.batch; i += 64)
+      n += max(1u, (uint32_t)__builtin_ceilf((float)cache_len(A, i, false) * per));
+    const uint32_t all = wave_total(n);
+    if (all <= few || A.batch > few) break;  // more sequences than that: several rounds in any case
+  }
+  return chunk;
 }
 
-// By item (j >= 0) or by sequence (j < 0).
-__device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int64_t j, int64_t b, int lane,
-                                                bool tell) {
+__device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int32_t j, int lane, bool tell) {
   CacheItem it;
   if (!A.join) {  // one chunk each
-    it.b = (int32_t)(j >= 0 ? j : b);
+    it.b = -1;
+    if (j >= A.batch) return it;
+    it.b = it.first = j;
     it.n = 1;
-    it.first = it.b;
     it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, true));
-    it.chunk = HQ_CACHE_LEAST;
+    it.chunk = HQ_CACHE_WHOLE;
     return it;
   }
-  it.chunk = cache_chunk(A, lane, tell);
+  int32_t len = lane < A.batch ? cache_len(A, lane, tell) : 0;
+  const uint32_t chunk = (uint32_t)cache_chunk(A, lane, len, tell);
   it.b = -1;
-  int64_t base = 0;
+  int32_t base = 0;
   for (int64_t i0 = 0; i0 < A.batch; i0 += 64) {
     const bool in = i0 + lane < A.batch;
-    const int32_t len = in ? cache_len(A, i0 + lane, false) : 0;
-    const uint32_t n = !in ? 0u : len == 0 ? 1u : ((uint32_t)len + it.chunk - 1) / (uint32_t)it.chunk;
-    const uint32_t incl = wave_scan_incl(n), all = __builtin_amdgcn_readlane(incl, 63);
-    if (j >= 0 ? j < base + all : b < i0 + 64) {
-      const int at = j >= 0 ? __popcll(__ballot(base + incl <= j)) : (int)(b - i0);
+    if (i0) len = in ? cache_len(A, i0 + lane, false) : 0;
+    const uint32_t n = !in ? 0u : len == 0 ? 1u : ((uint32_t)len + chunk - 1) / chunk;
+    const int32_t incl = (int32_t)wave_scan_incl(n), all = __builtin_amdgcn_readlane(incl, 63);
+    if (j < base + all) {
+      const int at = __popcll(__ballot(base + incl <= j));
       it.b = (int32_t)i0 + at;
       it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
-      it.first = base + (uint32_t)__builtin_amdgcn_readlane(incl, at) - it.n;
+      it.first = base + __builtin_amdgcn_readlane(incl, at) - it.n;
       it.len = __builtin_amdgcn_readlane(len, at);
       // even chunks: whole steps of all waves
       it.chunk = (it.len + it.n * kStep - 1) / (it.n * kStep) * kStep;
@@ -689,10 +706,12 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   auto o_row = [&](int w, int row) { return (float*)(s_ring + w * R::WAVE) + row * kOPitch; };
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4, grp = tid >> 4;
   const int wave = (int)readfirst((uint32_t)(tid >> 6));
-  const uint32_t j = blockIdx.x / (uint32_t)A.heads_kv;
-  const int32_t head = (int32_t)(blockIdx.x - j * (uint32_t)A.heads_kv);
-  const CacheItem it = cache_item(A, j, 0, lane, blockIdx.x == 0 && wave == 0);
+  const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.heads_kv);
+  const int32_t head = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.heads_kv);
+  const CacheItem it = cache_item(A, j, lane, blockIdx.x == 0 && wave == 0);
   if (it.b < 0) return;
+  // what the join goes by
+  if (A.join && j == it.first && head == 0 && tid == 0) A.parts[it.b] = {it.first, it.n};
   const int32_t G = A.group, c0 = n * 8;
   const int64_t pair0 = (int64_t)it.b * A.heads_q + (int64_t)head * G;
   if (it.len == 0) {
@@ -850,9 +869,10 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
   const int64_t pair = blockIdx.x;
   const int64_t b = pair / A.heads_q;
   const int32_t hq = (int32_t)(pair - b * A.heads_q), head = hq / A.group;
-  const CacheItem it = cache_item(A, -1, b, lane, false);
-  if (it.n == 1) return;  // already whole
-  const int64_t part0 = (it.first * A.heads_kv + head) * A.group + (hq - head * A.group);
+  const hq_cache_of has = A.parts[b];
+  const int32_t parts = has.n;
+  if (parts == 1) return;  // already whole
+  const int64_t part0 = ((int64_t)has.first * A.heads_kv + head) * A.group + (hq - head * A.group);
   // a group's first four chunks are loaded whole before the maxima meet
   float M = -__builtin_inff(), m[4], l[4], a[4][8];
 #pragma unroll
@@ -862,7 +882,7 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
     l[i] = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) a[i][e] = 0.0f;
-    if (x >= it.n) continue;
+    if (x >= parts) continue;
     const int64_t part = part0 + (int64_t)x * A.heads_q;
     m[i] = A.part_m[part];
     l[i] = A.part_l[part];
@@ -870,7 +890,7 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) M = __builtin_fmaxf(M, m[i]);
-  for (int32_t x = grp + 64; x < it.n; x += 16) M = __builtin_fmaxf(M, A.part_m[part0 + (int64_t)x * A.heads_q]);
+  for (int32_t x = grp + 64; x < parts; x += 16) M = __builtin_fmaxf(M, A.part_m[part0 + (int64_t)x * A.heads_q]);
   if (n == 0) s_red[grp] = M;
   __syncthreads();
 #pragma unroll
@@ -885,7 +905,7 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
   };
 #pragma unroll
   for (int i = 0; i < 4; ++i) add(m[i], l[i], a[i]);
-  for (int32_t x = grp + 64; x < it.n; x += 16) {
+  for (int32_t x = grp + 64; x < parts; x += 16) {
     const int64_t part = part0 + (int64_t)x * A.heads_q;
     float ax[8];
     load8(A.part_acc, part * HQ_TILE + c0, false, ax);

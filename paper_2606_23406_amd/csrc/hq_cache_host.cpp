@@ -151,8 +151,10 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
   if (!k || batch <= 0 || heads_q <= 0 || max_blocks <= 0 || k->heads <= 0 || k->block_tokens <= 0 ||
       heads_q % k->heads != 0)
     return 0;
-  const int64_t n = hq_cache_items(batch, k->heads, (int64_t)max_blocks * k->block_tokens) * heads_q;
-  return (size_t)n * (HQ_TILE + 2) * sizeof(float);
+  const int64_t max_tokens = (int64_t)max_blocks * k->block_tokens;
+  if (max_tokens <= HQ_CACHE_WHOLE) return 0;
+  const int64_t n = hq_cache_items(batch, k->heads, max_tokens) * heads_q;
+  return (size_t)n * (HQ_TILE + 2) * sizeof(float) + (size_t)batch * sizeof(hq_cache_of);
 }
 
 hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, const hq_cache* v, const void* q,
@@ -175,7 +177,7 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
       !aligned(seq_lens, 4))
     return HQ_ERR_INVALID_ARG;
   const int64_t items = hq_cache_items(batch, k->heads, max_tokens);
-  const bool join = max_tokens > HQ_CACHE_LEAST;
+  const bool join = max_tokens > HQ_CACHE_WHOLE;
   if (items * heads_q > 0x7FFFFFFF) return HQ_ERR_UNSUPPORTED;
   if (join && (!workspace || !aligned(workspace, 16) ||
                ws_bytes < hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)))
@@ -198,6 +200,7 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
     a.part_acc = (float*)workspace;
     a.part_m = a.part_acc + n * HQ_TILE;
     a.part_l = a.part_m + n;
+    a.parts = (hq_cache_of*)(a.part_l + n);
   }
   a.stats = k->stats;
   a.batch = batch;

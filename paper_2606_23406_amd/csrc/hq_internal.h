@@ -278,6 +278,11 @@ struct hq_cache_io_args {
   int32_t y_bf16;
 };
 
+// A sequence's first item of a cache attention, and how many it has.
+struct hq_cache_of {
+  int32_t first, n;
+};
+
 // One-token attention over a fixed-rate cache.  Workspace (where a sequence may
 // be split): per (item, query head of its KV heads) the sum of 128 values, its
 // maximum and its weight.
@@ -295,6 +300,7 @@ struct hq_cache_attn_args {
   float* part_acc;
   float* part_m;
   float* part_l;
+  hq_cache_of* parts;       // per sequence
   hq_stats* stats;
   int64_t batch;
   int64_t items;            // bound on the chunks of all sequences
@@ -312,15 +318,18 @@ struct hq_cache_attn_args {
 // whose rounding then opens a second round, 29.9 instead of 20.5.
 #define HQ_CACHE_WAVES 4
 #define HQ_CACHE_WG_TARGET 512  // workgroups a cache attention call aims at
-// Tokens of the smallest chunk.  Four steps of a wave take 3 us more than one, and
-// joining chunks a launch of 4 to 5 us: 512 tokens of 8 KV heads take 8.5 us whole.
+// Tokens of the smallest chunk, and tokens of the longest sequence that a call may
+// have whose sequences are not split at all.  Joining chunks takes a launch of 4 us, and
+// a wave's step of 32 tokens 0.5 to 1.
 #define HQ_CACHE_LEAST 512
+#define HQ_CACHE_WHOLE 1024
 
-// Bound on the chunks of a call's sequences: a chunk is at least HQ_CACHE_LEAST
-// tokens and total * heads_kv / HQ_CACHE_WG_TARGET, so all sequences together have
-// at most HQ_CACHE_WG_TARGET / heads_kv beside the one each that rounding adds.
-// Grows with every argument but heads_kv; times heads_kv it grows with that too.
+// Bound on the chunks of a call's sequences, one each where none is split.  A chunk is
+// at least HQ_CACHE_LEAST tokens and total * heads_kv / HQ_CACHE_WG_TARGET, so all
+// sequences together have at most HQ_CACHE_WG_TARGET / heads_kv beside the one each that
+// rounding adds.
 static inline int64_t hq_cache_items(int64_t batch, int64_t heads_kv, int64_t max_tokens) {
+  if (max_tokens <= HQ_CACHE_WHOLE) return batch;
   const int64_t most = (max_tokens + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST;
   const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
   return batch * most < batch + even ? batch * most : batch + even;

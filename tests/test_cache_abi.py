@@ -57,17 +57,26 @@ def test_chunks_fit_the_workspace(hq, tmp_path):
                     str(src)], check=True)
     L = hq.lib()
     rng = np.random.default_rng(0)
-    for batch, heads, blocks in [(1, 1, 1), (1, 8, 8192), (3, 3, 400), (64, 8, 33), (65, 2, 700), (300, 1, 1000),
+    for batch, heads, blocks in [(1, 1, 1), (8, 8, 63), (8, 8, 64), (8, 8, 65), (1, 8, 8192), (3, 3, 400), (64, 8, 33), (65, 2, 700), (300, 1, 1000),
                                  (2000, 16, 64), (1, 512, 100), (7, 600, 90)]:
         target, least, items = map(int, subprocess.run([str(exe), str(batch), str(heads), str(16 * blocks)],
                                                        capture_output=True, text=True, check=True).stdout.split())
+        if 16 * blocks <= 1024:  # no sequence is split: workgroup j takes sequence j
+            assert items == batch
+            assert L.hq_cache_attention_workspace_bytes(C.byref(hq.CacheStruct(None, None, 1, 16, heads, 3, 0, None)),
+                                                        batch, 2 * heads, blocks) == 0
+            continue
         for lens in (np.full(batch, 16 * blocks), rng.integers(0, 16 * blocks + 1, batch),
                      np.where(np.arange(batch) == 0, 16 * blocks, 1), np.zeros(batch, np.int64)):
-            chunk = max(least, (-(-int(lens.sum()) * heads // target) + 127) // 128 * 128)
-            n = np.where(lens == 0, 1, -(-lens // chunk))
-            assert batch <= n.sum() <= items, (batch, heads, blocks)
+            even = -(-int(lens.sum()) * heads // target)
+            for eighths in range(8, 17):  # the kernel takes one of these
+                chunk = max(least, ((even * eighths >> 3) + 127) // 128 * 128)
+                n = np.where(lens == 0, 1, -(-lens // chunk))
+                assert batch <= n.sum() <= items, (batch, heads, blocks)
+                own = -(-lens // (n * 128)) * 128  # the even chunk of each
+                assert (own * n >= lens).all() and (own * (n - 1) <= lens).all()
         c = hq.CacheStruct(None, None, 1, 16, heads, 3, 0, None)
-        assert items * heads * 2 * 130 * 4 == L.hq_cache_attention_workspace_bytes(C.byref(c), batch, 2 * heads, blocks)
+        assert items * heads * 2 * 130 * 4 + batch * 8 == L.hq_cache_attention_workspace_bytes(C.byref(c), batch, 2 * heads, blocks)
 
 
 def test_the_oracle_transforms_back():

@@ -179,7 +179,8 @@ def test_attention_heads(hq, fmt, heads, group):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
-@pytest.mark.parametrize("lens", [[1000], [2500, 3, 0, 700], [9000], [64] * 70, [5] * 600])
+@pytest.mark.parametrize("lens", [[1000], [2500, 3, 0, 700], [9000], [64] * 70, [5] * 600, [0] * 66 + [600, 1, 1300], [1000] * 9, [1024, 0, 513],
+                                  [129 * (i % 7) for i in range(150)], [0, 0, 513]])
 def test_attention_splits_and_joins(hq, fmt, lens):
     print(f"[cache] attention splits {fmt} {len(lens)} x {max(lens)}", flush=True)
     case = attention_case(hq, fmt, lens, 2, 4, 64, seed=3)
@@ -287,7 +288,7 @@ def test_streams_and_graphs(hq):
     """A step (write, attend) on a side stream and captured, each replay equal to the eager run on
     the same inputs."""
     heads, group, bt = 4, 4, 32
-    case = attention_case(hq, "int8", [700, 33], heads, group, bt, seed=12)
+    case = attention_case(hq, "int8", [1700, 33], heads, group, bt, seed=12)
     kp, vp, kc, vc, table, q, ln, scale = case
     table, q, ln = table.cuda(), q.cuda(), ln.cuda()
     k, v = (x.cuda() for x in inputs(2, heads, torch.bfloat16, 13))
