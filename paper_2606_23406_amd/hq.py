@@ -163,9 +163,9 @@ def _stream_handle(stream=None):
 
 
 def _dtype_code(dt):
-    if dt == torch.bfloat16:
+    if dt is torch.bfloat16:
         return HQ_BF16
-    if dt == torch.float32:
+    if dt is torch.float32:
         return HQ_FP32
     raise ValueError(f"unsupported dtype {dt}")
 
@@ -521,24 +521,32 @@ def hq_decode_attention(k_plan: Plan, k: EncodedStream, v_plan: Plan, v: Encoded
     return out
 
 
-def _on_device(*tensors):
-    """The tensors lie on the current device, whose stream the call goes to."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t.get_device() != dev:
-            raise ValueError(f"a tensor on {t.device} in a call on cuda:{dev}")
+def _dense(t, dtype, shape, dev, name):
+    """The address of a contiguous tensor of one type, shape and (the current) device."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} on cuda:{dev}, not "
+                     f"{t.dtype} {list(t.shape)} of strides {t.stride()} on {t.device}")
 
 
-def _rows(t, rows, width, dtype, name):
-    """A [rows, width] tensor of `dtype` with contiguous rows: its row stride."""
-    if t.dtype is not dtype or t.shape != (rows, width):
-        raise ValueError(f"{name} must be {dtype} [{rows}, {width}]")
-    if t.is_contiguous():
-        return width
-    ld, step = t.stride()
-    if step != 1:
-        raise ValueError(f"{name} must have contiguous rows")
-    return ld if rows > 1 else width
+def _rows(t, dtype, shape, dev, name):
+    """Address and row stride of a [rows, width] tensor whose rows are contiguous."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+        if t.is_contiguous():
+            return t.data_ptr(), shape[1]
+        ld, step = t.stride()
+        if step == 1:
+            return t.data_ptr(), ld if shape[0] > 1 else shape[1]
+    raise ValueError(f"{name} must be {dtype} {list(shape)} with contiguous rows on cuda:{dev}, not "
+                     f"{t.dtype} {list(t.shape)} of strides {t.stride()} on {t.device}")
+
+
+def _empty(shape, dtype, dev, stream):
+    """New memory of the stream that the call goes to."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
 
 
 class Cache:
@@ -584,42 +592,45 @@ class Cache:
             self.stats.zero_()
 
 
-def _slots(slots, rows):
-    if slots.dtype != torch.int64 or slots.shape != (rows,) or not slots.is_contiguous():
-        raise ValueError("slots must be a contiguous int64 tensor, one per row")
-    return slots.data_ptr()
-
-
 def hq_cache_write(k_plan: Plan, k: torch.Tensor, k_cache: Cache, v_plan, v, v_cache,
                    slots: torch.Tensor, stream=None):
     """hq_cache_write: k and v [rows, heads * 128] (bf16 or fp32) into the slots
     (int64 [rows], negative: skipped) of their caches; v_plan, v and v_cache
     None: k alone."""
-    rows, width, dt = k.shape[0], k_cache.heads * 128, k.dtype
-    ldk = _rows(k, rows, width, dt, "k")
+    dev, dt = torch.cuda.current_device(), k.dtype
+    shape = (k.shape[0], k_cache.heads * 128)
+    kp, ldk = _rows(k, dt, shape, dev, "k")
+    if k_cache.device.index != dev:
+        raise ValueError(f"a cache on {k_cache.device} in a call on cuda:{dev}")
     if v is None:
         if v_plan is not None or v_cache is not None:
             raise ValueError("v_plan, v and v_cache come together")
-        _on_device(k, slots, k_cache.codes)
-        vargs = (None, None, 0, None)
+        vh = vp = vc = None
+        ldv = 0
     else:
-        _on_device(k, v, slots, k_cache.codes, v_cache.codes)
-        vargs = (v_plan.handle, v.data_ptr(), _rows(v, rows, width, dt, "v"), C.byref(v_cache.c))
-    st = lib().hq_cache_write(k_plan.handle, k.data_ptr(), ldk, C.byref(k_cache.c), *vargs,
-                              _dtype_code(dt), rows, _slots(slots, rows), _stream_handle(stream))
+        vp, ldv = _rows(v, dt, shape, dev, "v")
+        if v_cache.device.index != dev:
+            raise ValueError(f"a cache on {v_cache.device} in a call on cuda:{dev}")
+        vh, vc = v_plan.handle, C.byref(v_cache.c)
+    st = lib().hq_cache_write(k_plan.handle, kp, ldk, C.byref(k_cache.c), vh, vp, ldv, vc,
+                              _dtype_code(dt), shape[0],
+                              _dense(slots, torch.int64, shape[:1], dev, "slots"), _stream_handle(stream))
     _check("hq_cache_write", st)
 
 
 def hq_cache_read(plan: Plan, cache: Cache, slots: torch.Tensor, out_dtype=torch.bfloat16, out=None,
                   stream=None):
     """hq_cache_read: the rows of the slots (int64, negative: zeros), [rows, heads * 128]."""
-    rows, width = slots.shape[0], cache.heads * 128
+    dev = torch.cuda.current_device()
+    shape = (slots.shape[0], cache.heads * 128)
+    if cache.device.index != dev:
+        raise ValueError(f"a cache on {cache.device} in a call on cuda:{dev}")
     if out is None:
-        out = torch.empty((rows, width), dtype=out_dtype, device=cache.device)
+        out = _empty(shape, out_dtype, dev, stream)
     dt = out.dtype
-    ld = _rows(out, rows, width, dt, "out")
-    _on_device(slots, out, cache.codes)
-    st = lib().hq_cache_read(plan.handle, C.byref(cache.c), _slots(slots, rows), rows, out.data_ptr(),
+    op, ld = _rows(out, dt, shape, dev, "out")
+    st = lib().hq_cache_read(plan.handle, C.byref(cache.c),
+                             _dense(slots, torch.int64, shape[:1], dev, "slots"), shape[0], op,
                              _dtype_code(dt), ld, _stream_handle(stream))
     _check("hq_cache_read", st)
     return out
@@ -635,61 +646,52 @@ def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.
     """hq_cache_attention: q [batch, heads_q, 128] (bf16 or fp32) attends over
     the caches' blocks block_table int32 [batch, max_blocks], seq_lens int32
     [batch] tokens each.  Returns [batch, heads_q, 128]."""
-    if q.dim() != 3 or q.shape[2] != 128 or not q.is_contiguous():
-        raise ValueError("q must be a contiguous [batch, heads_q, 128]")
-    batch, heads_q, _ = shape = q.shape
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != batch or \
-            not block_table.is_contiguous():
-        raise ValueError("block_table must be a contiguous int32 [batch, max_blocks]")
-    if seq_lens.dtype != torch.int32 or seq_lens.shape != (batch,) or not seq_lens.is_contiguous():
-        raise ValueError("seq_lens must be a contiguous int32 [batch]")
-    max_blocks = block_table.shape[1]
+    dev = torch.cuda.current_device()
+    if k.device.index != dev or v.device.index != dev:
+        raise ValueError(f"caches on {k.device} and {v.device} in a call on cuda:{dev}")
+    if q.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("q must be [batch, heads_q, 128] and block_table [batch, max_blocks]")
+    batch, heads_q, max_blocks = q.shape[0], q.shape[1], block_table.shape[1]
+    shape, qt = (batch, heads_q, 128), q.dtype
+    qp = _dense(q, qt, shape, dev, "q")
+    tp = _dense(block_table, torch.int32, (batch, max_blocks), dev, "block_table")
+    lp = _dense(seq_lens, torch.int32, (batch,), dev, "seq_lens")
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype, device=q.device)
-    elif out.shape != shape or not out.is_contiguous():
-        raise ValueError("out must be a contiguous [batch, heads_q, 128]")
+        out = _empty(shape, out_dtype, dev, stream)
+    ot = out.dtype
     if workspace is None:
         nb = hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)
-        workspace = torch.empty(max(nb, 16), dtype=torch.uint8, device=q.device)
-    elif not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
-    _on_device(q, block_table, seq_lens, out, workspace, k.codes, v.codes)
-    st = lib().hq_cache_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), q.data_ptr(),
-                                  _dtype_code(q.dtype), batch, heads_q,
-                                  128 ** -0.5 if scale is None else scale, block_table.data_ptr(),
-                                  max_blocks, seq_lens.data_ptr(), out.data_ptr(),
-                                  _dtype_code(out.dtype), workspace.data_ptr(),
-                                  workspace.nbytes, _stream_handle(stream))
+        workspace = _empty((max(nb, 16),), torch.uint8, dev, stream)
+    elif not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError(f"workspace must be contiguous on cuda:{dev}")
+    st = lib().hq_cache_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), qp,
+                                  _dtype_code(qt), batch, heads_q,
+                                  128 ** -0.5 if scale is None else scale, tp, max_blocks, lp,
+                                  _dense(out, ot, shape, dev, "out"), _dtype_code(ot),
+                                  workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
     _check("hq_cache_attention", st)
     return out
 
 
 def _rmsnorm_act_prep(fn, code, plan, x, weight, eps, residual, h, xq, sx, stream):
-    M, K = x.shape[0], plan.info.cols
-    bf16 = torch.bfloat16
-    ldx, ldr, ldh, rp, hp = _rows(x, M, K, bf16, "x"), 0, 0, None, None
-    if weight.shape != (K,) or not weight.is_contiguous():
-        raise ValueError("weight must hold one contiguous value per column")
-    if xq is None:
-        xq = torch.empty((M, K), dtype=code, device=x.device)
-    elif xq.shape != (M, K) or xq.dtype != code or not xq.is_contiguous():
-        raise ValueError(f"xq must be a contiguous {code} [{M}, {K}]")
-    if sx is None:
-        sx = torch.empty((M,), dtype=torch.float32, device=x.device)
-    elif sx.shape != (M,) or sx.dtype != torch.float32 or not sx.is_contiguous():
-        raise ValueError(f"sx must be a contiguous fp32 [{M}]")
-    _on_device(x, weight, xq, sx)
-    if residual is not None:
+    dev, bf16 = torch.cuda.current_device(), torch.bfloat16
+    shape = (x.shape[0], plan.info.cols)
+    xp, ldx = _rows(x, bf16, shape, dev, "x")
+    wt = weight.dtype
+    if residual is None:
+        rp, ldr = None, 0
+    else:
+        rp, ldr = _rows(residual, bf16, shape, dev, "residual")
         if h is None:
-            h = torch.empty((M, K), dtype=bf16, device=x.device)
-        _on_device(residual)
-        ldr, rp = _rows(residual, M, K, bf16, "residual"), residual.data_ptr()
-    if h is not None:
-        _on_device(h)
-        ldh, hp = _rows(h, M, K, bf16, "h"), h.data_ptr()
-    st = getattr(lib(), fn)(plan.handle, x.data_ptr(), ldx, rp, ldr, weight.data_ptr(),
-                            _dtype_code(weight.dtype), eps, M, hp, ldh, xq.data_ptr(), sx.data_ptr(),
-                            _stream_handle(stream))
+            h = _empty(shape, bf16, dev, stream)
+    hp, ldh = (None, 0) if h is None else _rows(h, bf16, shape, dev, "h")
+    if xq is None:
+        xq = _empty(shape, code, dev, stream)
+    if sx is None:
+        sx = _empty(shape[:1], torch.float32, dev, stream)
+    st = getattr(lib(), fn)(plan.handle, xp, ldx, rp, ldr, _dense(weight, wt, shape[1:], dev, "weight"),
+                            _dtype_code(wt), eps, shape[0], hp, ldh, _dense(xq, code, shape, dev, "xq"),
+                            _dense(sx, torch.float32, shape[:1], dev, "sx"), _stream_handle(stream))
     _check(fn, st)
     return (xq, sx) if residual is None else (xq, sx, h)
 

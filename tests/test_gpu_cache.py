@@ -312,6 +312,14 @@ def test_streams_and_graphs(hq):
     torch.cuda.current_stream().wait_stream(side)
     torch.cuda.synchronize()
     assert torch.equal(out, eager)
+    # the stream given to the calls, which take their workspace and outputs from it
+    side.wait_stream(torch.cuda.current_stream())
+    hq.hq_cache_write(kp, k, kc, vp, v, vc, slots, stream=side)
+    got = hq.hq_cache_attention(kp, kc, vp, vc, q, table, ln, scale=scale, stream=side)
+    back = hq.hq_cache_read(kp, kc, slots, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, eager) and torch.equal(back, hq.hq_cache_read(kp, kc, slots))
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         step()
