@@ -412,7 +412,7 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
 // ---- a wave's tokens
 // A wave's tokens come through LDS, loaded there straight from memory (no register
 // waits for them) in a ring of two steps of 32 tokens, each two halves of 16: the key
-// codes, the value codes, and the 64 bytes of scales of each.  A row's 16-byte chunks are
+// codes, the value codes, and the 64 bytes of scales of each (256 with their copies).  A row's 16-byte chunks are
 // permuted by its index, which the loads' source addresses do, so that the reads
 // below meet no bank twice.
 template <int FMT>
@@ -492,10 +492,10 @@ struct CacheWalk {
         enter<FMT>(A, lane);
       }
       // a half behind the end loads its block's first tokens, one of a block outside the
-      // cache nothing, so that a step is always the same loads; nothing reads them
-      const int32_t some = min(max(end - t - 16 * h, 0), 16);
-      live[h] = bad ? 0 : some;
-      const uint32_t at = some ? off : 0;
+      // cache nothing (its buffers are empty), so that a step is always the same loads;
+      // nothing reads them
+      live[h] = bad ? 0 : min(max(end - t - 16 * h, 0), 16);
+      const uint32_t at = live[h] ? off : 0;
       off += 16;
       uint8_t* to = step + h * R::HALF;
 #pragma unroll
@@ -504,13 +504,12 @@ struct CacheWalk {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(k, (lds_void*)(to + i * 1024), 16, from, rows, 0, 0);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(v, (lds_void*)(to + R::V + i * 1024), 16, from, rows, 0, 0);
       }
-      // lanes 16 and up load what nobody reads (the next tokens' scales, or nothing behind the block)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_void*)(to + R::SCALES), 4, lane * 4, at * 4, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_void*)(to + R::SCALES + 256), 4, lane * 4, at * 4, 0, 0);
+      const uint32_t token = (lane & 15) * 4;  // four times over
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_void*)(to + R::SCALES), 4, token, at * 4, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_void*)(to + R::SCALES + 256), 4, token, at * 4, 0, 0);
     }
   }
 };
-
 
 // A step's codes and scales out of LDS.
 template <int FMT>
