@@ -548,9 +548,10 @@ hq_status hq_cache_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan_t v_pl
  *   xq, sx    as hq_act_prep: device int8 M x cols (contiguous, 8-byte aligned),
  *             fp32 [M]
  * x, residual, weight and h are 16-byte aligned, their strides multiples of 8.  A row
- * with an infinity or a NaN, or with a sum of squares past fp32, gets s_x = NaN; a row
- * of zeros (max|y rms(h)| below 2^-100) zeros (E4M3: of either sign) and s_x = 0.  Host
- * errors: HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (cols above 16384), HQ_ERR_HIP.
+ * with an infinity or a NaN in h, in h * weight or in their transform, or with a sum of
+ * squares past fp32, gets s_x = NaN; a row of zeros (max|y rms(h)| below 2^-100) zeros
+ * (E4M3: of either sign) and s_x = 0.  Host errors: HQ_ERR_INVALID_ARG,
+ * HQ_ERR_UNSUPPORTED (cols above 16384), HQ_ERR_HIP.
  * hq_rmsnorm_act_prep_fp8 -- the same with x_q and s_x of hq_act_prep_fp8. */
 hq_status hq_rmsnorm_act_prep(hq_plan_t plan, const void* x, int64_t ldx, const void* residual,
                               int64_t ldr, const void* weight, int32_t wt, float eps, int64_t M,

@@ -111,18 +111,18 @@ __global__ __launch_bounds__(64 * W) void hq_norm_prep_kernel(hq_norm_args A) {
 #pragma unroll
   for (int i = 0; i < NIT; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) amax = __builtin_fmaxf(amax, __builtin_fabsf(v[i][e]));
-  amax = __builtin_fmaxf(amax, dpp_xor<1>(amax));
+    for (int e = 0; e < 8; ++e) amax = __builtin_elementwise_maximum(amax, __builtin_fabsf(v[i][e]));
+  amax = __builtin_elementwise_maximum(amax, dpp_xor<1>(amax));
   sum += dpp_xor<1>(sum);
-  amax = __builtin_fmaxf(amax, dpp_xor<2>(amax));
+  amax = __builtin_elementwise_maximum(amax, dpp_xor<2>(amax));
   sum += dpp_xor<2>(sum);
-  amax = __builtin_fmaxf(amax, swz_xor4(amax));
+  amax = __builtin_elementwise_maximum(amax, swz_xor4(amax));
   sum += swz_xor4(sum);
-  amax = __builtin_fmaxf(amax, dpp_xor<8>(amax));
+  amax = __builtin_elementwise_maximum(amax, dpp_xor<8>(amax));
   sum += dpp_xor<8>(sum);
-  amax = __builtin_fmaxf(amax, swz_xor16(amax));
+  amax = __builtin_elementwise_maximum(amax, swz_xor16(amax));
   sum += swz_xor16(sum);
-  amax = __builtin_fmaxf(amax, lane_xor32(amax));
+  amax = __builtin_elementwise_maximum(amax, lane_xor32(amax));
   sum += lane_xor32(sum);
   if (lane == 0) {
     s_max[wave] = amax;
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(64 * W) void hq_norm_prep_kernel(hq_norm_args A) {
   sum = s_sum[0];
 #pragma unroll
   for (int x = 1; x < W; ++x) {
-    amax = __builtin_fmaxf(amax, s_max[x]);
+    amax = __builtin_elementwise_maximum(amax, s_max[x]);
     sum += s_sum[x];
   }
   const float top = FP8 ? 448.0f : 127.0f;  // E4M3's largest magnitude, or int8's
@@ -156,8 +156,10 @@ __global__ __launch_bounds__(64 * W) void hq_norm_prep_kernel(hq_norm_args A) {
   }
   if (tid == 0) {
     const float rms = __builtin_sqrtf(sum / (float)A.K + A.eps);
-    // a NaN or an infinity anywhere in the row makes its scale NaN
-    A.sx[row] = rms <= 3.4028234663852886e38f ? amax < 0x1p-100f ? 0.0f : amax / top / rms : __builtin_nanf("");
+    // a NaN or an infinity anywhere in h, h * weight or the transform makes the row's scale
+    // NaN (the maximum keeps a NaN)
+    constexpr float most = 3.4028234663852886e38f;
+    A.sx[row] = !(rms <= most && amax <= most) ? __builtin_nanf("") : amax < 0x1p-100f ? 0.0f : amax / top / rms;
   }
 }
 

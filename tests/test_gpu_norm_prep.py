@@ -117,6 +117,24 @@ def test_zero_rows_and_rows_that_are_not_finite(hq, fp8):
     check(x[3:], w, 5, 128, 1e-5, xq[3:], sx[3:], fp8)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("tile", [128, 2048])
+def test_weights_that_are_not_finite_reach_the_scale(hq, tile, fp8):
+    plan = hq.hq_plan(tile=tile, cols=4096, bps=4.0, rht_seed=5)
+    x, _, w = make(5, 4096, 12, torch.float32)
+    ref = prep(hq, fp8)(plan, x.cuda(), w.cuda())
+    assert torch.isfinite(ref[1]).all()
+    for value in (float("nan"), float("inf"), float("-inf")):
+        bad = w.clone()
+        bad[4000] = value
+        assert prep(hq, fp8)(plan, x.cuda(), bad.cuda())[1].isnan().all()
+    big, bad = x.clone(), w.clone()
+    big[:, 3], big[2, 3], bad[3] = 0, 1e18, 1e30  # one product past fp32, the squares' sum not
+    xq, sx = prep(hq, fp8)(plan, big.cuda(), bad.cuda())
+    assert sx[2].isnan() and torch.isfinite(sx[[0, 1, 3, 4]]).all()
+    check(big[[0, 1, 3, 4]], bad, 5, tile, 1e-5, xq[[0, 1, 3, 4]], sx[[0, 1, 3, 4]], fp8)
+
+
 def test_graph_replays(hq):
     plan = hq.hq_plan(cols=1024, bps=4.0)
     x, r, w = (t.cuda() for t in make(5, 1024, 9))
