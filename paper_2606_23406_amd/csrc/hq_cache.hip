@@ -328,7 +328,8 @@ __device__ __forceinline__ float groups_sum(float x) {
 // The tokens of a call are cut into chunks of about one length, as many workgroups
 // as the chip holds at once over all sequences and KV heads, so that a batch of uneven
 // lengths keeps it as busy as an even one.  Item j is chunk j - first of sequence b.
-// Every wave finds its item by itself, 64 lengths a step, one per lane.
+// Up to 64 sequences every wave finds its item by itself, one length per lane; more are
+// planned by a launch before (hq_cache_plan_kernel), whose table the waves search.
 constexpr int32_t kStep = 32 * HQ_CACHE_WAVES;
 struct CacheItem {
   int32_t b;       // -1: behind the last item
@@ -345,39 +346,44 @@ __device__ __forceinline__ int32_t cache_len(const hq_cache_attn_args& A, int64_
   return len < 0 ? 0 : (int32_t)cap;
 }
 
+__device__ __forceinline__ uint32_t cache_parts(int32_t len, uint32_t chunk) {
+  return len == 0 ? 1u : ((uint32_t)len + chunk - 1) / chunk;
+}
+
 // The longest a chunk may be: whole steps of all waves, HQ_CACHE_LEAST tokens at
 // least; one of 2^30 holds any sequence.  An even share of the workgroups aimed at
 // would be right if every sequence were a multiple of it.  A sequence's last chunk is
 // not, and what that adds opens a second round of workgroups, so the share grows by
 // eighths until the chunks fit but for a few, to its double at most.  (24 sequences of
 // up to 6001 tokens, 8 KV heads in E4M3: 560 chunks of the even share take 51.7 us, 528 of
-// its 9 / 8 take 41.4.)  `mine`: the lane's own length, of the first 64 sequences.
-__device__ __forceinline__ int32_t cache_chunk(const hq_cache_attn_args& A, int lane, int32_t mine, bool tell) {
-  int64_t total = mine;
-  for (int64_t i = lane + 64; i < A.batch; i += 64) total += cache_len(A, i, tell);
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
+// its 9 / 8 take 41.4.)  More sequences than that take several rounds in any case.
+// `total`: all tokens; `mine`: a lane's or thread's own sequence's, -1 without one; `sum`
+// adds a number over all of these.
+template <typename SUM>
+__device__ __forceinline__ uint32_t cache_chunk(const hq_cache_attn_args& A, int64_t total, int32_t mine, SUM sum) {
   const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
   const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.heads_kv;
-  int32_t chunk = HQ_CACHE_LEAST;
+  uint32_t chunk = HQ_CACHE_LEAST;
   for (int e = 8; e <= 16; ++e) {
     const int64_t c = min(((even * e >> 3) + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
-    chunk = max(chunk, (int32_t)readfirst((uint32_t)c));
+    chunk = max(chunk, readfirst((uint32_t)c));
+    if (A.batch > few) break;
     // about: a length a hair over a multiple may count as the multiple
     const float per = __builtin_amdgcn_rcpf((float)chunk) * 0.999999f;
-    uint32_t n = lane < A.batch ? max(1u, (uint32_t)__builtin_ceilf((float)mine * per)) : 0u;
-    for (int64_t i = lane + 64; i < A.batch; i += 64)
-      n += max(1u, (uint32_t)__builtin_ceilf((float)cache_len(A, i, false) * per));
-    const uint32_t all = wave_total(n);
-    if (all <= few || A.batch > few) break;  // more sequences than that: several rounds in any case
+    if (sum(mine < 0 ? 0u : max(1u, (uint32_t)__builtin_ceilf((float)mine * per))) <= few) break;
   }
   return chunk;
 }
 
+// Whole steps of all waves, about as many in each of a sequence's n chunks.
+__device__ __forceinline__ int32_t even_chunk(int32_t len, int32_t n) {
+  return (len + n * kStep - 1) / (n * kStep) * kStep;
+}
+
 __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int32_t j, int lane, bool tell) {
   CacheItem it;
+  it.b = -1;
   if (!A.join) {  // one chunk each
-    it.b = -1;
     if (j >= A.batch) return it;
     it.b = it.first = j;
     it.n = 1;
@@ -385,28 +391,84 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.chunk = HQ_CACHE_WHOLE;
     return it;
   }
-  int32_t len = lane < A.batch ? cache_len(A, lane, tell) : 0;
-  const uint32_t chunk = (uint32_t)cache_chunk(A, lane, len, tell);
-  it.b = -1;
-  int32_t base = 0;
-  for (int64_t i0 = 0; i0 < A.batch; i0 += 64) {
-    const bool in = i0 + lane < A.batch;
-    if (i0) len = in ? cache_len(A, i0 + lane, false) : 0;
-    const uint32_t n = !in ? 0u : len == 0 ? 1u : ((uint32_t)len + chunk - 1) / chunk;
-    const int32_t incl = (int32_t)wave_scan_incl(n), all = __builtin_amdgcn_readlane(incl, 63);
-    if (j < base + all) {
-      const int at = __popcll(__ballot(base + incl <= j));
-      it.b = (int32_t)i0 + at;
-      it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
-      it.first = base + __builtin_amdgcn_readlane(incl, at) - it.n;
-      it.len = __builtin_amdgcn_readlane(len, at);
-      // even chunks: whole steps of all waves
-      it.chunk = (it.len + it.n * kStep - 1) / (it.n * kStep) * kStep;
-      break;
+  if (A.batch > 64) {
+    // the last sequence whose first item is j at most, 64 places a step
+    int64_t lo = 0;
+    for (int64_t span = A.batch; span > 1;) {
+      const int64_t stride = (span + 63) >> 6, at = lo + lane * stride;
+      const bool below = lane * stride < span && A.parts[at].first <= j;
+      const int64_t last = __popcll(__ballot(below)) - 1;  // the first place is always below
+      lo += last * stride;
+      span = min(stride, span - last * stride);
     }
-    base += all;
+    const hq_cache_of of = A.parts[lo];
+    it.first = (int32_t)readfirst((uint32_t)of.first);
+    it.n = (int32_t)readfirst((uint32_t)of.n);
+    if (j >= it.first + it.n) return it;
+    it.b = (int32_t)readfirst((uint32_t)lo);
+    it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, false));
+  } else {
+    const bool in = lane < A.batch;
+    const int32_t len = in ? cache_len(A, lane, tell) : -1;
+    int64_t total = max(len, 0);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
+    const uint32_t chunk = cache_chunk(A, total, len, [](uint32_t n) { return wave_total(n); });
+    const uint32_t n = in ? cache_parts(len, chunk) : 0u;
+    const int32_t incl = (int32_t)wave_scan_incl(n);
+    if (j >= __builtin_amdgcn_readlane(incl, 63)) return it;
+    const int at = __popcll(__ballot(incl <= j));
+    it.b = at;
+    it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
+    it.first = __builtin_amdgcn_readlane(incl, at) - it.n;
+    it.len = __builtin_amdgcn_readlane(len, at);
   }
+  it.chunk = even_chunk(it.len, it.n);
   return it;
+}
+
+// The items of more than 64 sequences, in one workgroup.  (1024 sequences of about 900
+// tokens, 8 KV heads in int8, take 335 us; 474 with every wave going through all lengths.)
+constexpr int kPlanThreads = 1024;
+__global__ __launch_bounds__(kPlanThreads) void hq_cache_plan_kernel(hq_cache_attn_args A) {
+  __shared__ uint64_t s_sum[kPlanThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // over the workgroup; every thread gets it
+  auto sum = [&](uint64_t x) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
+    __syncthreads();  // the last sum has been read
+    if (lane == 0) s_sum[wave] = x;
+    __syncthreads();
+    x = 0;
+    for (int i = 0; i < kPlanThreads / 64; ++i) x += s_sum[i];
+    return x;
+  };
+  int64_t total = 0;
+  for (int64_t i = tid; i < A.batch; i += kPlanThreads) total += cache_len(A, i, true);
+  total = (int64_t)sum((uint64_t)total);
+  // it counts chunks for few sequences only: at most one per thread
+  static_assert(HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32 <= kPlanThreads, "");
+  const uint32_t chunk = cache_chunk(A, total, tid < A.batch ? cache_len(A, tid, false) : -1,
+                                     [&](uint32_t n) { return (int64_t)sum(n); });
+  uint64_t base = 0;  // items, and from bit 32 on split sequences, before these
+  for (int64_t i0 = 0; i0 < A.batch; i0 += kPlanThreads) {
+    const int64_t i = i0 + tid;
+    const uint32_t n = i < A.batch ? cache_parts(cache_len(A, i, false), chunk) : 0u, split = n > 1;
+    uint32_t items = n, splits = split;
+    wave_scan_incl2(items, splits);
+    __syncthreads();  // the last sums have been read
+    if (lane == 63) s_sum[wave] = (uint64_t)splits << 32 | items;
+    __syncthreads();
+    uint64_t at = base + ((uint64_t)(splits - split) << 32 | (items - n));
+    for (int x = 0; x < kPlanThreads / 64; ++x) {
+      if (x < wave) at += s_sum[x];
+      base += s_sum[x];
+    }
+    if (i < A.batch) A.parts[i] = {(int32_t)(uint32_t)at, (int32_t)n};
+    if (split) A.split[at >> 32] = (int32_t)i;
+  }
+  if (tid == 0) A.split[A.joins] = (int32_t)(base >> 32);
 }
 
 // ---- a wave's tokens
@@ -710,7 +772,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   const CacheItem it = cache_item(A, j, lane, blockIdx.x == 0 && wave == 0);
   if (it.b < 0) return;
   // what the join goes by
-  if (A.join && j == it.first && head == 0 && tid == 0) A.parts[it.b] = {it.first, it.n};
+  if (A.join && A.batch <= 64 && j == it.first && head == 0 && tid == 0) A.parts[it.b] = {it.first, it.n};
   const int32_t G = A.group, c0 = n * 8;
   const int64_t pair0 = (int64_t)it.b * A.heads_q + (int64_t)head * G;
   if (it.len == 0) {
@@ -860,14 +922,19 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
 }
 
 // Joins a query head's chunks under one maximum, in order, and moves the result
-// back: one workgroup per query head, 16 lanes per chunk.
+// back: one workgroup per query head, 16 lanes per chunk.  Of a planned call only the split
+// sequences have one (4096 sequences of about 100 tokens, 32 query heads: 416 us so, 478
+// with a workgroup for each).
 __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A) {
   __shared__ float s_red[16];
   __shared__ float4 s_acc[16][32];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4, c0 = n * 8;
-  const int64_t pair = blockIdx.x;
-  const int64_t b = pair / A.heads_q;
-  const int32_t hq = (int32_t)(pair - b * A.heads_q), head = hq / A.group;
+  int64_t b = blockIdx.x / (uint32_t)A.heads_q;
+  const int32_t hq = (int32_t)(blockIdx.x - (uint32_t)b * (uint32_t)A.heads_q), head = hq / A.group;
+  if (A.batch > 64) {
+    if (b >= A.split[A.joins]) return;
+    b = A.split[b];
+  }
   const hq_cache_of has = A.parts[b];
   const int32_t parts = has.n;
   if (parts == 1) return;  // already whole
@@ -927,7 +994,7 @@ __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A
     L += s_red[k];
   }
   cache_finish(A, L, v, head, lane);
-  store8(A.out, pair * HQ_TILE + c0, A.out_bf16, v);
+  store8(A.out, (b * A.heads_q + hq) * HQ_TILE + c0, A.out_bf16, v);
 }
 
 }  // namespace
@@ -969,12 +1036,13 @@ int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* str
   const hipStream_t st = (hipStream_t)stream;
   const dim3 grid((uint32_t)(a.items * a.heads_kv)), wg(256);
   int e = 0;
+  if (a.join && a.batch > 64) hipLaunchKernelGGL(hq_cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
   switch (format) {
     case HQ_INT8: e = launch_attn<kInt8>(a, grid, st); break;
     case HQ_E4M3: e = launch_attn<kE4M3>(a, grid, st); break;
     default: e = launch_attn<kMx>(a, grid, st);
   }
   if (e) return e;
-  if (a.join) hipLaunchKernelGGL(hq_cache_join_kernel, dim3((uint32_t)(a.batch * a.heads_q)), wg, 0, st, a);
+  if (a.join) hipLaunchKernelGGL(hq_cache_join_kernel, dim3((uint32_t)(a.joins * a.heads_q)), wg, 0, st, a);
   return (int)hipGetLastError();
 }

@@ -154,7 +154,8 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
   const int64_t max_tokens = (int64_t)max_blocks * k->block_tokens;
   if (max_tokens <= HQ_CACHE_WHOLE) return 0;
   const int64_t n = hq_cache_items(batch, k->heads, max_tokens) * heads_q;
-  return (size_t)n * (HQ_TILE + 2) * sizeof(float) + (size_t)batch * sizeof(hq_cache_of);
+  return (size_t)n * (HQ_TILE + 2) * sizeof(float) + (size_t)batch * sizeof(hq_cache_of) +
+         (size_t)(hq_cache_joins(batch, k->heads) + 1) * sizeof(int32_t);
 }
 
 hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, const hq_cache* v, const void* q,
@@ -201,6 +202,7 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
     a.part_m = a.part_acc + n * HQ_TILE;
     a.part_l = a.part_m + n;
     a.parts = (hq_cache_of*)(a.part_l + n);
+    a.split = (int32_t*)(a.parts + batch);
   }
   a.stats = k->stats;
   a.batch = batch;
@@ -211,6 +213,7 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
   a.max_blocks = max_blocks;
   a.block_tokens = k->block_tokens;
   a.items = items;
+  a.joins = hq_cache_joins(batch, k->heads);
   a.join = join;
   a.q_bf16 = qt == HQ_BF16;
   a.out_bf16 = ot == HQ_BF16;

@@ -301,9 +301,11 @@ struct hq_cache_attn_args {
   float* part_m;
   float* part_l;
   hq_cache_of* parts;       // per sequence
+  int32_t* split;           // of a planned call: the split sequences; [joins] their number
   hq_stats* stats;
   int64_t batch;
   int64_t items;            // bound on the chunks of all sequences
+  int64_t joins;            // bound on the sequences of several chunks
   int32_t heads_q, heads_kv, group;
   int32_t max_blocks, blocks, block_tokens;
   int32_t join;             // a sequence may have several chunks
@@ -333,6 +335,11 @@ static inline int64_t hq_cache_items(int64_t batch, int64_t heads_kv, int64_t ma
   const int64_t most = (max_tokens + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST;
   const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
   return batch * most < batch + even ? batch * most : batch + even;
+}
+// Bound on the sequences that have several: each takes one of what rounding does not add.
+static inline int64_t hq_cache_joins(int64_t batch, int64_t heads_kv) {
+  const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
+  return batch < even ? batch : even;
 }
 
 // RMS norm fused with the 8-bit activation prep.

@@ -50,8 +50,9 @@ def test_chunks_fit_the_workspace(hq, tmp_path):
     than the bound that the grid and the workspace go by, whatever the lengths."""
     src = tmp_path / "rule.cpp"
     src.write_text('#include "hq_internal.h"\n#include <cstdio>\n#include <cstdlib>\n'
-                   'int main(int, char** a) {\n  printf("%d %d %ld\\n", HQ_CACHE_WG_TARGET, HQ_CACHE_LEAST,\n'
-                   '         (long)hq_cache_items(atol(a[1]), atol(a[2]), atol(a[3])));\n}\n')
+                   'int main(int, char** a) {\n  printf("%d %d %ld %ld\\n", HQ_CACHE_WG_TARGET, HQ_CACHE_LEAST,\n'
+                   '         (long)hq_cache_items(atol(a[1]), atol(a[2]), atol(a[3])),\n'
+                   '         (long)hq_cache_joins(atol(a[1]), atol(a[2])));\n}\n')
     exe = tmp_path / "rule"
     subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2606_23406_amd", "csrc"), "-o", str(exe),
                     str(src)], check=True)
@@ -59,8 +60,8 @@ def test_chunks_fit_the_workspace(hq, tmp_path):
     rng = np.random.default_rng(0)
     for batch, heads, blocks in [(1, 1, 1), (8, 8, 63), (8, 8, 64), (8, 8, 65), (1, 8, 8192), (3, 3, 400), (64, 8, 33), (65, 2, 700), (300, 1, 1000),
                                  (2000, 16, 64), (1, 512, 100), (7, 600, 90)]:
-        target, least, items = map(int, subprocess.run([str(exe), str(batch), str(heads), str(16 * blocks)],
-                                                       capture_output=True, text=True, check=True).stdout.split())
+        target, least, items, joins = map(int, subprocess.run([str(exe), str(batch), str(heads), str(16 * blocks)],
+                                                              capture_output=True, text=True, check=True).stdout.split())
         if 16 * blocks <= 1024:  # no sequence is split: workgroup j takes sequence j
             assert items == batch
             assert L.hq_cache_attention_workspace_bytes(C.byref(hq.CacheStruct(None, None, 1, 16, heads, 3, 0, None)),
@@ -73,10 +74,11 @@ def test_chunks_fit_the_workspace(hq, tmp_path):
                 chunk = max(least, ((even * eighths >> 3) + 127) // 128 * 128)
                 n = np.where(lens == 0, 1, -(-lens // chunk))
                 assert batch <= n.sum() <= items, (batch, heads, blocks)
+                assert (n > 1).sum() <= joins, (batch, heads, blocks)
                 own = -(-lens // (n * 128)) * 128  # the even chunk of each
                 assert (own * n >= lens).all() and (own * (n - 1) <= lens).all()
         c = hq.CacheStruct(None, None, 1, 16, heads, 3, 0, None)
-        assert items * heads * 2 * 130 * 4 + batch * 8 == L.hq_cache_attention_workspace_bytes(C.byref(c), batch, 2 * heads, blocks)
+        assert items * heads * 2 * 130 * 4 + batch * 8 + (joins + 1) * 4 == L.hq_cache_attention_workspace_bytes(C.byref(c), batch, 2 * heads, blocks)
 
 
 def test_the_oracle_transforms_back():

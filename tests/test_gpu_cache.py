@@ -187,6 +187,50 @@ def test_attention_splits_and_joins(hq, fmt, lens):
     check_attention(hq, case, 2, 4, 64)
 
 
+def many_case(hq, fmt, B, heads, group, bt, seed):
+    """B sequences over a small cache (blocks repeat), most of them short or empty, a few long."""
+    kp, vp = R.plans(hq, heads)
+    kc, vc = (R.random_cache(hq, p, fmt, 40, heads, bt, seed + i) for i, p in enumerate((kp, vp)))
+    g = torch.Generator().manual_seed(seed + 2)
+    lens = torch.randint(-40, 90, (B,), generator=g).clamp(min=0).to(torch.int32)
+    lens[torch.randint(0, B, (5,), generator=g)] = torch.tensor([1023, 1024, 1025, 1536, 2000], dtype=torch.int32)
+    table = torch.randint(0, 40, (B, -(-2000 // bt)), generator=g).to(torch.int32)
+    q = torch.randn((B, heads * group, N), generator=g)
+    return kp, vp, kc, vc, table, q, lens, N ** -0.5
+
+
+@pytest.mark.parametrize("B,heads,group", [(64, 1, 2), (65, 1, 2), (129, 3, 5), (528, 1, 1), (529, 1, 1), (1024, 2, 1),
+                                           (1025, 1, 4), (4097, 1, 1)])
+def test_attention_many_sequences(hq, B, heads, group):
+    print(f"[cache] attention many {B} x {heads} x {group}", flush=True)
+    check_attention(hq, many_case(hq, "int8", B, heads, group, 48, B), heads, group, 48)
+
+
+def test_attention_many_sequences_replayed_and_out_of_range(hq):
+    case = many_case(hq, "e4m3", 200, 2, 2, 64, 7)
+    kp, vp, kc, vc, table, q, lens, scale = case
+    cap = table.shape[1] * 64
+    q, table, ln, out = q.cuda(), table.cuda(), lens.cuda(), torch.empty_like(q, device="cuda")
+    ws = torch.empty(hq.hq_cache_attention_workspace_bytes(kc, 200, 4, table.shape[1]), dtype=torch.uint8, device="cuda")
+    call = lambda o: hq.hq_cache_attention(kp, kc, vp, vc, q, table, ln, out=o, workspace=ws)
+    call(out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for i in range(4):
+        ln.copy_(lens.roll(61 * i))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, call(torch.empty_like(out)))
+    assert kc.read_stats()["status"] == 0
+    ln[3], ln[150], ln[199] = -5, cap + 1, 2 ** 31 - 1
+    graph.replay()
+    assert kc.read_stats()["status"] == INVALID_ARG
+    ln[3], ln[150], ln[199] = 0, cap, cap
+    assert torch.equal(out, call(torch.empty_like(out)))
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.05, 1.0])
 def test_attention_scales(hq, scale):
     case = attention_case(hq, "int8", [200, 33], 4, 2, 16, seed=5, scale=scale)
