@@ -619,12 +619,18 @@ struct CacheState {
 };
 
 // One step: 32 tokens' scores, the running maximum and sum, their values' sum.
-// PACK: column l % 16 is term l % 4 of head (l / 4) % 4.  Otherwise it is a head, and the
-// terms are three products.
-template <int FMT, bool PACK>
+// A head has C of the 16 columns, for the three terms of its query and weights: C = 4 (up
+// to four heads) a column per term and one of zeros, in one product; C = 2 (up to eight)
+// the first two in one product and the third beside zeros in another; C = 1 three products.
+// (16 x 8192 tokens of MXFP4, 8 query heads per KV head: 37.8 us with two products, 39.9
+// with three.)
+template <int C>
+constexpr int products() { return C == 4 ? 1 : C == 2 ? 2 : 3; }
+
+template <int FMT, int C>
 __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&live)[2],
-                                           const uint32_t (&q)[PACK ? 1 : 3][4][4], int lane, CacheState& z) {
-  constexpr int T = PACK ? 1 : 3;
+                                           const uint32_t (&q)[products<C>()][4][4], int lane, CacheState& z) {
+  constexpr int T = products<C>();
   const int n = lane & 15, g = lane >> 4;
   if (live[0] + live[1] < 32) {
     // stale or absent tokens: their value codes count as zeros (their weight is
@@ -644,9 +650,10 @@ __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const float f = FMT == kMx ? __uint_as_float(cur.kx[h] << 23) : 1.0f;
-    v4_t c[T];
+    constexpr int S = C == 1 ? T : 1;  // sums: columns of a head share one
+    v4_t c[S];
 #pragma unroll
-    for (int i = 0; i < T; ++i) c[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < S; ++i) c[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       uint32_t a[4];
@@ -657,15 +664,14 @@ __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&
         pairs_of<FMT>(cur.k[h][2 * s + 1], f, a + 2);
       }
 #pragma unroll
-      for (int i = 0; i < T; ++i) c[i] = mfma_bf16(a, q[i][s], c[i]);
+      for (int i = T - 1; i >= 0; --i) c[i % S] = mfma_bf16(a, q[i][s], c[i % S]);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      float x = PACK ? c[0][r] : c[0][r] + (c[T / 2][r] + c[T - 1][r]);
-      if constexpr (PACK) {  // the terms' sum, in each lane of the head's four
-        x += dpp_xor<1>(x);
-        x += dpp_xor<2>(x);
-      }
+      float x = C == 1 ? c[0][r] + (c[S / 2][r] + c[S - 1][r]) : c[0][r];
+      // the terms' sum, in each of the head's lanes
+      if constexpr (C >= 2) x += dpp_xor<1>(x);
+      if constexpr (C == 4) x += dpp_xor<2>(x);
       p[h][r] = FMT == kMx ? x : x * cur.ks[h][r];
     }
   }
@@ -691,7 +697,7 @@ __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&
   }
   const float ref = z.m == -__builtin_inff() ? 0.0f : z.m;  // nothing seen yet
   uint32_t pt[T][4];  // the weights' terms: k index 4 h + r
-  const uint32_t cut1 = PACK && (n & 3) < 1 ? 0u : 0xFFFF0000u, cut2 = PACK && (n & 3) < 2 ? 0u : 0xFFFF0000u;
+  const uint32_t cut1 = (n & 3) < 1 ? 0u : 0xFFFF0000u, cut2 = (n & 3) < 2 ? 0u : 0xFFFF0000u;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t tt[4][T];
@@ -700,9 +706,14 @@ __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&
       const float e = __builtin_amdgcn_exp2f(p[h][r] - ref);
       z.l += e;
       const float x = FMT == kMx ? e : e * cur.vs[h][r];
-      if constexpr (PACK) {  // the column's own term
+      if constexpr (C == 4) {  // the column's own term
         const float y = x - __uint_as_float(__float_as_uint(x) & cut1);
         tt[r][0] = __float_as_uint(y - __uint_as_float(__float_as_uint(y) & cut2));
+      } else if constexpr (C == 2) {
+        uint32_t t[3];
+        three_terms(x, t);
+        tt[r][0] = n & 1 ? t[1] : t[0];
+        tt[r][1] = n & 1 ? 0u : t[2];
       } else {
         three_terms(x, tt[r]);
       }
@@ -753,11 +764,11 @@ __device__ __forceinline__ void cache_finish(const hq_cache_attn_args& A, float 
   flip8(v, sign_words(A.v_dsign16, head * HQ_TILE + (lane & 15) * 8));
 }
 
-template <int FMT, bool PACK>
+template <int FMT, int C>
 __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_attn_kernel(
     hq_cache_attn_args A) {
   using R = CacheRing<FMT>;
-  constexpr int HEADS = PACK ? 4 : 16, T = PACK ? 1 : 3;
+  constexpr int HEADS = 16 / C, T = products<C>();
   extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];  // a wave's ring after the other
   __shared__ float s_m[HQ_CACHE_WAVES][HEADS], s_l[HQ_CACHE_WAVES][HEADS];
   // term i of the query lies in the second step of wave i's ring until that is first
@@ -817,9 +828,9 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
       o.y = high_pair(t[2][i], t[3][i]);
       o.z = high_pair(t[4][i], t[5][i]);
       o.w = high_pair(t[6][i], t[7][i]);
-      *(uint4*)((PACK ? q_row(0, grp * 4 + i) : q_row(i, grp)) + c0) = o;
+      *(uint4*)(q_row(C == 4 ? 0 : C == 2 ? i >> 1 : i, C * grp + (C == 4 ? i : C == 2 ? i & 1 : 0)) + c0) = o;
     }
-    if (PACK) *(uint4*)(q_row(0, grp * 4 + 3) + c0) = make_uint4(0u, 0u, 0u, 0u);
+    if (C > 1) *(uint4*)(q_row(C == 4 ? 0 : 1, C * grp + C - 1) + c0) = make_uint4(0u, 0u, 0u, 0u);
   }
   __syncthreads();
   // step s of the contraction takes dims 32 (l / 16) + 8 s + j in lane l (the codes
@@ -857,43 +868,30 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
       w.fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next);
     }
     slot ^= 1;
-    cache_step<FMT, PACK>(cur, here, q, lane, z);
+    cache_step<FMT, C>(cur, here, q, lane, z);
   }
   z.l = groups_sum(z.l);
   // ---- the waves' sums under one maximum, one head per 16 lanes
-  if constexpr (PACK) {
-    // the terms' sums: in the fourth lane of a head the weights' columns were a term over again
-    const float keep = (n & 3) == 3 ? 0.0f : 1.0f;
+  // the head's columns together (with four, the last one's weights were a term over again),
+  // its rows written by each of its lanes in turn
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+  for (int r = 0; r < 4; ++r) {
+    float x[8];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = keep == 0.0f ? 0.0f : z.acc[i][r];
-        x += dpp_xor<1>(x);
-        z.acc[i][r] = x + dpp_xor<2>(x);
-      }
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if ((n & 3) == r) {
-        float* o = o_row(wave, n >> 2) + (4 * g + r) * 8;
-        *(float4*)o = make_float4(z.acc[0][r], z.acc[1][r], z.acc[2][r], z.acc[3][r]);
-        *(float4*)(o + 4) = make_float4(z.acc[4][r], z.acc[5][r], z.acc[6][r], z.acc[7][r]);
-      }
-    if (g == 0 && (n & 3) == 0) {
-      s_m[wave][n >> 2] = z.m;
-      s_l[wave][n >> 2] = z.l;
+    for (int i = 0; i < 8; ++i) {
+      x[i] = C == 4 && (n & 3) == 3 ? 0.0f : z.acc[i][r];
+      if constexpr (C >= 2) x[i] += dpp_xor<1>(x[i]);
+      if constexpr (C == 4) x[i] += dpp_xor<2>(x[i]);
     }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float* o = o_row(wave, n) + (4 * g + r) * 8;
-      *(float4*)o = make_float4(z.acc[0][r], z.acc[1][r], z.acc[2][r], z.acc[3][r]);
-      *(float4*)(o + 4) = make_float4(z.acc[4][r], z.acc[5][r], z.acc[6][r], z.acc[7][r]);
+    if (n % C == r % C) {
+      float* o = o_row(wave, n / C) + (4 * g + r) * 8;
+      *(float4*)o = make_float4(x[0], x[1], x[2], x[3]);
+      *(float4*)(o + 4) = make_float4(x[4], x[5], x[6], x[7]);
     }
-    if (g == 0) {
-      s_m[wave][n] = z.m;
-      s_l[wave][n] = z.l;
-    }
+  }
+  if (g == 0 && n % C == 0) {
+    s_m[wave][n / C] = z.m;
+    s_l[wave][n / C] = z.l;
   }
   __syncthreads();
   if (grp >= G) return;
@@ -1018,18 +1016,20 @@ int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream) {
   return (int)hipGetLastError();
 }
 
-template <int FMT, bool PACK>
+template <int FMT, int C>
 static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
   static hq_lds_granted granted;
   constexpr size_t lds = (size_t)HQ_CACHE_WAVES * CacheRing<FMT>::WAVE;
-  if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, PACK>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, PACK>), grid, dim3(64 * HQ_CACHE_WAVES), lds, st, a);
+  if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, C>, lds, granted)) return e;
+  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, C>), grid, dim3(64 * HQ_CACHE_WAVES), lds, st, a);
   return 0;
 }
 
 template <int FMT>
 static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
-  return a.group <= 4 ? launch_attn<FMT, true>(a, grid, st) : launch_attn<FMT, false>(a, grid, st);
+  return a.group <= 4   ? launch_attn<FMT, 4>(a, grid, st)
+         : a.group <= 8 ? launch_attn<FMT, 2>(a, grid, st)
+                        : launch_attn<FMT, 1>(a, grid, st);
 }
 
 int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* stream) {
