@@ -12,7 +12,9 @@ namespace {
 // 1 / rms(h) is one positive factor of the whole row, so the codes round(y top /
 // max|y|) do not depend on it: y is formed from h * w alone, and the factor enters
 // s_x = max|y| / (top rms).  So the sum of squares and the maximum meet at one
-// barrier, and a row is read once and written once.
+// barrier, and a row is read once and written once: memory bounds it.  8192 x 4096 with a
+// residual takes 46.7 us (5.0 TB/s), 4000 x 14336 76.6 (5.25), as a large copy; 1000 rows, two
+// rounds of workgroups, 60 % of that.
 // Blocks of 512 columns: up to tile 512 wave w of W takes the blocks W i + w; LONG (tiles
 // of 1024 and 2048, two or four blocks) groups of four, 4 W (i / 4) + 4 w + i % 4, so that
 // a tile lies inside one wave.
