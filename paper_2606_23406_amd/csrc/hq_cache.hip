@@ -769,13 +769,13 @@ __device__ __forceinline__ void cache_finish(const hq_cache_attn_args& A, float 
   flip8(v, sign_words(A.v_dsign16, head * HQ_TILE + (lane & 15) * 8));
 }
 
-template <int FMT, int C>
-__global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_attn_kernel(
+template <int FMT, int C, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_attn_kernel(
     hq_cache_attn_args A) {
   using R = CacheRing<FMT>;
   constexpr int HEADS = 16 / C, T = products<C>();
   extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];  // a wave's ring after the other
-  __shared__ float s_m[HQ_CACHE_WAVES][HEADS], s_l[HQ_CACHE_WAVES][HEADS];
+  __shared__ float s_m[WAVES][HEADS], s_l[WAVES][HEADS];
   // term i of the query lies in the second step of wave i's ring until that is first
   // loaded, a wave's sums in its own ring at the end
   static_assert(16 * kQPitch * sizeof(uint16_t) <= R::STEP && HEADS * kOPitch * sizeof(float) <= R::WAVE, "");
@@ -805,7 +805,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   }
   // the chunk's steps of 32 tokens shared out over the waves
   const int32_t begin0 = (int32_t)((j - it.first) * it.chunk), tokens = min(it.chunk, it.len - begin0);
-  const int32_t per = (tokens + 32 * HQ_CACHE_WAVES - 1) / (32 * HQ_CACHE_WAVES) * 32;
+  const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
   CacheWalk w;
   w.table = A.table + (int64_t)it.b * A.max_blocks;
@@ -902,10 +902,10 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   if (grp >= G) return;
   float M = s_m[0][grp], L = 0.0f, v[8] = {};
 #pragma unroll
-  for (int x = 1; x < HQ_CACHE_WAVES; ++x) M = __builtin_fmaxf(M, s_m[x][grp]);
+  for (int x = 1; x < WAVES; ++x) M = __builtin_fmaxf(M, s_m[x][grp]);
   const float ref = M == -__builtin_inff() ? 0.0f : M;
 #pragma unroll
-  for (int x = 0; x < HQ_CACHE_WAVES; ++x) {
+  for (int x = 0; x < WAVES; ++x) {
     const float f = __builtin_amdgcn_exp2f(s_m[x][grp] - ref);
     L = __builtin_fmaf(f, s_l[x][grp], L);
 #pragma unroll
@@ -1021,13 +1021,22 @@ int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream) {
   return (int)hipGetLastError();
 }
 
-template <int FMT, int C>
+template <int FMT, int C, int WAVES>
 static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
   static hq_lds_granted granted;
-  constexpr size_t lds = (size_t)HQ_CACHE_WAVES * CacheRing<FMT>::WAVE;
-  if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, C>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, C>), grid, dim3(64 * HQ_CACHE_WAVES), lds, st, a);
+  constexpr size_t lds = (size_t)WAVES * CacheRing<FMT>::WAVE;
+  if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, C, WAVES>, lds, granted)) return e;
+  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, C, WAVES>), grid, dim3(64 * WAVES), lds, st, a);
   return 0;
+}
+
+// Calls that leave half the CUs without a workgroup have eight waves share its tokens.
+// (8 KV heads in E4M3: one sequence of 1000 tokens takes 10.6 us, 12.3 with four waves, 16 of
+// them 12.2 and 13.3; but 32 of 300, on every CU, 10.9 and 9.8.)
+template <int FMT, int C>
+static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
+  return grid.x <= 128 ? launch_attn<FMT, C, 2 * HQ_CACHE_WAVES>(a, grid, st)
+                       : launch_attn<FMT, C, HQ_CACHE_WAVES>(a, grid, st);
 }
 
 template <int FMT>

@@ -313,8 +313,9 @@ struct hq_cache_attn_args {
   float qscale;             // softmax scale times log2(e) / 128
 };
 
-// Workgroups of four waves; their rings take 70 KB of LDS each in the 8-bit formats, so
-// two fit a CU and 512 the chip: one round of them, and the chunks are cut for that.
+// Workgroups of four waves (eight in calls that leave CUs idle); four waves' rings take 72
+// KB of LDS in the 8-bit formats, so two workgroups fit a CU and 512 the chip: one round of
+// them, and the chunks are cut for that.
 // 16 sequences of 8192 tokens take 59.2 us at 512, 64.7 at 1024 and 69.6 at 768 (a
 // part of a round more); with eight waves and 256 they take 59.8 and uneven lengths,
 // whose rounding then opens a second round, 29.9 instead of 20.5.

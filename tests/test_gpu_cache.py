@@ -206,6 +206,17 @@ def test_attention_many_sequences(hq, B, heads, group):
     check_attention(hq, many_case(hq, "int8", B, heads, group, 48, B), heads, group, 48)
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("heads,group", [(4, 2), (2, 6), (4, 8), (3, 9), (2, 16)])
+def test_attention_enough_for_the_chip(hq, fmt, heads, group):
+    """Every head layout with more workgroups than one CU in two has."""
+    print(f"[cache] attention enough {fmt} {heads} x {group}", flush=True)
+    check_attention(hq, many_case(hq, fmt, 71, heads, group, 32, group), heads, group, 32)
+    short = list(many_case(hq, fmt, 71, heads, group, 32, group))
+    short[4], short[6] = short[4][:, :32].contiguous(), short[6].clamp(max=1024)  # no sequence is split
+    check_attention(hq, tuple(short), heads, group, 32)
+
+
 def test_attention_many_sequences_replayed_and_out_of_range(hq):
     case = many_case(hq, "e4m3", 200, 2, 2, 64, 7)
     kp, vp, kc, vc, table, q, lens, scale = case
