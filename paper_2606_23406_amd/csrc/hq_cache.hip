@@ -471,7 +471,8 @@ __global__ __launch_bounds__(kPlanThreads) void hq_cache_plan_kernel(hq_cache_at
       base += s_sum[x];
     }
     if (i < A.batch) A.parts[i] = {(int32_t)(uint32_t)at, (int32_t)n};
-    if (split) A.split[at >> 32] = (int32_t)i;
+    // (a length that changes meanwhile could make them more than the table holds)
+    if (split && (int64_t)(at >> 32) < A.joins) A.split[at >> 32] = (int32_t)i;
   }
   if (tid == 0) A.split[A.joins] = (int32_t)(base >> 32);
 }
