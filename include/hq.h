@@ -513,7 +513,7 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
  *   scale        softmax scale (1 / sqrt(128) for standard attention), finite.
  *   block_table  device int32 [batch, max_blocks]: token t of sequence b is token
  *                t % block_tokens of block block_table[b, t / block_tokens].
- *                Entries behind a sequence's last block are not read.
+ *                Entries behind a sequence's last block are not used.
  *   seq_lens     device int32 [batch] token counts; an empty sequence gives zeros.
  *                What lies in the cache behind a sequence's last token does not
  *                matter (stale codes, NaN scales).
