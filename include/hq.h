@@ -481,7 +481,7 @@ typedef struct {
  * differ) and share no memory.  Device-side, in each cache's stats: a slot past the
  * cache is skipped (HQ_ERR_INVALID_ARG); a vector with a non-finite transform
  * counts in overflow_tiles (HQ_ERR_OVERFLOW).  Host errors: HQ_ERR_INVALID_ARG,
- * HQ_ERR_UNSUPPORTED (rows * heads >= 2^31), HQ_ERR_HIP. */
+ * HQ_ERR_UNSUPPORTED (rows * heads above 2^28), HQ_ERR_HIP. */
 hq_status hq_cache_write(hq_plan_t k_plan, const void* k, int64_t ldk, const hq_cache* k_cache,
                          hq_plan_t v_plan, const void* v, int64_t ldv, const hq_cache* v_cache,
                          int32_t xt, int64_t rows, const int64_t* slots, void* stream);
@@ -527,8 +527,8 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
  * lengths, so results repeat bit for bit.  Device-side, in k->stats: a
  * length outside 0 .. max_blocks * block_tokens is clamped, tokens of a block id
  * outside the cache are left out (both HQ_ERR_INVALID_ARG).  Host errors:
- * HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (max_blocks * block_tokens above 2^30),
- * HQ_ERR_HIP. */
+ * HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (max_blocks * block_tokens above 2^30, about
+ * 2^24 sequences times KV heads), HQ_ERR_HIP. */
 hq_status hq_cache_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan_t v_plan, const hq_cache* v,
                              const void* q, int32_t qt, int64_t batch, int32_t heads_q, float scale,
                              const int32_t* block_table, int32_t max_blocks, const int32_t* seq_lens,

@@ -11,6 +11,10 @@ namespace {
 
 hq_status hip_status(int e) { return e == 0 ? HQ_OK : HQ_ERR_HIP; }
 
+// A grid holds less than 2^32 threads: 2^24 workgroups of 256 less one, and of a cache's
+// vectors, 32 a workgroup, 2^28 with room to spare.
+constexpr int64_t kMaxGroups = (1 << 24) - 1, kMaxTiles = 1 << 28;
+
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 // The plan gives the cache its signs only: tile 128, no KV option (a stored
@@ -103,7 +107,7 @@ hq_status hq_cache_write(hq_plan_t kp, const void* k, int64_t ldk, const hq_cach
     return HQ_ERR_INVALID_ARG;
   }
   if (!float_type(xt) || rows < 0) return HQ_ERR_INVALID_ARG;
-  if (rows > 0x7FFFFFFF / kc->heads) return HQ_ERR_UNSUPPORTED;
+  if (rows > kMaxTiles / kc->heads) return HQ_ERR_UNSUPPORTED;
   if (rows == 0) return HQ_OK;
   const int64_t width = (int64_t)kc->heads * HQ_TILE;
   if (!slots || !aligned(slots, 8) || !rows_ok(k, xt, ldk, width) || (both && !rows_ok(v, xt, ldv, width)))
@@ -128,7 +132,7 @@ hq_status hq_cache_read(hq_plan_t p, const hq_cache* c, const int64_t* slots, in
   hq_status st = check_cache(p, c);
   if (st != HQ_OK) return st;
   if (!float_type(yt) || rows < 0) return HQ_ERR_INVALID_ARG;
-  if (rows > 0x7FFFFFFF / c->heads) return HQ_ERR_UNSUPPORTED;
+  if (rows > kMaxTiles / c->heads) return HQ_ERR_UNSUPPORTED;
   if (rows == 0) return HQ_OK;
   if (!slots || !aligned(slots, 8) || !rows_ok(y, yt, ld, (int64_t)c->heads * HQ_TILE)) return HQ_ERR_INVALID_ARG;
   if ((st = check_device(p)) != HQ_OK) return st;
@@ -179,7 +183,7 @@ hq_status hq_cache_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, cons
     return HQ_ERR_INVALID_ARG;
   const int64_t items = hq_cache_items(batch, k->heads, max_tokens);
   const bool join = max_tokens > HQ_CACHE_WHOLE;
-  if (items * heads_q > 0x7FFFFFFF) return HQ_ERR_UNSUPPORTED;
+  if (items * heads_q > 0x7FFFFFFF || items * k->heads > kMaxGroups) return HQ_ERR_UNSUPPORTED;
   if (join && (!workspace || !aligned(workspace, 16) ||
                ws_bytes < hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)))
     return HQ_ERR_INVALID_ARG;

@@ -195,10 +195,22 @@ static void launch(const hq_norm_args& a, hipStream_t st) {
   }
 }
 
-int hq_launch_norm_prep(const hq_norm_args& a, void* stream) {
-  if (a.fp8)
-    launch<true>(a, (hipStream_t)stream);
-  else
-    launch<false>(a, (hipStream_t)stream);
-  return (int)hipGetLastError();
+int hq_launch_norm_prep(const hq_norm_args& args, void* stream) {
+  // a grid holds less than 2^32 threads: at most 2^21 rows of 1024 a launch
+  constexpr int64_t kRows = (int64_t)1 << 21;
+  hq_norm_args a = args;
+  for (int64_t left = args.M; left > 0; left -= kRows) {
+    a.M = left < kRows ? left : kRows;
+    if (a.fp8)
+      launch<true>(a, (hipStream_t)stream);
+    else
+      launch<false>(a, (hipStream_t)stream);
+    if (const hipError_t e = hipGetLastError()) return (int)e;
+    a.x = (const uint16_t*)a.x + kRows * a.ldx;
+    if (a.residual) a.residual = (const uint16_t*)a.residual + kRows * a.ldr;
+    if (a.h) a.h = (uint16_t*)a.h + kRows * a.ldh;
+    a.xq += kRows * a.K;
+    a.sx += kRows;
+  }
+  return 0;
 }

@@ -454,6 +454,22 @@ def test_refusals(hq):
     torch.cuda.synchronize()
 
 
+def test_more_work_than_a_grid_holds_is_refused(hq):
+    """2^32 threads: 2^28 vectors of a write or a read, 2^24 workgroups of an attention."""
+    import ctypes as C
+    L = hq.lib()
+    heads, bt = 4, 32
+    kp, vp, kc, vc, table, q, ln, scale = attention_case(hq, "int8", [40], heads, 2, bt)
+    p = q.cuda().data_ptr()  # never reached
+    k, v = C.byref(kc.c), C.byref(vc.c)
+    rows = (1 << 28) // heads + 1
+    assert L.hq_cache_write(kp.handle, p, heads * N, k, None, None, 0, None, 1, rows, p, None) == -2
+    assert L.hq_cache_read(kp.handle, k, p, rows, p, 1, heads * N, None) == -2
+    for blocks in (2, 400):
+        assert L.hq_cache_attention(kp.handle, k, vp.handle, v, p, 1, (1 << 24) // heads, heads, 0.1, p, blocks, p, p,
+                                    1, p, 1 << 60, None) == -2
+
+
 def test_attention_block_step_on_casts(hq):
     """A layer's attention block as it is served: residual and norm into int8, the fused QKV
     product on a coded weight, the new keys and values into the cache, attention over it; each

@@ -135,6 +135,19 @@ def test_weights_that_are_not_finite_reach_the_scale(hq, tile, fp8):
     check(big[[0, 1, 3, 4]], bad, 5, tile, 1e-5, xq[[0, 1, 3, 4]], sx[[0, 1, 3, 4]], fp8)
 
 
+def test_more_rows_than_a_grid_of_threads(hq):
+    """2^32 threads at four waves a row: the rows behind are the same rows again."""
+    plan = hq.hq_plan(cols=512, bps=4.0)
+    rows, period = (1 << 24) + 3, 1 << 10
+    x, _, w = make(period, 512, 21)
+    x, w = x.cuda(), w.cuda()
+    xq, sx = hq.hq_rmsnorm_act_prep(plan, x.repeat((rows + period - 1) // period, 1)[:rows], w)
+    ref = hq.hq_rmsnorm_act_prep(plan, x, w)
+    for at in (0, (1 << 21) - period, 1 << 21, (1 << 23) + period, (1 << 24) - period):
+        assert torch.equal(xq[at:at + period], ref[0]) and torch.equal(sx[at:at + period], ref[1])
+    assert torch.equal(xq[1 << 24:], ref[0][:3]) and torch.equal(sx[1 << 24:], ref[1][:3])
+
+
 def test_graph_replays(hq):
     plan = hq.hq_plan(cols=1024, bps=4.0)
     x, r, w = (t.cuda() for t in make(5, 1024, 9))
