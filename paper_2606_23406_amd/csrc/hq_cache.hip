@@ -25,35 +25,38 @@ constexpr int kInt8 = HQ_INT8, kE4M3 = HQ_E4M3, kMx = HQ_MXFP4;
 template <int FMT>
 constexpr int row_bytes() { return FMT == kMx ? HQ_TILE / 2 : HQ_TILE; }
 
-// 8 consecutive values (16-byte aligned) of a bf16 or fp32 array: as they lie, and as fp32.
+// 8 consecutive values (16-byte aligned) of a bf16 or fp32 array as fp32.
+__device__ __forceinline__ void load8(const void* p, int64_t i, bool bf16, float* v) {
+  if (bf16) {
+    const uint4 raw = *(const uint4*)((const uint16_t*)p + i);
+    const uint32_t w4[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = bf16_to_f32(w4[k] & 0xFFFFu);
+      v[2 * k + 1] = __uint_as_float(w4[k] & 0xFFFF0000u);
+    }
+  } else {
+    const float4 a = *(const float4*)((const float*)p + i);
+    const float4 b = *(const float4*)((const float*)p + i + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+
+// The same in two steps, so that other loads start between them.  The loads have no
+// branch, whose end would wait for them: of bf16 the second takes the first's words again.
 struct Raw8 {
   uint4 a, b;
 };
 __device__ __forceinline__ Raw8 load_raw8(const void* p, int64_t i, bool bf16) {
-  Raw8 r = {};
-  if (bf16) {
-    r.a = *(const uint4*)((const uint16_t*)p + i);
-  } else {
-    r.a = *(const uint4*)((const float*)p + i);
-    r.b = *(const uint4*)((const float*)p + i + 4);
-  }
-  return r;
+  const uint8_t* at = (const uint8_t*)p + (bf16 ? 2 * i : 4 * i);
+  return {*(const uint4*)at, *(const uint4*)(at + (bf16 ? 0 : 16))};
 }
 __device__ __forceinline__ void expand8(const Raw8& r, bool bf16, float* v) {
   const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
-  if (bf16) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[2 * k] = bf16_to_f32(w[k] & 0xFFFFu);
-      v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
-  }
-}
-__device__ __forceinline__ void load8(const void* p, int64_t i, bool bf16, float* v) {
-  expand8(load_raw8(p, i, bf16), bf16, v);
+  for (int k = 0; k < 8; ++k)
+    v[k] = __uint_as_float(!bf16 ? w[k] : k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
 }
 
 __device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const float* v) {
@@ -537,15 +540,18 @@ struct CacheWalk {
   int32_t first, ids;  // lane l: block first + l
   __amdgpu_buffer_rsrc_t k, v, ks, vs;
   bool bad;  // the block lies outside the cache: its buffers are empty
-  __device__ __forceinline__ void look_up(int lane) {
+  __device__ __forceinline__ void ask(int lane) {
     first = blk;
     ids = table[min(blk + lane, last)];
-    // the wait for it stands here: at its uses it would wait for the tokens in flight
-    asm volatile("" : "+v"(ids));
   }
-  template <int FMT>
+  // the wait for it stands here: at its uses it would wait for the tokens in flight
+  __device__ __forceinline__ void got() { asm volatile("" : "+v"(ids)); }
+  template <int FMT, bool KNOWN>  // KNOWN: the ids are those of this block on
   __device__ __forceinline__ void enter(const hq_cache_attn_args& A, int lane) {
-    if (blk - first >= 64) look_up(lane);
+    if (!KNOWN && blk - first >= 64) {
+      ask(lane);
+      got();
+    }
     const int32_t id = __builtin_amdgcn_readlane(ids, blk - first);
     bad = (uint32_t)id >= (uint32_t)A.blocks;
     if (bad && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
@@ -570,7 +576,7 @@ struct CacheWalk {
       if (t + 16 * h < end && off == A.block_tokens) {  // 16 divides a block
         off = 0;
         ++blk;
-        enter<FMT>(A, lane);
+        enter<FMT, false>(A, lane);
       }
       // a half behind the end loads its block's first tokens, one of a block outside the
       // cache nothing (its buffers are empty), so that a step is always the same loads;
@@ -826,8 +832,6 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     if (grp < G) store8(A.out, (pair0 + grp) * HQ_TILE + c0, A.out_bf16, zero);
     return;
   }
-  // the query's loads, then the table's, then the tokens': each is waited for once
-  if (A.join) load_query(it.b);
   // the chunk's steps of 32 tokens shared out over the waves
   const int32_t begin0 = (int32_t)((j - it.first) * it.chunk), tokens = min(it.chunk, it.len - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
@@ -839,12 +843,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   w.blk = min(begin / A.block_tokens, w.last);
   w.off = begin - w.blk * A.block_tokens;
   if (A.join) {
-    w.look_up(lane);
+    w.ask(lane);
+    load_query(it.b);
   } else {
     w.first = 0;
     w.ids = ids;
   }
-  w.enter<FMT>(A, lane);
+  w.got();
+  w.enter<FMT, true>(A, lane);
   uint8_t* ring = s_ring + wave * R::WAVE;
   int32_t live[2], next[2] = {0, 0};
   if (begin < end) w.fetch<FMT>(A, begin, end, lane, ring, live);
