@@ -349,8 +349,9 @@ __device__ __forceinline__ float groups_sum(float x) {
 // The tokens of a call are cut into chunks of about one length, as many workgroups
 // as the chip holds at once over all sequences and KV heads, so that a batch of uneven
 // lengths keeps it as busy as an even one.  Item j is chunk j - first of sequence b.
-// Up to 64 sequences every wave finds its item by itself, one length per lane; more are
-// planned by a launch before (hq_cache_plan_kernel), whose table the waves search.
+// Up to HQ_CACHE_UNPLANNED sequences every wave finds its item by itself, one length per
+// lane; more are planned by a launch before (hq_cache_plan_kernel), whose table the waves
+// search.
 constexpr int32_t kStep = 32 * HQ_CACHE_WAVES;
 struct CacheItem {
   int32_t b;       // -1: behind the last item
@@ -412,7 +413,7 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.chunk = HQ_CACHE_WHOLE;
     return it;
   }
-  if (A.batch > 64) {
+  if (A.batch > HQ_CACHE_UNPLANNED) {
     // the last sequence whose first item is j at most, 64 places a step
     int64_t lo = 0;
     for (int64_t span = A.batch; span > 1;) {
@@ -429,6 +430,7 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.b = (int32_t)readfirst((uint32_t)lo);
     it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, false));
   } else {
+    static_assert(HQ_CACHE_UNPLANNED <= 64, "");
     const bool in = lane < A.batch;
     const int32_t len = in ? cache_len(A, lane, tell) : -1;
     int64_t total = max(len, 0);
@@ -448,8 +450,9 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
   return it;
 }
 
-// The items of more than 64 sequences, in one workgroup.  (1024 sequences of about 900
-// tokens, 8 KV heads in int8, take 335 us; 474 with every wave going through all lengths.)
+// The items of more than HQ_CACHE_UNPLANNED sequences, in one workgroup.  (1024 sequences
+// of about 900 tokens, 8 KV heads in int8, take 335 us; 474 with every wave going through
+// all lengths.)
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void hq_cache_plan_kernel(hq_cache_attn_args A) {
   __shared__ uint64_t s_sum[kPlanThreads / 64];
@@ -825,7 +828,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   const CacheItem it = cache_item(A, j, lane, blockIdx.x == 0 && wave == 0);
   if (it.b < 0) return;
   // what the join goes by
-  if (A.join && A.batch <= 64 && j == it.first && head == 0 && tid == 0) A.parts[it.b] = {it.first, it.n};
+  if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && head == 0 && tid == 0)
+    A.parts[it.b] = {it.first, it.n};
   const int64_t pair0 = (int64_t)it.b * A.heads_q + (int64_t)head * G;
   if (it.len == 0) {
     const float zero[8] = {};
@@ -963,16 +967,16 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 }
 
 // Joins a query head's chunks under one maximum, in order, and moves the result
-// back: one workgroup per query head, 16 lanes per chunk.  Of a planned call only the split
-// sequences have one (4096 sequences of about 100 tokens, 32 query heads: 416 us so, 478
-// with a workgroup for each).
+// back: one workgroup per query head, 16 lanes per chunk, for every sequence by its index;
+// of a planned call only for the split ones (4096 sequences of about 100 tokens, 32 query
+// heads: 416 us so, 478 with a workgroup for each).
 __global__ __launch_bounds__(256) void hq_cache_join_kernel(hq_cache_attn_args A) {
   __shared__ float s_red[16];
   __shared__ float4 s_acc[16][32];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4, c0 = n * 8;
   int64_t b = blockIdx.x / (uint32_t)A.heads_q;
   const int32_t hq = (int32_t)(blockIdx.x - (uint32_t)b * (uint32_t)A.heads_q), head = hq / A.group;
-  if (A.batch > 64) {
+  if (A.batch > HQ_CACHE_UNPLANNED) {
     if (b >= A.split[A.joins]) return;
     b = A.split[b];
   }
@@ -1088,7 +1092,8 @@ int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* str
   const hipStream_t st = (hipStream_t)stream;
   const dim3 grid((uint32_t)(a.items * a.heads_kv)), wg(256);
   int e = 0;
-  if (a.join && a.batch > 64) hipLaunchKernelGGL(hq_cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
+  if (a.join && a.batch > HQ_CACHE_UNPLANNED)
+    hipLaunchKernelGGL(hq_cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
   switch (format) {
     case HQ_INT8: e = launch_attn<kInt8>(a, grid, st); break;
     case HQ_E4M3: e = launch_attn<kE4M3>(a, grid, st); break;

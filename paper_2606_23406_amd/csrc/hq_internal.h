@@ -305,7 +305,7 @@ struct hq_cache_attn_args {
   hq_stats* stats;
   int64_t batch;
   int64_t items;            // bound on the chunks of all sequences
-  int64_t joins;            // bound on the sequences of several chunks
+  int64_t joins;            // sequences that the join has workgroups for
   int32_t heads_q, heads_kv, group;
   int32_t max_blocks, blocks, block_tokens;
   int32_t join;             // a sequence may have several chunks
@@ -337,10 +337,15 @@ static inline int64_t hq_cache_items(int64_t batch, int64_t heads_kv, int64_t ma
   const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
   return batch * most < batch + even ? batch * most : batch + even;
 }
-// Bound on the sequences that have several: each takes one of what rounding does not add.
+// Up to this many sequences every wave goes through all lengths, one per lane; the items
+// of more are planned by a launch before.
+#define HQ_CACHE_UNPLANNED 64
+// Sequences that the join has workgroups for.  Of an unplanned call all, each by its own
+// index, whichever are split; of a planned one the list of those that have several chunks,
+// of which each takes one of what rounding does not add to the items.
 static inline int64_t hq_cache_joins(int64_t batch, int64_t heads_kv) {
   const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
-  return batch < even ? batch : even;
+  return batch <= HQ_CACHE_UNPLANNED || batch < even ? batch : even;
 }
 
 // RMS norm fused with the 8-bit activation prep.
