@@ -1100,6 +1100,7 @@ int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* str
     default: e = launch_attn<kMx>(a, grid, st);
   }
   if (e) return e;
-  if (a.join) hipLaunchKernelGGL(hq_cache_join_kernel, dim3((uint32_t)(a.joins * a.heads_q)), wg, 0, st, a);
+  if (a.join && a.joins)
+    hipLaunchKernelGGL(hq_cache_join_kernel, dim3((uint32_t)(a.joins * a.heads_q)), wg, 0, st, a);
   return (int)hipGetLastError();
 }

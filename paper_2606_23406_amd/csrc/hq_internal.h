@@ -342,8 +342,11 @@ static inline int64_t hq_cache_items(int64_t batch, int64_t heads_kv, int64_t ma
 #define HQ_CACHE_UNPLANNED 64
 // Sequences that the join has workgroups for.  Of an unplanned call all, each by its own
 // index, whichever are split; of a planned one the list of those that have several chunks,
-// of which each takes one of what rounding does not add to the items.
+// of which each takes one of what rounding does not add to the items.  None from
+// HQ_CACHE_WG_TARGET heads on, where a chunk is at least all sequences together; so the
+// join's grid, up to 16 query heads a KV head, stays below 2^20 workgroups.
 static inline int64_t hq_cache_joins(int64_t batch, int64_t heads_kv) {
+  if (heads_kv >= HQ_CACHE_WG_TARGET) return 0;
   const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
   return batch <= HQ_CACHE_UNPLANNED || batch < even ? batch : even;
 }

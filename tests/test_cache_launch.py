@@ -76,3 +76,24 @@ def test_the_join_reaches_every_split_sequence(attend):
                 if batch <= 64 and len(split):
                     assert split[-1] < joins, (batch, heads, split[-1], joins)
     assert checked > 1000
+
+
+def test_the_join_fits_a_grid(attend):
+    """2^24 workgroups of 256 are more threads than a grid holds.  From 512 KV heads on a chunk is at least
+    all tokens together: nothing is split, and nothing joined."""
+    shapes = [(b, h, g) for b in (1, 3, 4, 16, 63, 64, 65, 100) for g in (1, 16)
+              for h in (1, 8, 64, 256, 511, 512, 513, 4096, 1 << 16, 1 << 18, 1 << 20)]
+    done = 0
+    for (batch, heads, group), (st, launched, items, joins) in zip(shapes, attend([s + (65,) for s in shapes])):
+        if items_past_a_grid(batch, heads):
+            assert st == -2 and not launched
+            continue
+        assert st == 0 and launched == 1, (batch, heads, group)
+        assert joins * heads * group < 1 << 20, (batch, heads, group, joins)
+        assert (joins == 0) == (heads >= 512)
+        done += 1
+    assert done > 100
+
+
+def items_past_a_grid(batch, heads):
+    return min(3 * batch, batch + 512 // heads + 1) * heads >= 1 << 24

@@ -66,3 +66,15 @@ def test_long_sequences_wander_through_a_replayed_batch(hq):
         eager = call(torch.full_like(out, float("nan")))
         torch.cuda.synchronize()
         assert torch.isfinite(got).all() and torch.equal(got, eager)
+
+
+@pytest.mark.parametrize("heads", [256, 512, 600])
+def test_as_many_heads_as_workgroups(hq, heads):
+    """From 512 KV heads on no sequence is split, however long the table."""
+    lens = torch.tensor([1100, 0, 1500, 3], dtype=torch.int32)
+    kp, vp, kc, vc, table, q = case(hq, "int8", len(lens), heads, 1, heads)
+    out = torch.full_like(q, float("nan"), device="cuda")
+    hq.hq_cache_attention(kp, kc, vp, vc, q.cuda(), table.cuda(), lens.cuda(), out=out)
+    torch.cuda.synchronize()
+    ref, tol = R.attend(q.numpy(), R.values(kc), R.values(vc), table.numpy(), lens.numpy(), BT, N ** -0.5, heads, 1)
+    assert (np.abs(out.cpu().numpy() - ref) <= tol).all()  # a NaN is not
