@@ -200,9 +200,10 @@ __global__ __launch_bounds__(256) void hq_cache_write_kernel(hq_cache_io_args A)
   }
 }
 
-// The factor that an E8M0 byte stands for: 2^(byte - 127), NaN for 255.
-__device__ __forceinline__ float e8m0(uint32_t byte) {
-  return byte == 255u ? __builtin_nanf("") : byte == 0u ? 0x1p-127f : __uint_as_float(byte << 23);
+// 1 / 128 of the factor that an E8M0 byte stands for: 2^(byte - 134), NaN for 255.  Bytes
+// below 8 give subnormal factors; a code times one is a multiple of 2^-135 and exact.
+__device__ __forceinline__ float e8m0_128th(uint32_t byte) {
+  return byte == 255u ? __builtin_nanf("") : __uint_as_float(byte < 8u ? 1u << (byte + 15u) : (byte - 7u) << 23);
 }
 
 template <int FMT>
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
   const CacheTiles t(A);
   uint2 w[U];
   uint4 d[U];
-  float scale[U];
+  float scale[U];  // of the transformed codes
   bool live[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
@@ -221,7 +222,6 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
     if constexpr (FMT == kMx) {
       w[i].x = *(const uint32_t*)(S.codes + vec * row_bytes<FMT>() + c0 / 2);
       w[i].y = ((const uint8_t*)S.scales)[vec * 4 + ((lane & 15) >> 2)];
-      scale[i] = 1.0f;
     } else {
       w[i] = *(const uint2*)(S.codes + vec * row_bytes<FMT>() + c0);
       scale[i] = ((const float*)S.scales)[vec];
@@ -233,7 +233,9 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
   for (int i = 0; i < U; ++i) {
     float v[8];
     if constexpr (FMT == kMx) {
-      const float f = e8m0(w[i].y);
+      // the blocks' factors and the 1 / 128 before H: sums of vectors near the largest that
+      // can be written (X up to 125) would pass fp32 without it
+      const float f = e8m0_128th(w[i].y);
       const v2f_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i].x, 1.0f, 0);
       const v2f_t b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i].x, 1.0f, 1);
       const v2f_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i].x, 1.0f, 2);
@@ -255,8 +257,8 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
       }
     }
     fwht128_tw(v, sg);
-    // H of the codes first, then the scale: integer codes sum exactly
-    const float f = xor_sign(scale[i] * 0.0078125f, sg.sigma);
+    // int8 and E4M3: H of the codes first, then the scale: integer codes sum exactly
+    const float f = xor_sign(FMT == kMx ? 1.0f : scale[i] * 0.0078125f, sg.sigma);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= f;
     flip8(v, d[i]);
