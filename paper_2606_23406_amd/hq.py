@@ -155,11 +155,17 @@ def _check(fn, status):
         raise HQError(fn, status)
 
 
+# the current stream's handle alone, in a torch that gives it: building the Stream object
+# around it takes 2.7 us
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_handle(stream=None):
     if stream is not None:
         return stream.cuda_stream
-    # the handle alone: building torch's Stream object around it takes 2.7 us
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _dtype_code(dt):
