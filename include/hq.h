@@ -524,10 +524,14 @@ size_t hq_cache_attention_workspace_bytes(const hq_cache* k, int64_t batch, int3
  *                block_tokens is at most 1024.  Calls that may overlap (on two
  *                streams, or two captured graphs that may) need one each.
  * Scores, maxima and sums are fp32, in an order fixed by the call's shape and its
- * lengths, so results repeat bit for bit.  Device-side, in k->stats: a
- * length outside 0 .. max_blocks * block_tokens is clamped, tokens of a block id
- * outside the cache are left out (both HQ_ERR_INVALID_ARG).  Host errors:
- * HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (max_blocks * block_tokens above 2^30, about
+ * lengths, so results repeat bit for bit.  They are formed in the stored coordinates,
+ * the values' sum before its division by the weights': infinities or NaN come out where
+ * H D q, a score, or the attended tokens' |y| of one coordinate together pass 3.4e38 (of
+ * H D q and the values never while max|q| and tokens * max|v^| stay below 2.6e36), and
+ * the query loses low bits where scale H D q / 128, or scale itself, lies below 2^-100.
+ * Device-side, in k->stats: a length outside 0 .. max_blocks * block_tokens is clamped,
+ * tokens of a block id outside the cache are left out (both HQ_ERR_INVALID_ARG).  Host
+ * errors: HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (max_blocks * block_tokens above 2^30, about
  * 2^24 sequences times KV heads), HQ_ERR_HIP. */
 hq_status hq_cache_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan_t v_plan, const hq_cache* v,
                              const void* q, int32_t qt, int64_t batch, int32_t heads_q, float scale,

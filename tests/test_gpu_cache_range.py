@@ -61,3 +61,47 @@ def test_mxfp4_scales_of_the_whole_range(hq, low):
     g = torch.Generator().manual_seed(low)
     c.scales.copy_(torch.randint(low, low + 4, c.scales.shape, generator=g, dtype=torch.uint8))
     check_read(hq, plan, c, torch.randperm(2 * bt, generator=g))
+
+
+def attend_over(hq, fmt, k, v, q, scale):
+    """One sequence of all rows; the 64-bit form of what the caches hold."""
+    heads, bt, T = 4, 16, k.shape[0]
+    kp, vp = R.plans(hq, heads)
+    form = {"int8": hq.HQ_INT8, "e4m3": hq.HQ_E4M3, "mxfp4": hq.HQ_MXFP4}[fmt]
+    kc, vc = (hq.Cache(p, -(-T // bt), bt, form, heads=heads) for p in (kp, vp))
+    hq.hq_cache_write(kp, k.cuda(), kc, vp, v.cuda(), vc, torch.arange(T, device="cuda"))
+    table = torch.arange(kc.blocks, dtype=torch.int32).view(1, -1)
+    lens = torch.tensor([T], dtype=torch.int32)
+    out = hq.hq_cache_attention(kp, kc, vp, vc, q.cuda(), table.cuda(), lens.cuda(), scale=scale)
+    torch.cuda.synchronize()
+    assert kc.read_stats()["status"] == 0 and vc.read_stats()["status"] == 0
+    ref, tol = R.attend(q.numpy(), R.values(kc), R.values(vc), table.numpy(), lens.numpy(), bt, scale, heads,
+                        q.shape[1] // heads)
+    return out.cpu().numpy().astype(np.float64), ref, tol
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3", "mxfp4"])
+@pytest.mark.parametrize("tokens", [1, 100, 1500])
+@pytest.mark.parametrize("size", [2.1e36, 2.55e36])
+def test_attention_over_values_at_the_stated_bound(hq, fmt, tokens, size):
+    """tokens * |v| just below 2.6e36, every vector with all of it in one coordinate of y, the weights
+    nearly alike: the largest sums that the bound allows.  The bound is of what the cache holds:
+    2.55e36 / 1500 is 5.24 steps of MXFP4's block and stored as 6, so 1500 of them are 2.92e36, past it."""
+    g = torch.Generator().manual_seed(tokens)
+    k = 0.01 * torch.randn((tokens, 4 * N), generator=g)
+    v = torch.from_numpy(R.signs(R.SEED_V, 4 * N)).float().repeat(tokens, 1) * (size / tokens)
+    got, ref, tol = attend_over(hq, fmt, k, v, torch.randn((1, 8, N), generator=g), N ** -0.5)
+    if tokens * np.abs(ref).max() < 2.6e36:  # the rows are alike, and so is their mean
+        assert (np.abs(got - ref) <= tol).all() and np.abs(ref).min() > 1.5e36 / tokens
+    else:
+        assert (fmt, tokens, size) == ("mxfp4", 1500, 2.55e36) and tokens * np.abs(ref).max() > 2.9e36
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3", "mxfp4"])
+def test_attention_of_queries_at_the_stated_bound(hq, fmt):
+    g = torch.Generator().manual_seed(4)
+    k, v = 1e-2 * torch.randn((70, 4 * N), generator=g), torch.randn((70, 4 * N), generator=g)
+    q = torch.from_numpy(R.signs(R.SEED_K, 4 * N)).float().view(1, 4, N).repeat_interleave(2, 1) * 2.55e36
+    q[:, 1::2] *= torch.where(torch.rand((1, 4, N), generator=g) < 0.5, -1.0, 1.0)
+    got, ref, tol = attend_over(hq, fmt, k, v, q, 3e-35)
+    assert (np.abs(got - ref) <= tol).all() and np.ptp(ref) > 0.1
