@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256) void hq_cache_read_kernel(hq_cache_io_args A) 
 // lane's own but for two moves across the lane groups.
 // Every code and scale is read once, so memory bounds it: 16 x 8192 tokens of int8, 8 KV
 // heads (277 MB), take 54.4 us without the join (5.1 TB/s, a large copy's rate), 50.1 of them
-// the loads alone; MXFP4 (143 MB) 35.4 with it, its conversions nearly as long as its loads.
+// the loads alone; MXFP4 (143 MB) 35.7 with it, its conversions nearly as long as its loads.
 // Below about 40 MB the chain from lengths over block ids and tokens to the end, 5.5 us, and
 // the join's launch weigh more.
 typedef float v4_t __attribute__((ext_vector_type(4)));
@@ -652,7 +652,7 @@ struct CacheState {
 // A head has C of the 16 columns, for the three terms of its query and weights: C = 4 (up
 // to four heads) a column per term and one of zeros, in one product; C = 2 (up to eight)
 // the first two in one product and the third beside zeros in another; C = 1 three products.
-// (16 x 8192 tokens of MXFP4, 8 query heads per KV head: 37.8 us with two products, 39.9
+// (16 x 8192 tokens of MXFP4, 8 query heads per KV head: 40.0 us with two products, 42.2
 // with three.)
 template <int C>
 constexpr int products() { return C == 4 ? 1 : C == 2 ? 2 : 3; }
