@@ -15,7 +15,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ("hq_encode.hip", "hq_decode.hip", "hq
                                           "hq_cache.hip", "hq_norm.hip", "hq_host.cpp",
                                           "hq_cache_host.cpp")]
 DEPS = SOURCES + [os.path.join(CSRC, "hq_internal.h"), os.path.join(CSRC, "hq_device.h"),
-                  os.path.join(CSRC, "hq_lds.h"), os.path.join(CSRC, "calib_table.inc"),
+                  os.path.join(CSRC, "hq_lds.h"), os.path.join(CSRC, "hq_cache_device.h"), os.path.join(CSRC, "calib_table.inc"),
                   os.path.join(os.path.dirname(HERE), "include", "hq.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

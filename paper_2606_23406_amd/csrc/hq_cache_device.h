@@ -1,0 +1,377 @@
+// What the kernels over the fixed-rate key-value cache share: head vectors in and out of
+// registers, the chunks of a call's sequences, and a wave's way over a sequence's tokens.
+#ifndef HQ_CACHE_DEVICE_H
+#define HQ_CACHE_DEVICE_H
+#include <hip/hip_runtime.h>
+
+#include "hq_device.h"
+
+#pragma clang fp contract(off)
+
+namespace {
+
+typedef float v2f_t __attribute__((ext_vector_type(2)));
+
+constexpr int kInt8 = HQ_INT8, kE4M3 = HQ_E4M3, kMx = HQ_MXFP4;
+
+template <int FMT>
+constexpr int row_bytes() { return FMT == kMx ? HQ_TILE / 2 : HQ_TILE; }
+
+// 8 consecutive values (16-byte aligned) of a bf16 or fp32 array as fp32.
+__device__ __forceinline__ void load8(const void* p, int64_t i, bool bf16, float* v) {
+  if (bf16) {
+    const uint4 raw = *(const uint4*)((const uint16_t*)p + i);
+    const uint32_t w4[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = bf16_to_f32(w4[k] & 0xFFFFu);
+      v[2 * k + 1] = __uint_as_float(w4[k] & 0xFFFF0000u);
+    }
+  } else {
+    const float4 a = *(const float4*)((const float*)p + i);
+    const float4 b = *(const float4*)((const float*)p + i + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+
+// The same in two steps, so that other loads start between them.  The loads have no
+// branch, whose end would wait for them: of bf16 the second takes the first's words again.
+struct Raw8 {
+  uint4 a, b;
+};
+__device__ __forceinline__ Raw8 load_raw8(const void* p, int64_t i, bool bf16) {
+  const uint8_t* at = (const uint8_t*)p + (bf16 ? 2 * i : 4 * i);
+  return {*(const uint4*)at, *(const uint4*)(at + (bf16 ? 0 : 16))};
+}
+__device__ __forceinline__ void expand8(const Raw8& r, bool bf16, float* v) {
+  const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    v[k] = __uint_as_float(!bf16 ? w[k] : k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+}
+
+__device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const float* v) {
+  if (bf16) {
+    uint4 o;
+    o.x = cvt_pk_bf16(v[0], v[1]);
+    o.y = cvt_pk_bf16(v[2], v[3]);
+    o.z = cvt_pk_bf16(v[4], v[5]);
+    o.w = cvt_pk_bf16(v[6], v[7]);
+    *(uint4*)((uint16_t*)p + i) = o;
+  } else {
+    float* o = (float*)p + i;
+    *(float4*)o = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4*)(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+// D of the 8 columns from col on, as bf16 sign bits per pair of columns.
+__device__ __forceinline__ uint4 sign_words(const uint32_t* dsign16, int64_t col) {
+  return *(const uint4*)(dsign16 + (col >> 1));
+}
+
+__device__ __forceinline__ void flip8(float* v, uint4 d) {
+  const uint32_t w[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = xor_sign(v[2 * i], w[i] << 16);
+    v[2 * i + 1] = xor_sign(v[2 * i + 1], w[i] & 0xFFFF0000u);
+  }
+}
+
+// a / b for a constant b, correctly rounded where nothing underflows: the quotient
+// by the rounded reciprocal, corrected by its exact remainder.
+__device__ __forceinline__ float over(float a, float b) {
+  const float r = 1.0f / b, q = a * r;
+  return __builtin_fmaf(__builtin_fmaf(-b, q, a), r, q);
+}
+
+__device__ __forceinline__ void report(hq_stats* s, int32_t err) {
+  if (s) atomicCAS(&s->status, 0u, (uint32_t)err);
+}
+
+typedef float v4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 v8b_t __attribute__((ext_vector_type(8)));
+typedef uint32_t v4w_t __attribute__((ext_vector_type(4)));
+
+// Maximum and sum over the four lane groups (lanes l, l ^ 16, l ^ 32, l ^ 48): a swap
+// of a value with itself leaves the two halves (or row pairs) side by side.
+typedef uint32_t v2u_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float groups_max(float x) {
+  const v2u_t a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const v2u_t b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float groups_sum(float x) {
+  const v2u_t a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const v2u_t b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// ---- who does what
+// The tokens of a call are cut into chunks of about one length, as many workgroups
+// as the chip holds at once over all sequences and KV heads, so that a batch of uneven
+// lengths keeps it as busy as an even one.  Item j is chunk j - first of sequence b.
+// Up to HQ_CACHE_UNPLANNED sequences every wave finds its item by itself, one length per
+// lane; more are planned by a launch before (hq_cache_plan_kernel), whose table the waves
+// search.
+constexpr int32_t kStep = 32 * HQ_CACHE_WAVES;
+struct CacheItem {
+  int32_t b;       // -1: behind the last item
+  int32_t n;       // chunks of this sequence (an empty one has one, which writes its zeros)
+  int32_t first;   // the sequence's first item
+  int32_t len, chunk;
+};
+
+__device__ __forceinline__ int32_t cache_len(const hq_cache_attn_args& A, int64_t b, bool tell) {
+  const int64_t cap = (int64_t)A.max_blocks * A.block_tokens;
+  const int64_t len = A.seq_lens[b];
+  if (len >= 0 && len <= cap) return (int32_t)len;
+  if (tell) report(A.stats, HQ_ERR_INVALID_ARG);
+  return len < 0 ? 0 : (int32_t)cap;
+}
+
+__device__ __forceinline__ uint32_t cache_parts(int32_t len, uint32_t chunk) {
+  return len == 0 ? 1u : ((uint32_t)len + chunk - 1) / chunk;
+}
+
+// The longest a chunk may be: whole steps of all waves, HQ_CACHE_LEAST tokens at
+// least; one of 2^30 holds any sequence.  An even share of the workgroups aimed at
+// would be right if every sequence were a multiple of it.  A sequence's last chunk is
+// not, and what that adds opens a second round of workgroups, so the share grows by
+// eighths until the chunks fit but for a few, to its double at most.  (24 sequences of
+// up to 6001 tokens, 8 KV heads in E4M3: 560 chunks of the even share take 51.7 us, 528 of
+// its 9 / 8 take 41.4.)  More sequences than that take several rounds in any case.
+// `total`: all tokens; `mine`: a lane's or thread's own sequence's, -1 without one; `sum`
+// adds a number over all of these.
+template <typename SUM>
+__device__ __forceinline__ uint32_t cache_chunk(const hq_cache_attn_args& A, int64_t total, int32_t mine, SUM sum) {
+  const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
+  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.heads_kv;
+  uint32_t chunk = HQ_CACHE_LEAST;
+  for (int e = 8; e <= 16; ++e) {
+    const int64_t c = min(((even * e >> 3) + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
+    chunk = max(chunk, readfirst((uint32_t)c));
+    if (A.batch > few) break;
+    // about: a length a hair over a multiple may count as the multiple
+    const float per = __builtin_amdgcn_rcpf((float)chunk) * 0.999999f;
+    if (sum(mine < 0 ? 0u : max(1u, (uint32_t)__builtin_ceilf((float)mine * per))) <= few) break;
+  }
+  return chunk;
+}
+
+// Whole steps of all waves, about as many in each of a sequence's n chunks.
+__device__ __forceinline__ int32_t even_chunk(int32_t len, int32_t n) {
+  return (len + n * kStep - 1) / (n * kStep) * kStep;
+}
+
+__device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int32_t j, int lane, bool tell) {
+  CacheItem it;
+  it.b = -1;
+  if (!A.join) {  // one chunk each
+    if (j >= A.batch) return it;
+    it.b = it.first = j;
+    it.n = 1;
+    it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, true));
+    it.chunk = HQ_CACHE_WHOLE;
+    return it;
+  }
+  if (A.batch > HQ_CACHE_UNPLANNED) {
+    // the last sequence whose first item is j at most, 64 places a step
+    int64_t lo = 0;
+    for (int64_t span = A.batch; span > 1;) {
+      const int64_t stride = (span + 63) >> 6, at = lo + lane * stride;
+      const bool below = lane * stride < span && A.parts[at].first <= j;
+      const int64_t last = __popcll(__ballot(below)) - 1;  // the first place is always below
+      lo += last * stride;
+      span = min(stride, span - last * stride);
+    }
+    const hq_cache_of of = A.parts[lo];
+    it.first = (int32_t)readfirst((uint32_t)of.first);
+    it.n = (int32_t)readfirst((uint32_t)of.n);
+    if (j >= it.first + it.n) return it;
+    it.b = (int32_t)readfirst((uint32_t)lo);
+    it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, false));
+  } else {
+    static_assert(HQ_CACHE_UNPLANNED <= 64, "");
+    const bool in = lane < A.batch;
+    const int32_t len = in ? cache_len(A, lane, tell) : -1;
+    int64_t total = max(len, 0);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
+    const uint32_t chunk = cache_chunk(A, total, len, [](uint32_t n) { return wave_total(n); });
+    const uint32_t n = in ? cache_parts(len, chunk) : 0u;
+    const int32_t incl = (int32_t)wave_scan_incl(n);
+    if (j >= __builtin_amdgcn_readlane(incl, 63)) return it;
+    const int at = __popcll(__ballot(incl <= j));
+    it.b = at;
+    it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
+    it.first = __builtin_amdgcn_readlane(incl, at) - it.n;
+    it.len = __builtin_amdgcn_readlane(len, at);
+  }
+  it.chunk = even_chunk(it.len, it.n);
+  return it;
+}
+
+// ---- a wave's tokens
+// A wave's tokens come through LDS, loaded there straight from memory (no register
+// waits for them) in a ring of two steps of 32 tokens, each two halves of 16: the key
+// codes, the value codes, and the 64 bytes of scales of each (256 with their copies).  A row's 16-byte chunks are
+// permuted by its index, which the loads' source addresses do, so that the reads
+// below meet no bank twice.
+template <int FMT>
+struct CacheRing {
+  static constexpr int RB = row_bytes<FMT>();
+  static constexpr int V = 16 * RB, SCALES = 32 * RB;      // places in a half
+  static constexpr int HALF = SCALES + 512, STEP = 2 * HALF, WAVE = 2 * STEP;
+  static constexpr int LOADS = 2 * (2 * (16 * RB / 1024) + 2);  // of a step
+  // 16-byte chunk c of row r lies at chunk c ^ swizzle(r)
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t r) { return FMT == kMx ? (r >> 1) & 3 : r & 7; }
+};
+
+// One step's codes and scales in registers.
+template <int FMT>
+struct CacheStep {
+  static constexpr int KW = FMT == kMx ? 4 : 8;  // words of 32 codes
+  static constexpr int VW = FMT == kMx ? 1 : 2;  // words of 8 codes
+  uint32_t k[2][KW];         // token 16 h + l % 16, dims 32 (l / 16) ..
+  uint32_t v[2][4][VW];      // token 16 h + 4 (l / 16) + r, dims 8 (l % 16) ..
+  float ks[2][4], vs[2][4];  // fp32 scales of those four tokens
+  uint32_t kx[2], vx[2][4];  // MXFP4: the scale byte of k, the four bytes of v's tokens
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// A run of `bytes` from p on as a buffer resource (p the same in every lane).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t run_of(const void* p, int64_t at, uint32_t bytes) {
+  const uint64_t a = (uint64_t)p + at;
+  const uint64_t u = (uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)u, 0, bytes, 0x00020000);
+}
+
+// Where a wave stands in its sequence: token off of block blk of the table row, and
+// that block's head as buffers.  The ids of 64 blocks ahead are one per lane, so that
+// following the table costs a lane read and not a load that the next loads' addresses
+// wait for.
+struct CacheWalk {
+  const int32_t* table;
+  int32_t last;  // the sequence's last block
+  int32_t head, blk, off;
+  int32_t first, ids;  // lane l: block first + l
+  __amdgpu_buffer_rsrc_t k, v, ks, vs;
+  bool bad;  // the block lies outside the cache: its buffers are empty
+  __device__ __forceinline__ void ask(int lane) {
+    first = blk;
+    ids = table[min(blk + lane, last)];
+  }
+  // the wait for it stands here: at its uses it would wait for the tokens in flight
+  __device__ __forceinline__ void got() { asm volatile("" : "+v"(ids)); }
+  template <int FMT, bool KNOWN>  // KNOWN: the ids are those of this block on
+  __device__ __forceinline__ void enter(const hq_cache_attn_args& A, int lane) {
+    if (!KNOWN && blk - first >= 64) {
+      ask(lane);
+      got();
+    }
+    const int32_t id = __builtin_amdgcn_readlane(ids, blk - first);
+    bad = (uint32_t)id >= (uint32_t)A.blocks;
+    if (bad && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
+    const uint32_t n = bad ? 0u : (uint32_t)A.block_tokens;
+    const int64_t row = bad ? 0 : ((int64_t)id * A.heads_kv + head) * A.block_tokens;
+    k = run_of(A.k_codes, row * row_bytes<FMT>(), n * row_bytes<FMT>());
+    v = run_of(A.v_codes, row * row_bytes<FMT>(), n * row_bytes<FMT>());
+    ks = run_of(A.k_scales, row * 4, n * 4);
+    vs = run_of(A.v_scales, row * 4, n * 4);
+  }
+  // Starts the loads of the 32 tokens from t on into `step` (LDS) and moves the walk
+  // past them; live[h]: tokens of each half to attend to.
+  template <int FMT>
+  __device__ __forceinline__ void fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step,
+                                        int32_t (&live)[2]) {
+    using R = CacheRing<FMT>;
+    constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
+    const uint32_t row_in = lane / CPR, chunk = lane % CPR;
+    const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (t + 16 * h < end && off == A.block_tokens) {  // 16 divides a block
+        off = 0;
+        ++blk;
+        enter<FMT, false>(A, lane);
+      }
+      // a half behind the end loads its block's first tokens, one of a block outside the
+      // cache nothing (its buffers are empty), so that a step is always the same loads;
+      // nothing reads them
+      live[h] = bad ? 0 : min(max(end - t - 16 * h, 0), 16);
+      const uint32_t at = live[h] ? off : 0;
+      off += 16;
+      uint8_t* to = step + h * R::HALF;
+#pragma unroll
+      for (uint32_t i = 0; i < 16 / RPL; ++i) {
+        const uint32_t rows = at * R::RB + i * 1024;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(k, (lds_void*)(to + i * 1024), 16, from, rows, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(v, (lds_void*)(to + R::V + i * 1024), 16, from, rows, 0, 0);
+      }
+      const uint32_t token = (lane & 15) * 4;  // four times over
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_void*)(to + R::SCALES), 4, token, at * 4, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_void*)(to + R::SCALES + 256), 4, token, at * 4, 0, 0);
+    }
+  }
+};
+
+// A step's codes and scales out of LDS.
+template <int FMT>
+__device__ __forceinline__ void cache_take(const uint8_t* step, int lane, CacheStep<FMT>& s) {
+  using R = CacheRing<FMT>;
+  const uint32_t n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint8_t* half = step + h * R::HALF;
+#pragma unroll
+    for (int i = 0; i < CacheStep<FMT>::KW; i += 4) {
+      const uint32_t chunk = (FMT == kMx ? g : 2 * g + i / 4) ^ R::swizzle(n);
+      const uint4 x = *(const uint4*)(half + n * R::RB + chunk * 16);
+      s.k[h][i] = x.x; s.k[h][i + 1] = x.y; s.k[h][i + 2] = x.z; s.k[h][i + 3] = x.w;
+    }
+    const uint8_t* sc = half + R::SCALES;
+    if constexpr (FMT == kMx) {
+      s.kx[h] = sc[4 * n + g];
+      const uint4 x = *(const uint4*)(sc + 256 + 16 * g);
+      s.vx[h][0] = x.x; s.vx[h][1] = x.y; s.vx[h][2] = x.z; s.vx[h][3] = x.w;
+    } else {
+      const float4 x = *(const float4*)(sc + 16 * g);
+      const float4 y = *(const float4*)(sc + 256 + 16 * g);
+      s.ks[h][0] = x.x; s.ks[h][1] = x.y; s.ks[h][2] = x.z; s.ks[h][3] = x.w;
+      s.vs[h][0] = y.x; s.vs[h][1] = y.y; s.vs[h][2] = y.z; s.vs[h][3] = y.w;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t row = 4 * g + r;
+      if constexpr (FMT == kMx) {
+        s.v[h][r][0] = *(const uint32_t*)(half + R::V + row * R::RB + ((n >> 2) ^ R::swizzle(row)) * 16 + (n & 3) * 4);
+      } else {
+        const uint2 x = *(const uint2*)(half + R::V + row * R::RB + ((n >> 1) ^ R::swizzle(row)) * 16 + (n & 1) * 8);
+        s.v[h][r][0] = x.x; s.v[h][r][1] = x.y;
+      }
+    }
+  }
+}
+
+constexpr int kQPitch = HQ_TILE + 8;  // bf16 of a query row in LDS
+constexpr int kOPitch = HQ_TILE + 4;  // floats of an output row in LDS
+
+// v * 1 / (128 sum) moved back to the head's own coordinates.
+__device__ __forceinline__ void cache_finish(const hq_cache_attn_args& A, float L, float* v, int32_t head, int lane) {
+  const float inv = L == 0.0f ? 0.0f : 1.0f / (L * 128.0f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= inv;
+  const XSigns sg(lane);
+  fwht128(v, sg);
+  flip8(v, sign_words(A.v_dsign16, head * HQ_TILE + (lane & 15) * 8));
+}
+
+}  // namespace
+
+#endif
