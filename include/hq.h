@@ -538,6 +538,131 @@ hq_status hq_cache_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan_t v_pl
                              const int32_t* block_table, int32_t max_blocks, const int32_t* seq_lens,
                              void* out, int32_t ot, void* workspace, size_t ws_bytes, void* stream);
 
+/* Rotary positions: pair i of a head's first `dims` values, (a, b), is turned by its
+ * row's position on the pair's axis, (a c - b s, b c + a s) with c and s the table's
+ * cosine and sine; the head's other values stay.
+ *   table        device fp32 [positions, 2, dims / 2], 16-byte aligned: a position's
+ *                cosines, then its sines (hq_rope_table makes one; factors in them scale
+ *                the turned values).
+ *   dims         a multiple of 16 up to 128 (an even number that is none:
+ *                HQ_ERR_UNSUPPORTED).
+ *   interleaved  0: pair i is values i and i + dims / 2; 1: values 2 i and 2 i + 1.
+ *   axes         positions of a row, 1 .. 4 (time, height, width, ...).
+ *   axis         host, [dims / 2]: each pair's axis, below axes; may be null with one.  Read
+ *                by the call, not after it.
+ *   stats        nullable device hq_stats.
+ * A row whose first position is negative is padding; one with any other position outside
+ * 0 .. positions - 1 is reported (HQ_ERR_INVALID_ARG in stats).  Neither is written. */
+typedef struct {
+  const float* table;
+  int64_t positions;
+  int32_t dims;
+  int32_t interleaved;
+  int32_t axes;
+  int32_t reserved0;
+  const uint8_t* axis;
+  hq_stats* stats;
+} hq_rotary;
+
+/* hq_rope_table -- factor * cos(p freqs[i]) and factor * sin(p freqs[i]) of positions p =
+ * 0 .. positions - 1, formed in 64 bits and rounded once.
+ *   freqs   device fp64 [pairs], 1 .. 64 of them (HQ_ERR_UNSUPPORTED above), radians a position
+ *   table   device fp32 [positions, 2, pairs], 16-byte aligned
+ * Host errors: HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED, HQ_ERR_HIP. */
+hq_status hq_rope_table(const double* freqs, int32_t pairs, int64_t positions, float factor,
+                        float* table, void* stream);
+
+/* hq_rope -- rows of head vectors turned by their positions, in fp32, rounded once to yt.
+ *   x           device, rows x heads * 128, HQ_BF16 or HQ_FP32, row stride ldx; aligned as
+ *               for hq_cache_write
+ *   positions   device int32 [rows, axes]
+ *   transposed  0: as above; 1: the transpose, (a c + b s, b c - a s): the gradient of x from
+ *               that of y, and without a factor the inverse
+ *   y           device, as x, of type yt and stride ldy; may be x itself (same type and
+ *               stride), and may not overlap it otherwise.  Rows that are not turned (padding)
+ *               are left as they were.
+ * Host errors: HQ_ERR_INVALID_ARG, HQ_ERR_UNSUPPORTED (rows * heads above 2^28), HQ_ERR_HIP. */
+hq_status hq_rope(const hq_rotary* r, const void* x, int32_t xt, int64_t ldx, int64_t rows,
+                  int32_t heads, const int32_t* positions, int32_t transposed, void* y, int32_t yt,
+                  int64_t ldy, void* stream);
+
+/* hq_cache_append -- hq_cache_write with the keys turned on the way, and the same tokens'
+ * queries turned beside them, in one launch: y = H D rope(k), without a rounding in between.
+ *   k .. slots  as for hq_cache_write (v, v_plan and v_cache may be null together)
+ *   r           as above; positions device int32 [rows, axes].  A row without positions leaves
+ *               both sides of its slot as they were; one without a slot turns its queries.
+ *   q           nullable device, rows x heads_q * 128 of type xt, row stride ldq: turned into
+ *               q_out (type qot, stride ldqo; may be q itself with the same type and stride).
+ *               null: heads_q 0 and q_out null.
+ * q, k and v may be columns of one array; q_out may not overlap k or v.  Device-side and host
+ * errors as hq_cache_write and hq_rope. */
+hq_status hq_cache_append(hq_plan_t k_plan, const void* k, int64_t ldk, const hq_cache* k_cache,
+                          hq_plan_t v_plan, const void* v, int64_t ldv, const hq_cache* v_cache,
+                          int32_t xt, int64_t rows, const int64_t* slots, const hq_rotary* r,
+                          const int32_t* positions, const void* q, int64_t ldq, int32_t heads_q,
+                          void* q_out, int32_t qot, int64_t ldqo, void* stream);
+
+/* hq_cache_window_attention -- hq_cache_attention that looks at the last `window` tokens of
+ * each sequence and at its first `sinks` ones only: tokens t < sinks and t >= len - window.
+ *   window       1 or more; sinks 0 or more.
+ *   block_table  entries of blocks without such a token are not used: they may be freed.
+ *   workspace    >= hq_cache_window_workspace_bytes(k, batch, heads_q, max_blocks, window,
+ *                sinks); may be null where that is 0.
+ * All else, errors among it, as hq_cache_attention; what a call costs goes by the tokens it
+ * looks at.
+ * hq_cache_window_workspace_bytes -- 0 for invalid arguments, and never less for a larger
+ * batch, heads_q, max_blocks, window or sinks. */
+size_t hq_cache_window_workspace_bytes(const hq_cache* k, int64_t batch, int32_t heads_q,
+                                       int32_t max_blocks, int32_t window, int32_t sinks);
+hq_status hq_cache_window_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan_t v_plan,
+                                    const hq_cache* v, const void* q, int32_t qt, int64_t batch,
+                                    int32_t heads_q, float scale, const int32_t* block_table,
+                                    int32_t max_blocks, const int32_t* seq_lens, int32_t window,
+                                    int32_t sinks, void* out, int32_t ot, void* workspace,
+                                    size_t ws_bytes, void* stream);
+
+/* hq_cache_tree_attention -- the attention of drafted tokens: the last n tokens of a sequence
+ * (written into the cache before) are a tree, and token i of it attends over the sequence's
+ * tokens before the tree and over the tree's tokens j whose bit j its mask has (its ancestors
+ * and, if it is to see itself, bit i).  A chain (bits 0 .. i) is a causal step of n tokens.
+ *   q            device [rows, heads_q, 128], HQ_BF16 or HQ_FP32, 16-byte aligned: the trees of
+ *                all sequences one after the other
+ *   masks        device uint64 [rows]; bits from n on do not matter.  A row that sees nothing
+ *                gives zeros.
+ *   starts       device int32 [batch + 1]: sequence b has rows starts[b] .. starts[b + 1] - 1.
+ *                Rows of no sequence are left as they were.
+ *   max_tree     most rows of a sequence, 1 .. 64 (HQ_ERR_UNSUPPORTED above)
+ *   seq_lens     device int32 [batch] token counts, the tree's among them
+ *   window       0: all tokens before the tree; else a row whose mask has d bits looks at those of
+ *                the last window - d of them and at the first `sinks` tokens.  At least max_tree
+ *                (HQ_ERR_UNSUPPORTED below).
+ *   out          device [rows, heads_q, 128], HQ_FP32 or HQ_BF16, 16-byte aligned
+ *   workspace    >= hq_cache_tree_workspace_bytes(k, batch, heads_q, max_blocks, max_tree, window,
+ *                sinks); may be null where that is 0.  Overlapping calls need one each.
+ * k, v, block_table, scale and the rest as hq_cache_attention.  Scores and sums are fp32; the
+ * queries (in the stored coordinates) enter the products with 22 bits of the row's largest
+ * value, the weights with 22 bits of the row's largest term: each term is off by at most 2^-21
+ * of the largest.  Results repeat bit for bit.  Infinities or NaN come out where a score times
+ * 2^22 or the attended tokens' |y| of one coordinate together pass 3.4e38.  An E4M3 code that
+ * is a NaN (hq_cache_write stores none) makes every row of its sequence NaN; a NaN scale the
+ * rows that see its token.
+ * Device-side, in k->stats (HQ_ERR_INVALID_ARG): lengths and block ids as hq_cache_attention;
+ * a sequence whose starts fall, leave 0 .. rows or hold more rows than max_tree or than its
+ * tokens is left out, its rows as they were.  Host errors: HQ_ERR_INVALID_ARG,
+ * HQ_ERR_UNSUPPORTED, HQ_ERR_HIP.
+ * hq_cache_tree_workspace_bytes -- 0 for invalid arguments, and never less for a larger batch,
+ * heads_q, max_blocks, max_tree, window (0 the largest) or sinks. */
+size_t hq_cache_tree_workspace_bytes(const hq_cache* k, int64_t batch, int32_t heads_q,
+                                     int32_t max_blocks, int32_t max_tree, int32_t window,
+                                     int32_t sinks);
+hq_status hq_cache_tree_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan_t v_plan,
+                                  const hq_cache* v, const void* q, int32_t qt, int64_t rows,
+                                  int32_t heads_q, float scale, const uint64_t* masks,
+                                  const int32_t* starts, int64_t batch, int32_t max_tree,
+                                  const int32_t* block_table, int32_t max_blocks,
+                                  const int32_t* seq_lens, int32_t window, int32_t sinks, void* out,
+                                  int32_t ot, void* workspace, size_t ws_bytes, void* stream);
+
 /* hq_rmsnorm_act_prep -- the residual's addition, an RMS norm and hq_act_prep in
  * one pass: h = bf16(x + residual), y = H D (h * weight) / rms(h) per tile with
  * rms(h) = sqrt(mean(h^2) + eps), then x_q and s_x of y as hq_act_prep defines them

@@ -78,44 +78,7 @@ __global__ __launch_bounds__(256) void hq_cache_write_kernel(hq_cache_io_args A)
     const bool live = t.at(A, S, lane, i, vec);
     flip8(v[i], d[i]);
     fwht128_tw(v[i], sg);
-    float am = amax_or_nan<8>(v[i]);
-    am = __builtin_elementwise_maximum(am, dpp_xor<1>(am));
-    am = __builtin_elementwise_maximum(am, dpp_xor<2>(am));
-    am = __builtin_elementwise_maximum(am, swz_xor4(am));
-    am = __builtin_elementwise_maximum(am, dpp_xor<8>(am));
-    // a vector with an infinite or NaN value has no scale: codes 0, scale NaN
-    const bool bad = !(am <= 3.4028234663852886e38f);
-    if (__builtin_expect(bad, 0)) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
-      if (live && (lane & 15) == 0 && S.stats) {
-        atomicAdd(&S.stats->overflow_tiles, 1u);
-        report(S.stats, HQ_ERR_OVERFLOW);
-      }
-    }
-    if constexpr (FMT == kMx) {
-      int32_t X;
-      const uint32_t packed = mxfp4_x8(v[i], X) ^ (sg.sigma ? 0x88888888u : 0u);
-      if (!live) continue;
-      *(uint32_t*)(S.codes + vec * row_bytes<FMT>() + c0 / 2) = packed;
-      if ((lane & 3) == 0) ((uint8_t*)S.scales)[vec * 4 + ((lane & 15) >> 2)] = bad ? 0xFFu : (uint8_t)(X + 127);
-    } else {
-      constexpr float top = FMT == kE4M3 ? 448.0f : 127.0f;
-      // below 2^-100 the reciprocal could overflow: such a vector is stored as zeros
-      const bool zero = bad || am < 0x1p-100f;
-      const float inv = zero ? 0.0f : xor_sign(top / am, sg.sigma);
-      // |q| is top (1 + 2^-23) at most, which rounds to top in both formats: no clamp
-      uint2 packed;
-      if constexpr (FMT == kE4M3) {
-        packed.x = e4m3x4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-        packed.y = e4m3x4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
-      } else {
-        packed = int8x8(v[i], inv);
-      }
-      if (!live) continue;
-      *(uint2*)(S.codes + vec * row_bytes<FMT>() + c0) = packed;
-      if ((lane & 15) == 0) ((float*)S.scales)[vec] = bad ? __builtin_nanf("") : zero ? 0.0f : over(am, top);
-    }
+    cache_put<FMT>(S, v[i], live, vec, lane, sg);
   }
 }
 
@@ -213,11 +176,6 @@ __device__ __forceinline__ v4_t mfma_bf16(const uint32_t* a, const uint32_t* b, 
                                                  0, 0);
 }
 
-// The high halves of two words: two bf16 from two fp32 by truncation, lo first.
-__device__ __forceinline__ uint32_t high_pair(uint32_t lo, uint32_t hi) {
-  return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-}
-
 // v as three bf16 terms (as fp32 bit patterns whose low halves do not matter).
 __device__ __forceinline__ void three_terms(float v, uint32_t* t) {
   t[0] = __float_as_uint(v);
@@ -251,6 +209,7 @@ __device__ __forceinline__ void pairs_of(uint32_t w, float f, uint32_t* o) {
 // of about 900 tokens, 8 KV heads in int8, take 335 us; 474 with every wave going through
 // all lengths.)
 constexpr int kPlanThreads = 1024;
+template <int MODE>
 __global__ __launch_bounds__(kPlanThreads) void hq_cache_plan_kernel(hq_cache_attn_args A) {
   __shared__ uint64_t s_sum[kPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -265,17 +224,21 @@ __global__ __launch_bounds__(kPlanThreads) void hq_cache_plan_kernel(hq_cache_at
     for (int i = 0; i < kPlanThreads / 64; ++i) x += s_sum[i];
     return x;
   };
+  auto seen = [&](int64_t i, bool tell) {
+    const CacheSpan of = cache_span_of<MODE>(A, i, tell);
+    return MODE == kAll ? of.len : of.seen();
+  };
   int64_t total = 0;
-  for (int64_t i = tid; i < A.batch; i += kPlanThreads) total += cache_len(A, i, true);
+  for (int64_t i = tid; i < A.batch; i += kPlanThreads) total += seen(i, true);
   total = (int64_t)sum((uint64_t)total);
   // it counts chunks for few sequences only: at most one per thread
   static_assert(HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32 <= kPlanThreads, "");
-  const uint32_t chunk = cache_chunk(A, total, tid < A.batch ? cache_len(A, tid, false) : -1,
+  const uint32_t chunk = cache_chunk(A, total, tid < A.batch ? seen(tid, false) : -1,
                                      [&](uint32_t n) { return (int64_t)sum(n); });
   uint64_t base = 0;  // items, and from bit 32 on split sequences, before these
   for (int64_t i0 = 0; i0 < A.batch; i0 += kPlanThreads) {
     const int64_t i = i0 + tid;
-    const uint32_t n = i < A.batch ? cache_parts(cache_len(A, i, false), chunk) : 0u, split = n > 1;
+    const uint32_t n = i < A.batch ? cache_parts(seen(i, false), chunk) : 0u, split = n > 1;
     uint32_t items = n, splits = split;
     wave_scan_incl2(items, splits);
     __syncthreads();  // the last sums have been read
@@ -309,19 +272,21 @@ struct CacheState {
 template <int C>
 constexpr int products() { return C == 4 ? 1 : C == 2 ? 2 : 3; }
 
-template <int FMT, int C>
+template <int FMT, int C, int MODE>
 __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&live)[2],
                                            const uint32_t (&q)[products<C>()][4][4], int lane, CacheState& z) {
   constexpr int T = products<C>();
   const int n = lane & 15, g = lane >> 4;
-  if (live[0] + live[1] < 32) {
+  const bool cut = MODE == kAll ? live[0] + live[1] < 32 : (live[0] & live[1]) != 0xFFFF;
+  auto dead = [&](int h, int r) { return MODE == kAll ? 4 * g + r >= live[h] : !((live[h] >> (4 * g + r)) & 1); };
+  if (cut) {
     // stale or absent tokens: their value codes count as zeros (their weight is
     // zero, but a stale code or scale may be a NaN)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (4 * g + r >= live[h]) {
+        if (dead(h, r)) {
 #pragma unroll
           for (int i = 0; i < CacheStep<FMT>::VW; ++i) cur.v[h][r][i] = 0u;
           cur.ks[h][r] = cur.vs[h][r] = 0.0f;
@@ -357,12 +322,12 @@ __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&
       p[h][r] = FMT == kMx ? x : x * cur.ks[h][r];
     }
   }
-  if (live[0] + live[1] < 32) {
+  if (cut) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (4 * g + r >= live[h]) p[h][r] = -__builtin_inff();
+        if (dead(h, r)) p[h][r] = -__builtin_inff();
   }
   // a NaN stays one: it makes the head's outputs NaN
   float top = p[0][0];
@@ -433,7 +398,7 @@ __device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&
   }
 }
 
-template <int FMT, int C, int WAVES>
+template <int FMT, int C, int WAVES, int MODE>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_attn_kernel(
     hq_cache_attn_args A) {
   using R = CacheRing<FMT>;
@@ -460,45 +425,45 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   };
   // A call that splits nothing knows its sequence: the whole table row (64 blocks at most)
   // and the query are on their way while the length is.  (8 of 1000 tokens: 11.1 us, 11.6.)
+  // Where a window's blocks lie in the row goes by the length.
   int32_t ids = 0;
   if (!A.join && j < A.batch) {
     static_assert(HQ_CACHE_WHOLE <= 64 * 16, "");
-    ids = A.table[(int64_t)j * A.max_blocks + min(lane, A.max_blocks - 1)];
+    if (MODE == kAll) ids = A.table[(int64_t)j * A.max_blocks + min(lane, A.max_blocks - 1)];
     load_query(j);
   }
-  const CacheItem it = cache_item(A, j, lane, blockIdx.x == 0 && wave == 0);
+  const CacheItem it = cache_item<MODE>(A, j, lane, blockIdx.x == 0 && wave == 0);
   if (it.b < 0) return;
   // what the join goes by
   if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && head == 0 && tid == 0)
     A.parts[it.b] = {it.first, it.n};
   const int64_t pair0 = (int64_t)it.b * A.heads_q + (int64_t)head * G;
-  if (it.len == 0) {
+  const int32_t seen = MODE == kAll ? it.span.len : it.span.seen();
+  if (seen == 0) {
     const float zero[8] = {};
     if (grp < G) store8(A.out, (pair0 + grp) * HQ_TILE + c0, A.out_bf16, zero);
     return;
   }
   // the chunk's steps of 32 tokens shared out over the waves
-  const int32_t begin0 = (int32_t)((j - it.first) * it.chunk), tokens = min(it.chunk, it.len - begin0);
+  const int32_t begin0 = (int32_t)((j - it.first) * it.chunk), tokens = min(it.chunk, seen - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
-  CacheWalk w;
+  CacheWalk<MODE> w;
   w.table = A.table + (int64_t)it.b * A.max_blocks;
-  w.last = (it.len - 1) / A.block_tokens;
   w.head = head;
-  w.blk = min(begin / A.block_tokens, w.last);
-  w.off = begin - w.blk * A.block_tokens;
-  if (A.join) {
+  w.start(A, it.span, begin);
+  if (A.join || MODE != kAll) {
     w.ask(lane);
-    load_query(it.b);
+    if (A.join) load_query(it.b);
   } else {
     w.first = 0;
     w.ids = ids;
   }
   w.got();
-  w.enter<FMT, true>(A, lane);
+  w.template enter<FMT, true>(A, lane);
   uint8_t* ring = s_ring + wave * R::WAVE;
-  int32_t live[2], next[2] = {0, 0};
-  if (begin < end) w.fetch<FMT>(A, begin, end, lane, ring, live);
+  int32_t live[2], next[2] = {0, 0}, at[2];
+  if (begin < end) w.template fetch<FMT>(A, begin, end, lane, ring, live, at);
   // ---- the query into the cache's coordinates, as three bf16 terms
   if (grp < HEADS) {
     float qv[8];
@@ -538,7 +503,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   z.l = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) z.acc[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  if (begin + 32 < end) w.fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP, next);
+  if (begin + 32 < end) w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP, next, at);
   int32_t slot = 0;
   for (int32_t t = begin; t < end; t += 32) {
     // the loads of this step are done when at most the next step's are not
@@ -553,10 +518,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     live[1] = next[1];
     if (t + 64 < end) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
-      w.fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next);
+      w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next, at);
     }
     slot ^= 1;
-    cache_step<FMT, C>(cur, here, q, lane, z);
+    cache_step<FMT, C, MODE>(cur, here, q, lane, z);
   }
   z.l = groups_sum(z.l);
   // ---- the waves' sums under one maximum, one head per 16 lanes
@@ -704,44 +669,59 @@ int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream) {
   return (int)hipGetLastError();
 }
 
-template <int FMT, int C, int WAVES>
+template <int FMT, int C, int WAVES, int MODE>
 static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
   static hq_lds_granted granted;
   constexpr size_t lds = (size_t)WAVES * CacheRing<FMT>::WAVE;
-  if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, C, WAVES>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, C, WAVES>), grid, dim3(64 * WAVES), lds, st, a);
+  if (const int e = hq_allow_lds((const void*)hq_cache_attn_kernel<FMT, C, WAVES, MODE>, lds, granted)) return e;
+  hipLaunchKernelGGL((hq_cache_attn_kernel<FMT, C, WAVES, MODE>), grid, dim3(64 * WAVES), lds, st, a);
   return 0;
 }
 
 // Calls that leave half the CUs without a workgroup have eight waves share its tokens.
 // (8 KV heads in E4M3: one sequence of 1000 tokens takes 10.6 us, 12.3 with four waves, 16 of
 // them 12.2 and 13.3; but 32 of 300, on every CU, 10.9 and 9.8.)
-template <int FMT, int C>
+template <int FMT, int C, int MODE>
 static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
-  return grid.x <= 128 ? launch_attn<FMT, C, 2 * HQ_CACHE_WAVES>(a, grid, st)
-                       : launch_attn<FMT, C, HQ_CACHE_WAVES>(a, grid, st);
+  return grid.x <= 128 ? launch_attn<FMT, C, 2 * HQ_CACHE_WAVES, MODE>(a, grid, st)
+                       : launch_attn<FMT, C, HQ_CACHE_WAVES, MODE>(a, grid, st);
 }
 
-template <int FMT>
+template <int FMT, int MODE>
 static int launch_attn(const hq_cache_attn_args& a, dim3 grid, hipStream_t st) {
-  return a.group <= 4   ? launch_attn<FMT, 4>(a, grid, st)
-         : a.group <= 8 ? launch_attn<FMT, 2>(a, grid, st)
-                        : launch_attn<FMT, 1>(a, grid, st);
+  return a.group <= 4   ? launch_attn<FMT, 4, MODE>(a, grid, st)
+         : a.group <= 8 ? launch_attn<FMT, 2, MODE>(a, grid, st)
+                        : launch_attn<FMT, 1, MODE>(a, grid, st);
 }
 
-int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* stream) {
+void hq_launch_cache_plan(const hq_cache_attn_args& a, void* stream) {
   const hipStream_t st = (hipStream_t)stream;
+  const dim3 one(1), wg(kPlanThreads);
+  if (a.starts)
+    hipLaunchKernelGGL(hq_cache_plan_kernel<kTree>, one, wg, 0, st, a);
+  else if (a.window)
+    hipLaunchKernelGGL(hq_cache_plan_kernel<kWindow>, one, wg, 0, st, a);
+  else
+    hipLaunchKernelGGL(hq_cache_plan_kernel<kAll>, one, wg, 0, st, a);
+}
+
+template <int MODE>
+static int launch_attn(const hq_cache_attn_args& a, int format, hipStream_t st) {
   const dim3 grid((uint32_t)(a.items * a.heads_kv)), wg(256);
   int e = 0;
-  if (a.join && a.batch > HQ_CACHE_UNPLANNED)
-    hipLaunchKernelGGL(hq_cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
+  if (a.join && a.batch > HQ_CACHE_UNPLANNED) hq_launch_cache_plan(a, st);
   switch (format) {
-    case HQ_INT8: e = launch_attn<kInt8>(a, grid, st); break;
-    case HQ_E4M3: e = launch_attn<kE4M3>(a, grid, st); break;
-    default: e = launch_attn<kMx>(a, grid, st);
+    case HQ_INT8: e = launch_attn<kInt8, MODE>(a, grid, st); break;
+    case HQ_E4M3: e = launch_attn<kE4M3, MODE>(a, grid, st); break;
+    default: e = launch_attn<kMx, MODE>(a, grid, st);
   }
   if (e) return e;
   if (a.join && a.joins)
     hipLaunchKernelGGL(hq_cache_join_kernel, dim3((uint32_t)(a.joins * a.heads_q)), wg, 0, st, a);
   return (int)hipGetLastError();
+}
+
+int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* stream) {
+  return a.window ? launch_attn<kWindow>(a, format, (hipStream_t)stream)
+                  : launch_attn<kAll>(a, format, (hipStream_t)stream);
 }

@@ -91,9 +91,60 @@ __device__ __forceinline__ void report(hq_stats* s, int32_t err) {
   if (s) atomicCAS(&s->status, 0u, (uint32_t)err);
 }
 
+// Casts a vector of 16 lanes' transformed values, sigma times y (TwSigns), and stores it as
+// vector vec of the cache where it is live.
+template <int FMT>
+__device__ __forceinline__ void cache_put(const hq_cache_side& S, float* v, bool live, int64_t vec, int lane,
+                                          const TwSigns& sg) {
+  const int c0 = (lane & 15) * 8;
+  float am = amax_or_nan<8>(v);
+  am = __builtin_elementwise_maximum(am, dpp_xor<1>(am));
+  am = __builtin_elementwise_maximum(am, dpp_xor<2>(am));
+  am = __builtin_elementwise_maximum(am, swz_xor4(am));
+  am = __builtin_elementwise_maximum(am, dpp_xor<8>(am));
+  // a vector with an infinite or NaN value has no scale: codes 0, scale NaN
+  const bool bad = !(am <= 3.4028234663852886e38f);
+  if (__builtin_expect(bad, 0)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    if (live && (lane & 15) == 0 && S.stats) {
+      atomicAdd(&S.stats->overflow_tiles, 1u);
+      report(S.stats, HQ_ERR_OVERFLOW);
+    }
+  }
+  if constexpr (FMT == kMx) {
+    int32_t X;
+    const uint32_t packed = mxfp4_x8(v, X) ^ (sg.sigma ? 0x88888888u : 0u);
+    if (!live) return;
+    *(uint32_t*)(S.codes + vec * row_bytes<FMT>() + c0 / 2) = packed;
+    if ((lane & 3) == 0) ((uint8_t*)S.scales)[vec * 4 + ((lane & 15) >> 2)] = bad ? 0xFFu : (uint8_t)(X + 127);
+  } else {
+    constexpr float top = FMT == kE4M3 ? 448.0f : 127.0f;
+    // below 2^-100 the reciprocal could overflow: such a vector is stored as zeros
+    const bool zero = bad || am < 0x1p-100f;
+    const float inv = zero ? 0.0f : xor_sign(top / am, sg.sigma);
+    // |q| is top (1 + 2^-23) at most, which rounds to top in both formats: no clamp
+    uint2 packed;
+    if constexpr (FMT == kE4M3) {
+      packed.x = e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+      packed.y = e4m3x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+    } else {
+      packed = int8x8(v, inv);
+    }
+    if (!live) return;
+    *(uint2*)(S.codes + vec * row_bytes<FMT>() + c0) = packed;
+    if ((lane & 15) == 0) ((float*)S.scales)[vec] = bad ? __builtin_nanf("") : zero ? 0.0f : over(am, top);
+  }
+}
+
 typedef float v4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b_t __attribute__((ext_vector_type(8)));
 typedef uint32_t v4w_t __attribute__((ext_vector_type(4)));
+
+// The high halves of two words: two bf16 from two fp32 by truncation, lo first.
+__device__ __forceinline__ uint32_t high_pair(uint32_t lo, uint32_t hi) {
+  return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
 
 // Maximum and sum over the four lane groups (lanes l, l ^ 16, l ^ 32, l ^ 48): a swap
 // of a value with itself leaves the two halves (or row pairs) side by side.
@@ -119,13 +170,6 @@ __device__ __forceinline__ float groups_sum(float x) {
 // lane; more are planned by a launch before (hq_cache_plan_kernel), whose table the waves
 // search.
 constexpr int32_t kStep = 32 * HQ_CACHE_WAVES;
-struct CacheItem {
-  int32_t b;       // -1: behind the last item
-  int32_t n;       // chunks of this sequence (an empty one has one, which writes its zeros)
-  int32_t first;   // the sequence's first item
-  int32_t len, chunk;
-};
-
 __device__ __forceinline__ int32_t cache_len(const hq_cache_attn_args& A, int64_t b, bool tell) {
   const int64_t cap = (int64_t)A.max_blocks * A.block_tokens;
   const int64_t len = A.seq_lens[b];
@@ -133,6 +177,62 @@ __device__ __forceinline__ int32_t cache_len(const hq_cache_attn_args& A, int64_
   if (tell) report(A.stats, HQ_ERR_INVALID_ARG);
   return len < 0 ? 0 : (int32_t)cap;
 }
+
+// Which tokens of a sequence an attention looks at: all of them; those of a window with the
+// first ones (sinks); those before and of a tree of drafted tokens, the sequence's last ones.
+constexpr int kAll = 0, kWindow = 1, kTree = 2;
+
+// Tokens [0, sinks) and [low, len).  The way over them goes by groups of 16, with `gap` tokens
+// between the sinks' last group and the window's first left out: token i on the way is token
+// i below the sinks' end (rounded up), i + gap behind it.
+struct CacheSpan {
+  int32_t len;         // 0: nothing
+  int32_t low, sinks;  // sinks <= low
+  int32_t rows;        // drafted tokens
+  __device__ __forceinline__ int32_t turn() const { return (sinks + 15) & ~15; }
+  __device__ __forceinline__ int32_t gap() const { return max((low & ~15) - turn(), 0); }
+  __device__ __forceinline__ int32_t seen() const { return len - gap(); }
+  // bit i: token at + i is looked at
+  __device__ __forceinline__ uint32_t bits(int32_t at) const {
+    auto below = [&](int32_t t) { return (1u << min(max(t - at, 0), 16)) - 1u; };
+    return below(sinks) | (below(len) & ~below(low));
+  }
+};
+
+template <int MODE>
+__device__ __forceinline__ CacheSpan cache_span(const hq_cache_attn_args& A, int32_t len, int32_t rows) {
+  CacheSpan s = {len, 0, 0, rows};
+  if (MODE != kAll && A.window) {
+    s.low = max(len - rows - A.window, 0);
+    s.sinks = min(A.sinks, s.low);
+  }
+  return s;
+}
+
+// Drafted tokens of sequence b (0 for the other modes).  Places that are out of order or range,
+// more tokens than the call's bound or than the sequence: reported, and none.
+template <int MODE>
+__device__ __forceinline__ int32_t cache_rows(const hq_cache_attn_args& A, int64_t b, int32_t len, bool tell) {
+  if (MODE != kTree) return 0;
+  const int32_t from = A.starts[b], to = A.starts[b + 1];
+  const bool ok = from >= 0 && to >= from && to <= A.rows && to - from <= A.max_rows && to - from <= len;
+  if (!ok && tell) report(A.stats, HQ_ERR_INVALID_ARG);
+  return ok ? to - from : 0;
+}
+
+template <int MODE>
+__device__ __forceinline__ CacheSpan cache_span_of(const hq_cache_attn_args& A, int64_t b, bool tell) {
+  const int32_t len = cache_len(A, b, tell), rows = cache_rows<MODE>(A, b, len, tell);
+  return cache_span<MODE>(A, MODE == kTree && rows == 0 ? 0 : len, rows);
+}
+
+struct CacheItem {
+  int32_t b;       // -1: behind the last item
+  int32_t n;       // chunks of this sequence (an empty one has one, which writes its zeros)
+  int32_t first;   // the sequence's first item
+  int32_t chunk;
+  CacheSpan span;  // its tokens
+};
 
 __device__ __forceinline__ uint32_t cache_parts(int32_t len, uint32_t chunk) {
   return len == 0 ? 1u : ((uint32_t)len + chunk - 1) / chunk;
@@ -149,8 +249,8 @@ __device__ __forceinline__ uint32_t cache_parts(int32_t len, uint32_t chunk) {
 // adds a number over all of these.
 template <typename SUM>
 __device__ __forceinline__ uint32_t cache_chunk(const hq_cache_attn_args& A, int64_t total, int32_t mine, SUM sum) {
-  const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
-  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.heads_kv;
+  const int64_t even = (total * A.units + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
+  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.units;
   uint32_t chunk = HQ_CACHE_LEAST;
   for (int e = 8; e <= 16; ++e) {
     const int64_t c = min(((even * e >> 3) + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
@@ -168,6 +268,7 @@ __device__ __forceinline__ int32_t even_chunk(int32_t len, int32_t n) {
   return (len + n * kStep - 1) / (n * kStep) * kStep;
 }
 
+template <int MODE>
 __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int32_t j, int lane, bool tell) {
   CacheItem it;
   it.b = -1;
@@ -175,7 +276,9 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     if (j >= A.batch) return it;
     it.b = it.first = j;
     it.n = 1;
-    it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, true));
+    const CacheSpan s = cache_span_of<MODE>(A, it.b, true);
+    it.span = {(int32_t)readfirst((uint32_t)s.len), (int32_t)readfirst((uint32_t)s.low),
+               (int32_t)readfirst((uint32_t)s.sinks), (int32_t)readfirst((uint32_t)s.rows)};
     it.chunk = HQ_CACHE_WHOLE;
     return it;
   }
@@ -194,11 +297,14 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.n = (int32_t)readfirst((uint32_t)of.n);
     if (j >= it.first + it.n) return it;
     it.b = (int32_t)readfirst((uint32_t)lo);
-    it.len = (int32_t)readfirst((uint32_t)cache_len(A, it.b, false));
+    const CacheSpan s = cache_span_of<MODE>(A, it.b, false);
+    it.span = {(int32_t)readfirst((uint32_t)s.len), (int32_t)readfirst((uint32_t)s.low),
+               (int32_t)readfirst((uint32_t)s.sinks), (int32_t)readfirst((uint32_t)s.rows)};
   } else {
     static_assert(HQ_CACHE_UNPLANNED <= 64, "");
     const bool in = lane < A.batch;
-    const int32_t len = in ? cache_len(A, lane, tell) : -1;
+    const CacheSpan s = in ? cache_span_of<MODE>(A, lane, tell) : CacheSpan{-1, 0, 0, 0};
+    const int32_t len = MODE == kAll ? s.len : s.seen();
     int64_t total = max(len, 0);
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
@@ -210,9 +316,10 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.b = at;
     it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
     it.first = __builtin_amdgcn_readlane(incl, at) - it.n;
-    it.len = __builtin_amdgcn_readlane(len, at);
+    it.span = cache_span<MODE>(A, __builtin_amdgcn_readlane(s.len, at),
+                               MODE == kTree ? __builtin_amdgcn_readlane(s.rows, at) : 0);
   }
-  it.chunk = even_chunk(it.len, it.n);
+  it.chunk = even_chunk(MODE == kAll ? it.span.len : it.span.seen(), it.n);
   return it;
 }
 
@@ -255,17 +362,49 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t run_of(const void* p, int64_t 
 // Where a wave stands in its sequence: token off of block blk of the table row, and
 // that block's head as buffers.  The ids of 64 blocks ahead are one per lane, so that
 // following the table costs a lane read and not a load that the next loads' addresses
-// wait for.
+// wait for.  Blocks are numbered along the way: of a window, those of the sinks up to
+// `before`, then those of the window, `skip` further on in the table row.
+template <int MODE>
 struct CacheWalk {
   const int32_t* table;
-  int32_t last;  // the sequence's last block
+  int32_t last;  // the way's last block
   int32_t head, blk, off;
   int32_t first, ids;  // lane l: block first + l
   __amdgpu_buffer_rsrc_t k, v, ks, vs;
   bool bad;  // the block lies outside the cache: its buffers are empty
+  CacheSpan span;
+  int32_t jump, before, skip, to_off, gap;
+  // To token `begin` of the way.
+  __device__ __forceinline__ void start(const hq_cache_attn_args& A, const CacheSpan& s, int32_t begin) {
+    const int32_t bt = A.block_tokens;
+    last = (s.len - 1) / bt;
+    if constexpr (MODE == kAll) {
+      blk = min(begin / bt, last);
+      off = begin - blk * bt;
+    } else {
+      span = s;
+      gap = s.gap();
+      before = 0x7FFFFFFF;
+      jump = -1;
+      skip = to_off = 0;
+      if (gap) {
+        jump = s.turn();
+        const int32_t to = (jump + gap) / bt;
+        to_off = jump + gap - to * bt;
+        before = (jump + bt - 1) / bt - 1;
+        skip = to - before - 1;
+        last -= skip;
+      }
+      const int32_t real = gap && begin >= jump ? begin + gap : begin, at = real / bt;
+      blk = min(real == begin ? at : at - skip, last);
+      off = real - at * bt;
+    }
+  }
   __device__ __forceinline__ void ask(int lane) {
     first = blk;
-    ids = table[min(blk + lane, last)];
+    int32_t x = min(blk + lane, last);
+    if (MODE != kAll) x += x > before ? skip : 0;
+    ids = table[x];
   }
   // the wait for it stands here: at its uses it would wait for the tokens in flight
   __device__ __forceinline__ void got() { asm volatile("" : "+v"(ids)); }
@@ -286,37 +425,49 @@ struct CacheWalk {
     vs = run_of(A.v_scales, row * 4, n * 4);
   }
   // Starts the loads of the 32 tokens from t on into `step` (LDS) and moves the walk
-  // past them; live[h]: tokens of each half to attend to.
+  // past them; live[h]: tokens of each half to attend to, of kAll their number, else one bit
+  // each; at[h] (not of kAll): a half's first token.
   template <int FMT>
   __device__ __forceinline__ void fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step,
-                                        int32_t (&live)[2]) {
+                                        int32_t (&live)[2], int32_t (&at)[2]) {
     using R = CacheRing<FMT>;
     constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
     const uint32_t row_in = lane / CPR, chunk = lane % CPR;
     const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (t + 16 * h < end && off == A.block_tokens) {  // 16 divides a block
-        off = 0;
-        ++blk;
-        enter<FMT, false>(A, lane);
+      if (t + 16 * h < end) {
+        if (MODE != kAll && t + 16 * h == jump && blk <= before) {
+          off = to_off;
+          ++blk;
+          enter<FMT, false>(A, lane);
+        } else if (off == A.block_tokens) {  // 16 divides a block
+          off = 0;
+          ++blk;
+          enter<FMT, false>(A, lane);
+        }
       }
       // a half behind the end loads its block's first tokens, one of a block outside the
       // cache nothing (its buffers are empty), so that a step is always the same loads;
       // nothing reads them
-      live[h] = bad ? 0 : min(max(end - t - 16 * h, 0), 16);
-      const uint32_t at = live[h] ? off : 0;
+      if constexpr (MODE == kAll) {
+        live[h] = bad ? 0 : min(max(end - t - 16 * h, 0), 16);
+      } else {
+        at[h] = t + 16 * h + (blk > before ? gap : 0);
+        live[h] = bad || t + 16 * h >= end ? 0 : (int32_t)span.bits(at[h]);
+      }
+      const uint32_t place = live[h] ? off : 0;
       off += 16;
       uint8_t* to = step + h * R::HALF;
 #pragma unroll
       for (uint32_t i = 0; i < 16 / RPL; ++i) {
-        const uint32_t rows = at * R::RB + i * 1024;
+        const uint32_t rows = place * R::RB + i * 1024;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(k, (lds_void*)(to + i * 1024), 16, from, rows, 0, 0);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(v, (lds_void*)(to + R::V + i * 1024), 16, from, rows, 0, 0);
       }
       const uint32_t token = (lane & 15) * 4;  // four times over
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_void*)(to + R::SCALES), 4, token, at * 4, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_void*)(to + R::SCALES + 256), 4, token, at * 4, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_void*)(to + R::SCALES), 4, token, place * 4, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_void*)(to + R::SCALES + 256), 4, token, place * 4, 0, 0);
     }
   }
 };

@@ -278,6 +278,51 @@ struct hq_cache_io_args {
   int32_t y_bf16;
 };
 
+// Rotary positions as a kernel takes them.
+struct hq_turns {
+  const float* table;     // [count, 2, pairs] cosines and sines
+  const int32_t* pos;     // [rows, axes]
+  hq_stats* stats;
+  int32_t count, pairs, axes;
+  int32_t interleaved;
+  int32_t runs;           // the pairs that a lane holds have one axis
+  uint32_t axis[4];       // two bits a pair
+};
+struct hq_rope_table_args {
+  const double* freqs;
+  float* table;
+  int64_t count;
+  int32_t pairs;
+  float factor;
+};
+// Rows turned by their positions.
+#define HQ_ROPE_HEADS 4   // head vectors of a lane group
+struct hq_rope_args {
+  hq_turns turn;
+  const void* x;
+  void* y;
+  int64_t ldx, ldy;
+  uint32_t tiles;         // rows * groups
+  int32_t heads, groups;  // groups = ceil(heads / HQ_ROPE_HEADS)
+  hq_divisor by_groups;
+  int32_t x_bf16, y_bf16, transposed;
+};
+// Keys turned and cast into a cache with their values, queries turned beside them.
+#define HQ_APPEND_HEADS 2
+struct hq_cache_append_args {
+  hq_turns turn;
+  hq_cache_side side[2];
+  const int64_t* slots;
+  uint32_t tiles;         // rows * groups, of each side
+  int32_t heads, groups;  // groups = ceil(heads / HQ_APPEND_HEADS)
+  int32_t block_tokens;
+  hq_divisor by_groups, by_block;
+  int32_t x_bf16;
+  uint32_t side_groups;   // workgroups of a side
+  int32_t sides;
+  hq_rope_args q;         // tiles 0: none
+};
+
 // A sequence's first item of a cache attention, and how many it has.
 struct hq_cache_of {
   int32_t first, n;
@@ -311,7 +356,21 @@ struct hq_cache_attn_args {
   int32_t join;             // a sequence may have several chunks
   int32_t q_bf16, out_bf16;
   float qscale;             // softmax scale times log2(e) / 128
+  int32_t units;            // workgroups per chunk: the KV heads, of a tree times its row tiles
+  int32_t window, sinks;    // 0: every token
+  const int32_t* starts;    // of trees: batch + 1 places in the rows
+  const uint64_t* masks;    // of trees: ancestors, one per row
+  int32_t rows, max_rows;   // of trees: rows of the call, of a sequence at most
 };
+
+// Tokens of the longest sequence that an attention looks at, those of the groups of 16 that
+// the sinks' end and the window's start lie in among them.  `window` counts from the
+// sequence's last token (or from the first of a tree's rows, of which there are `rows`).
+static inline int64_t hq_cache_seen(int64_t max_tokens, int64_t window, int64_t sinks, int64_t rows) {
+  if (!window) return max_tokens;
+  const int64_t most = ((sinks + 15) & ~(int64_t)15) + window + rows + 15;
+  return most < max_tokens ? most : max_tokens;
+}
 
 // Workgroups of four waves (eight in calls that leave CUs idle); four waves' rings take 72
 // KB of LDS in the 8-bit formats, so two workgroups fit a CU and 512 the chip: one round of
@@ -351,6 +410,9 @@ static inline int64_t hq_cache_joins(int64_t batch, int64_t heads_kv) {
   return batch <= HQ_CACHE_UNPLANNED || batch < even ? batch : even;
 }
 
+// Rows of a tile of a tree attention, for so many of one KV head.
+static inline int32_t hq_tree_tile(int64_t rows) { return rows <= 16 ? 16 : 32; }
+
 // RMS norm fused with the 8-bit activation prep.
 struct hq_norm_args {
   const void* x;          // bf16 rows, stride ldx
@@ -372,6 +434,11 @@ struct hq_norm_args {
 int hq_launch_cache_write(const hq_cache_io_args& a, int format, int sides, void* stream);
 int hq_launch_cache_read(const hq_cache_io_args& a, int format, void* stream);
 int hq_launch_cache_attention(const hq_cache_attn_args& a, int format, void* stream);
+void hq_launch_cache_plan(const hq_cache_attn_args& a, void* stream);
+int hq_launch_cache_tree(const hq_cache_attn_args& a, int format, void* stream);
+int hq_launch_rope_table(const hq_rope_table_args& a, void* stream);
+int hq_launch_rope(const hq_rope_args& a, void* stream);
+int hq_launch_cache_append(const hq_cache_append_args& a, int format, void* stream);
 int hq_launch_norm_prep(const hq_norm_args& a, void* stream);
 int hq_launch_encode(const hq_plan_s* p, const hq_encode_args& a, const hq_rice_thr& t, int xt,
                      void* stream);

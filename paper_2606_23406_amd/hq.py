@@ -66,6 +66,12 @@ class CacheStruct(C.Structure):
                 ("reserved0", C.c_int32), ("stats", C.c_void_p)]
 
 
+class RotaryStruct(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_int64), ("dims", C.c_int32),
+                ("interleaved", C.c_int32), ("axes", C.c_int32), ("reserved0", C.c_int32),
+                ("axis", C.c_void_p), ("stats", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -137,6 +143,22 @@ def lib():
     L.hq_cache_attention.restype = i32
     L.hq_cache_attention.argtypes = [p, p, p, p, p, i32, i64, i32, f32, p, i32, p, p, i32, p,
                                      C.c_size_t, p]
+    L.hq_rope_table.restype = i32
+    L.hq_rope_table.argtypes = [p, i32, i64, f32, p, p]
+    L.hq_rope.restype = i32
+    L.hq_rope.argtypes = [p, p, i32, i64, i64, i32, p, i32, p, i32, i64, p]
+    L.hq_cache_append.restype = i32
+    L.hq_cache_append.argtypes = [p, p, i64, p, p, p, i64, p, i32, i64, p, p, p, p, i64, i32, p, i32, i64, p]
+    L.hq_cache_window_workspace_bytes.restype = C.c_size_t
+    L.hq_cache_window_workspace_bytes.argtypes = [p, i64, i32, i32, i32, i32]
+    L.hq_cache_window_attention.restype = i32
+    L.hq_cache_window_attention.argtypes = [p, p, p, p, p, i32, i64, i32, f32, p, i32, p, i32, i32, p, i32,
+                                            p, C.c_size_t, p]
+    L.hq_cache_tree_workspace_bytes.restype = C.c_size_t
+    L.hq_cache_tree_workspace_bytes.argtypes = [p, i64, i32, i32, i32, i32, i32]
+    L.hq_cache_tree_attention.restype = i32
+    L.hq_cache_tree_attention.argtypes = [p, p, p, p, p, i32, i64, i32, f32, p, p, i64, i32, p, i32, p, i32,
+                                          i32, p, i32, p, C.c_size_t, p]
     for fn in (L.hq_rmsnorm_act_prep, L.hq_rmsnorm_act_prep_fp8):
         fn.restype = i32
         fn.argtypes = [p, p, i64, p, i64, p, i32, f32, i64, p, i64, p, p, p]
@@ -646,6 +668,20 @@ def hq_cache_attention_workspace_bytes(k_cache: Cache, batch, heads_q, max_block
     return lib().hq_cache_attention_workspace_bytes(C.byref(k_cache.c), batch, heads_q, max_blocks)
 
 
+def _attention_caches(k, v, dev):
+    if k.device.index != dev or v.device.index != dev:
+        raise ValueError(f"caches on {k.device} and {v.device} in a call on cuda:{dev}")
+
+
+def _workspace(workspace, nbytes, dev, stream):
+    """The caller's workspace or a new one, as a tensor."""
+    if workspace is None:
+        return _empty((max(nbytes(), 16),), torch.uint8, dev, stream)
+    if not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError(f"workspace must be contiguous on cuda:{dev}")
+    return workspace
+
+
 def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor,
                        block_table: torch.Tensor, seq_lens: torch.Tensor, scale=None,
                        out_dtype=torch.float32, workspace=None, out=None, stream=None):
@@ -653,8 +689,7 @@ def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.
     the caches' blocks block_table int32 [batch, max_blocks], seq_lens int32
     [batch] tokens each.  Returns [batch, heads_q, 128]."""
     dev = torch.cuda.current_device()
-    if k.device.index != dev or v.device.index != dev:
-        raise ValueError(f"caches on {k.device} and {v.device} in a call on cuda:{dev}")
+    _attention_caches(k, v, dev)
     if q.dim() != 3 or block_table.dim() != 2:
         raise ValueError("q must be [batch, heads_q, 128] and block_table [batch, max_blocks]")
     batch, heads_q, max_blocks = q.shape[0], q.shape[1], block_table.shape[1]
@@ -665,17 +700,201 @@ def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.
     if out is None:
         out = _empty(shape, out_dtype, dev, stream)
     ot = out.dtype
-    if workspace is None:
-        nb = hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks)
-        workspace = _empty((max(nb, 16),), torch.uint8, dev, stream)
-    elif not workspace.is_contiguous() or workspace.get_device() != dev:
-        raise ValueError(f"workspace must be contiguous on cuda:{dev}")
+    workspace = _workspace(workspace, lambda: hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks),
+                           dev, stream)
     st = lib().hq_cache_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), qp,
                                   _dtype_code(qt), batch, heads_q,
                                   128 ** -0.5 if scale is None else scale, tp, max_blocks, lp,
                                   _dense(out, ot, shape, dev, "out"), _dtype_code(ot),
                                   workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
     _check("hq_cache_attention", st)
+    return out
+
+
+class Rope:
+    """Rotary positions (hq_rotary): `table` fp32 [positions, 2, dims / 2] (hq_rope_table
+    makes one), the axis of each pair (a list of dims / 2 numbers; None: one axis), pairs
+    (i, i + dims / 2) or, interleaved, (2 i, 2 i + 1)."""
+
+    def __init__(self, table: torch.Tensor, interleaved=False, axis=None, stats=True):
+        if table.dim() != 3 or table.shape[1] != 2 or table.dtype != torch.float32 or not table.is_contiguous() \
+                or not table.is_cuda:
+            raise ValueError("table must be a contiguous fp32 device tensor [positions, 2, dims / 2]")
+        pairs = table.shape[2]
+        axis = [0] * pairs if axis is None else [int(a) for a in axis]
+        if len(axis) != pairs or not all(0 <= a < 4 for a in axis):
+            raise ValueError(f"axis must be {pairs} numbers from 0 to 3")
+        self.table, self.axis, self.device = table, axis, table.device
+        self.axes = max(axis, default=0) + 1
+        self._axis = (C.c_uint8 * pairs)(*axis)
+        self.stats = torch.zeros(STATS_BYTES // 4, dtype=torch.int32, device=table.device) if stats else None
+        self.c = RotaryStruct(table.data_ptr(), table.shape[0], 2 * pairs, int(bool(interleaved)), self.axes, 0,
+                              C.addressof(self._axis), self.stats.data_ptr() if stats else None)
+
+    read_stats = Cache.read_stats
+    reset_stats = Cache.reset_stats
+
+
+def hq_rope_table(freqs: torch.Tensor, positions, factor=1.0, out=None, stream=None):
+    """hq_rope_table: cosines and sines of positions 0 .. positions - 1 at freqs (fp64
+    [pairs], radians a position), fp32 [positions, 2, pairs]."""
+    dev, pairs = torch.cuda.current_device(), freqs.shape[0]
+    shape = (positions, 2, pairs)
+    fp = _dense(freqs, torch.float64, (pairs,), dev, "freqs")
+    if out is None:
+        out = _empty(shape, torch.float32, dev, stream)
+    st = lib().hq_rope_table(fp, pairs, positions, factor, _dense(out, torch.float32, shape, dev, "out"),
+                             _stream_handle(stream))
+    _check("hq_rope_table", st)
+    return out
+
+
+def _positions(rope, positions, rows, dev):
+    if rope.device.index != dev:
+        raise ValueError(f"a table on {rope.device} in a call on cuda:{dev}")
+    if rope.axes == 1 and positions.dim() == 1:
+        return _dense(positions, torch.int32, (rows,), dev, "positions")
+    return _dense(positions, torch.int32, (rows, rope.axes), dev, "positions")
+
+
+def hq_rope(rope: Rope, x: torch.Tensor, positions: torch.Tensor, transposed=False, out_dtype=None, out=None,
+            stream=None):
+    """hq_rope: x [rows, heads * 128] (bf16 or fp32) turned by positions int32 [rows, axes]
+    (of one axis also [rows]); transposed: the gradient.  out may be x.  Without an out, rows
+    of padding (a negative first position) are zeros."""
+    dev, dt = torch.cuda.current_device(), x.dtype
+    shape = (x.shape[0], x.shape[1])
+    xp, ldx = _rows(x, dt, shape, dev, "x")
+    if shape[1] % 128:
+        raise ValueError(f"x must be [rows, heads * 128], not {list(shape)}")
+    pp = _positions(rope, positions, shape[0], dev)
+    if out is None:
+        out = _empty(shape, dt if out_dtype is None else out_dtype, dev, stream)
+        with torch.cuda.stream(stream):
+            out.zero_()
+    ot = out.dtype
+    op, ldo = _rows(out, ot, shape, dev, "out")
+    st = lib().hq_rope(C.byref(rope.c), xp, _dtype_code(dt), ldx, shape[0], shape[1] // 128, pp, int(bool(transposed)),
+                       op, _dtype_code(ot), ldo, _stream_handle(stream))
+    _check("hq_rope", st)
+    return out
+
+
+def hq_cache_append(k_plan: Plan, k: torch.Tensor, k_cache: Cache, v_plan, v, v_cache, slots: torch.Tensor,
+                    rope: Rope, positions: torch.Tensor, q=None, q_out=None, stream=None):
+    """hq_cache_append: hq_cache_write with k turned by positions int32 [rows, axes] on the
+    way; q [rows, heads_q * 128] turned into q_out, which may be q and is returned (a new
+    tensor of q's type without one, zeros in rows of padding)."""
+    dev, dt = torch.cuda.current_device(), k.dtype
+    shape = (k.shape[0], k_cache.heads * 128)
+    kp, ldk = _rows(k, dt, shape, dev, "k")
+    if k_cache.device.index != dev:
+        raise ValueError(f"a cache on {k_cache.device} in a call on cuda:{dev}")
+    if v is None:
+        if v_plan is not None or v_cache is not None:
+            raise ValueError("v_plan, v and v_cache come together")
+        vh = vp = vc = None
+        ldv = 0
+    else:
+        vp, ldv = _rows(v, dt, shape, dev, "v")
+        if v_cache.device.index != dev:
+            raise ValueError(f"a cache on {v_cache.device} in a call on cuda:{dev}")
+        vh, vc = v_plan.handle, C.byref(v_cache.c)
+    sp = _dense(slots, torch.int64, shape[:1], dev, "slots")
+    pp = _positions(rope, positions, shape[0], dev)
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q and q_out come together")
+        qp = op = None
+        ldq = ldo = heads_q = ot = 0
+    else:
+        qshape = (shape[0], q.shape[1])
+        if qshape[1] % 128:
+            raise ValueError(f"q must be [rows, heads_q * 128], not {list(q.shape)}")
+        qp, ldq = _rows(q, dt, qshape, dev, "q")
+        if q_out is None:
+            q_out = _empty(qshape, dt, dev, stream)
+            with torch.cuda.stream(stream):
+                q_out.zero_()
+        op, ldo = _rows(q_out, q_out.dtype, qshape, dev, "q_out")
+        heads_q, ot = qshape[1] // 128, _dtype_code(q_out.dtype)
+    st = lib().hq_cache_append(k_plan.handle, kp, ldk, C.byref(k_cache.c), vh, vp, ldv, vc, _dtype_code(dt), shape[0],
+                               sp, C.byref(rope.c), pp, qp, ldq, heads_q, op, ot, ldo, _stream_handle(stream))
+    _check("hq_cache_append", st)
+    return q_out
+
+
+def hq_cache_window_workspace_bytes(k_cache: Cache, batch, heads_q, max_blocks, window, sinks=0):
+    return lib().hq_cache_window_workspace_bytes(C.byref(k_cache.c), batch, heads_q, max_blocks, window, sinks)
+
+
+def hq_cache_window_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor,
+                              block_table: torch.Tensor, seq_lens: torch.Tensor, window, sinks=0, scale=None,
+                              out_dtype=torch.float32, workspace=None, out=None, stream=None):
+    """hq_cache_window_attention: hq_cache_attention over the last `window` tokens of each
+    sequence and its first `sinks`."""
+    dev = torch.cuda.current_device()
+    _attention_caches(k, v, dev)
+    if q.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("q must be [batch, heads_q, 128] and block_table [batch, max_blocks]")
+    batch, heads_q, max_blocks = q.shape[0], q.shape[1], block_table.shape[1]
+    shape, qt = (batch, heads_q, 128), q.dtype
+    qp = _dense(q, qt, shape, dev, "q")
+    tp = _dense(block_table, torch.int32, (batch, max_blocks), dev, "block_table")
+    lp = _dense(seq_lens, torch.int32, (batch,), dev, "seq_lens")
+    if out is None:
+        out = _empty(shape, out_dtype, dev, stream)
+    ot = out.dtype
+    workspace = _workspace(
+        workspace, lambda: hq_cache_window_workspace_bytes(k, batch, heads_q, max_blocks, window, sinks), dev, stream)
+    st = lib().hq_cache_window_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), qp,
+                                         _dtype_code(qt), batch, heads_q, 128 ** -0.5 if scale is None else scale, tp,
+                                         max_blocks, lp, window, sinks, _dense(out, ot, shape, dev, "out"),
+                                         _dtype_code(ot), workspace.data_ptr(), workspace.nbytes,
+                                         _stream_handle(stream))
+    _check("hq_cache_window_attention", st)
+    return out
+
+
+def hq_cache_tree_workspace_bytes(k_cache: Cache, batch, heads_q, max_blocks, max_tree, window=0, sinks=0):
+    return lib().hq_cache_tree_workspace_bytes(C.byref(k_cache.c), batch, heads_q, max_blocks, max_tree, window, sinks)
+
+
+def hq_cache_tree_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor, masks: torch.Tensor,
+                            starts: torch.Tensor, max_tree, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                            window=0, sinks=0, scale=None, out_dtype=torch.float32, workspace=None, out=None,
+                            stream=None):
+    """hq_cache_tree_attention: q [rows, heads_q, 128] (bf16 or fp32), the drafted tokens of all
+    sequences, sequence b's rows starts[b] .. starts[b + 1] - 1 (int32 [batch + 1], max_tree of
+    them at most), the last tokens of its seq_lens; masks int64 or uint64 [rows]: bit j for the
+    tree's token j.  Returns [rows, heads_q, 128]; without an out, rows of no sequence are zeros."""
+    dev = torch.cuda.current_device()
+    _attention_caches(k, v, dev)
+    if q.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("q must be [rows, heads_q, 128] and block_table [batch, max_blocks]")
+    rows, heads_q, (batch, max_blocks) = q.shape[0], q.shape[1], block_table.shape
+    shape, qt, mt = (rows, heads_q, 128), q.dtype, masks.dtype
+    if mt not in (torch.int64, torch.uint64):
+        raise ValueError(f"masks must be int64 or uint64, not {mt}")
+    qp = _dense(q, qt, shape, dev, "q")
+    mp = _dense(masks, mt, (rows,), dev, "masks")
+    sp = _dense(starts, torch.int32, (batch + 1,), dev, "starts")
+    tp = _dense(block_table, torch.int32, (batch, max_blocks), dev, "block_table")
+    lp = _dense(seq_lens, torch.int32, (batch,), dev, "seq_lens")
+    if out is None:
+        out = _empty(shape, out_dtype, dev, stream)
+        with torch.cuda.stream(stream):
+            out.zero_()
+    ot = out.dtype
+    workspace = _workspace(
+        workspace, lambda: hq_cache_tree_workspace_bytes(k, batch, heads_q, max_blocks, max_tree, window, sinks), dev,
+        stream)
+    st = lib().hq_cache_tree_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), qp, _dtype_code(qt),
+                                       rows, heads_q, 128 ** -0.5 if scale is None else scale, mp, sp, batch, max_tree,
+                                       tp, max_blocks, lp, window, sinks, _dense(out, ot, shape, dev, "out"),
+                                       _dtype_code(ot), workspace.data_ptr(), workspace.nbytes,
+                                       _stream_handle(stream))
+    _check("hq_cache_tree_attention", st)
     return out
 
 
@@ -737,6 +956,8 @@ EXPORTED = ["hq_plan", "hq_plan_destroy", "hq_plan_get_info", "hq_scan_bytes", "
             "hq_decode_fp8", "hq_act_prep_fp8", "hq_gemm_fp8_blockscaled",
             "hq_decode_mxfp4", "hq_act_prep_mxfp4", "hq_gemm_mxfp4_blockscaled",
             "hq_cache_write", "hq_cache_read", "hq_cache_attention_workspace_bytes",
-            "hq_cache_attention", "hq_rmsnorm_act_prep", "hq_rmsnorm_act_prep_fp8",
+            "hq_cache_attention", "hq_rope_table", "hq_rope", "hq_cache_append",
+            "hq_cache_window_workspace_bytes", "hq_cache_window_attention",
+            "hq_cache_tree_workspace_bytes", "hq_cache_tree_attention", "hq_rmsnorm_act_prep", "hq_rmsnorm_act_prep_fp8",
             "hq_rice_kstar",
             "hq_calibrated_snr", "hq_status_string"]
