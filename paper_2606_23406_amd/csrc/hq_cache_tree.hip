@@ -19,6 +19,8 @@
 // half as many products again and twice the instructions of cutting.)
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "hq_cache_device.h"
 #include "hq_lds.h"
 
@@ -34,12 +36,14 @@ __device__ __forceinline__ v4_t mfma_f16(const uint32_t* a, const uint32_t* b, v
                                                 __builtin_bit_cast(v8h16_t, (v4w_t){b[0], b[1], b[2], b[3]}), c, 0, 0, 0);
 }
 
-// Two values as the first and second fp16 terms, cut off; the first's remainder is exact.
+// Two values as the first and second fp16 terms, cut off.  The first's remainder is exact: an
+// fp16 half times -1 plus the fp32 value, one instruction.
 __device__ __forceinline__ void two_terms(float x, float y, uint32_t& hi, uint32_t& lo) {
-  const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
-  const auto l = __builtin_amdgcn_cvt_pkrtz(x - (float)h[0], y - (float)h[1]);
-  hi = __builtin_bit_cast(uint32_t, h);
-  lo = __builtin_bit_cast(uint32_t, l);
+  hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+  float a, b;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(a) : "v"(hi), "v"(x));
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(b) : "v"(hi), "v"(y));
+  lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
 }
 
 // Int8 codes c + 128 as bytes 0 and 2 of a word, which are the fp16 numbers (c + 128) 2^-24:
@@ -96,7 +100,6 @@ __device__ __forceinline__ void tokens_of(uint32_t w0, uint32_t w1, float f0, fl
 template <int FMT>
 struct TreeStep : CacheStep<FMT> {
   float kf[2], vf[2][4];
-  float lift[2][4];  // the power of two that moves a token's value scale below 2^15
 };
 
 // The power of two by which 2^(byte - 127) lies below the token's scale (a power of two or NaN).
@@ -139,11 +142,18 @@ __device__ __forceinline__ void tree_take(uint8_t* step, int lane, TreeStep<FMT>
   }
 }
 
-// What a lane knows of its column's row in each row tile.
+// What a row sees, in LDS: only steps that some row does not see some token of look at it.
 struct TreeRow {
   uint64_t mask;  // ancestors
   int32_t low;    // first token of its window
-  float f;        // 1 / the power of two that its query was moved by
+  // Bits of the 16 tokens from t on, those before the tree (below ctx) and the tree's.
+  __device__ __forceinline__ uint32_t sees(int32_t t, int32_t ctx, int32_t sinks) const {
+    auto below = [&](int32_t x) { return (1u << min(max(x - t, 0), 16)) - 1u; };
+    const uint32_t before = (below(sinks) | ~below(low)) & below(ctx);
+    if (t + 16 <= ctx) return before;
+    const int32_t d = t - ctx;  // below 64 where anybody sees a token
+    return before | (uint32_t)(d >= 0 ? mask >> (d & 63) : mask << -d);
+  }
 };
 
 // What a wave carries over its tokens per row tile; acc as in the one-token attention.
@@ -152,11 +162,118 @@ struct TreeState {
   v4_t acc[8];
 };
 
+// A row's reference lies above a score by the token's lift, the power of two (as its logarithm)
+// that leaves the weight times the value scale below 2^8.  It moves up only when a step's bound
+// passes it by 2^7, so that a product stays below 2^15 and the sums are seldom rescaled: with
+// 32 rows a wave some row has a new largest score in most steps.  Two terms hold 22 bits of a
+// product down to 2^-2, and 2^-24 below.
+constexpr float kSlack = 7.0f;
+
+// A scale below 2^-87 stays where it is: products with it are small, and sums of the weights
+// alone fit.
+__device__ __forceinline__ float lift_of(uint32_t scale_bits) {
+  return max((float)((int32_t)((scale_bits >> 23) & 0xFFu) - (126 + 8)), -94.0f);
+}
+
+// Whether one lift, the largest scale's, does for tokens whose scales lie between these: the
+// largest product of a row is then at least 2^1.
+__device__ __forceinline__ bool one_lift(uint32_t least, uint32_t most) { return (least >> 23) + 6 >= most >> 23; }
+
+// 32 tokens' scores in C's layout to their weights' terms pt (k index 4 h + r) and into the
+// rows' references and sums.  each: some row does not see some token, or the tokens' value scales
+// lie far apart: a lift for each; otherwise `lift` for all.  The sums are rescaled in one place:
+// with one for each of two ways the compiler keeps the accumulators twice.
+template <int RT>
+__device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)[2][4], const float (&vs)[2][4], bool each,
+                                             float lift, const int32_t (&live)[2], const int32_t (&at)[2], int32_t ctx,
+                                             int32_t sinks, const TreeRow* rows, const float (&back)[RT], int lane,
+                                             TreeState (&z)[RT], uint32_t (&pt)[RT][2][4]) {
+  const int g = lane >> 4;
+  float top[RT];
+  bool more = false;
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) c[i][h][r] *= ks[h][r];
+  }
+  if (each) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const TreeRow row = rows[16 * i + (lane & 15)];
+      top[i] = -__builtin_inff();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t sees = (row.sees(at[h], ctx, sinks) & (uint32_t)live[h]) >> (4 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          c[i][h][r] = (sees >> r) & 1 ? c[i][h][r] : -__builtin_inff();
+          top[i] = __builtin_fmaxf(top[i], __builtin_fmaf(c[i][h][r], back[i], lift_of(__float_as_uint(vs[h][r]))));
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      top[i] = c[i][0][0];
+#pragma unroll
+      for (int k = 1; k < 8; ++k) top[i] = __builtin_fmaxf(top[i], c[i][k >> 2][k & 3]);
+      top[i] = __builtin_fmaf(top[i], back[i], lift);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    top[i] = groups_max(top[i]);
+    more |= top[i] > z[i].m + kSlack;
+  }
+  if (__ballot(more)) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      // a row's own scores alone move it
+      const float mn = top[i] > z[i].m + kSlack ? top[i] : z[i].m;
+      const float alpha = __builtin_amdgcn_exp2f(z[i].m - (mn == -__builtin_inff() ? 0.0f : mn));
+      z[i].m = mn;
+      z[i].l *= alpha;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[i].acc[j] *= alpha;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const float ref = z[i].m == -__builtin_inff() ? 0.0f : z[i].m;  // nothing seen yet
+    float v[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[h][r] = vs[h][r];
+    if (each) {
+      // a scale that the row does not see may be a NaN
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[h][r] = c[i][h][r] == -__builtin_inff() ? 0.0f : vs[h][r];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float e[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i][h][r], back[i], -ref));
+        z[i].l += e[r];
+      }
+#pragma unroll
+      for (int r = 0; r < 4; r += 2)
+        two_terms(e[r] * v[h][r], e[r + 1] * v[h][r + 1], pt[i][0][2 * h + r / 2], pt[i][1][2 * h + r / 2]);
+    }
+  }
+}
+
 // One step: 32 tokens.  `each`: some row does not see some token.
 template <int FMT, int RT>
 __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const int32_t (&live)[2], const int32_t (&at)[2], bool each,
                                           int32_t ctx, int32_t sinks, const uint32_t (&q)[RT][2][4][4],
-                                          const TreeRow (&row)[RT], int lane, TreeState (&z)[RT]) {
+                                          const TreeRow* rows, const float (&back)[RT], int lane, TreeState (&z)[RT]) {
   const int g = lane >> 4;
   if (each) {
     // tokens that nobody sees: their value codes count as zeros (a stale code may be a NaN)
@@ -170,80 +287,40 @@ __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const int32_t (&li
           cur.ks[h][r] = cur.vs[h][r] = 0.0f;
         }
   }
+  float most = cur.vs[0][0], least = most;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      // a scale below 2^-80 stays where it is: weights times it are small, sums of the weights alone fit
-      cur.lift[h][r] = max((float)((int32_t)((__float_as_uint(cur.vs[h][r]) >> 23) & 0xFFu) - (126 + 15)), -94.0f);
+  for (int i = 1; i < 8; ++i) {
+    most = __builtin_fmaxf(most, cur.vs[i >> 2][i & 3]);
+    least = __builtin_fminf(least, cur.vs[i >> 2][i & 3]);
+  }
+  const uint32_t hi = readfirst(__float_as_uint(groups_max(most))), lo = readfirst(__float_as_uint(-groups_max(-least)));
+  each |= !one_lift(lo, hi);
   v4_t c[RT][2];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int h = 0; h < 2; ++h) c[i][h] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int s = 0; s < 4; ++s)
+  for (int s = 0; s < 4; ++s) {
+    uint32_t a[2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32_t a[4];
       if constexpr (FMT == kMx) {
-        dims_of<FMT>(cur.k[h][s], cur.kf[h], a);
+        dims_of<FMT>(cur.k[h][s], cur.kf[h], a[h]);
       } else {
-        dims_of<FMT>(cur.k[h][2 * s], 1.0f, a);
-        dims_of<FMT>(cur.k[h][2 * s + 1], 1.0f, a + 2);
+        dims_of<FMT>(cur.k[h][2 * s], 1.0f, a[h]);
+        dims_of<FMT>(cur.k[h][2 * s + 1], 1.0f, a[h] + 2);
       }
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int t = 1; t >= 0; --t) c[i][h] = mfma_f16(a, q[i][t][s], c[i][h]);
     }
-  uint32_t pt[RT][2][4];  // the weights' terms: k index 4 h + r
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    TreeState& y = z[i];
-    bool gone[2][4];
-    float x[2][4], top = -__builtin_inff();
+    for (int t = 1; t >= 0; --t)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[h][r] = c[i][h][r] * cur.ks[h][r];
-        float u = __builtin_fmaf(x[h][r], row[i].f, cur.lift[h][r]);
-        if (each) {
-          const int32_t t = at[h] + 4 * g + r, d = t - ctx;
-          const bool sees = d < 0 ? t >= row[i].low || t < sinks : (bool)((row[i].mask >> (d & 63)) & 1);
-          gone[h][r] = !sees || !((live[h] >> (4 * g + r)) & 1);
-          u = gone[h][r] ? -__builtin_inff() : u;
-        }
-        top = __builtin_fmaxf(top, u);
-      }
-    top = groups_max(top);
-    if (__ballot(top > y.m)) {
-      const float mn = __builtin_fmaxf(y.m, top);
-      const float alpha = __builtin_amdgcn_exp2f(y.m - (mn == -__builtin_inff() ? 0.0f : mn));
-      y.m = mn;
-      y.l *= alpha;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y.acc[j] *= alpha;
-    }
-    const float ref = y.m == -__builtin_inff() ? 0.0f : y.m;  // nothing seen yet
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float w[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[h][r], row[i].f, -ref));
-        w[r] = e * cur.vs[h][r];
-        if (each) {
-          e = gone[h][r] ? 0.0f : e;
-          w[r] = gone[h][r] ? 0.0f : w[r];
-        }
-        y.l += e;
-      }
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) two_terms(w[r], w[r + 1], pt[i][0][2 * h + r / 2], pt[i][1][2 * h + r / 2]);
-    }
+        for (int i = 0; i < RT; ++i) c[i][h] = mfma_f16(a[h], q[i][t][s], c[i][h]);
   }
+  uint32_t pt[RT][2][4];
+  tree_weights<RT>(c, cur.ks, cur.vs, each, lift_of(hi), live, at, ctx, sinks, rows, back, lane, z, pt);
   // value codes: per word the tokens' pairs of each of its dims
 #pragma unroll
   for (int w = 0; w < CacheStep<FMT>::VW; ++w) {
@@ -276,6 +353,57 @@ struct TreePlace {
   }
 };
 
+__device__ __forceinline__ TreeRow tree_row(const hq_cache_attn_args& A, int32_t row, int32_t rows, int32_t from, int32_t ctx) {
+  const TreePlace p(A, row);
+  uint64_t mask = p.i < rows ? A.masks[from + p.i] : 0;
+  if (rows < 64) mask &= (1ull << rows) - 1;
+  return {mask, A.window ? ctx + (int32_t)__popcll(mask) - A.window : 0};
+}
+
+// 8 values a lane of a query in the cache's coordinates, moved by a power of two so that the
+// largest of its 128 lies in [2^14, 2^15), as two terms; returns 1 / that power.
+__device__ __forceinline__ float tree_query(const Raw8& raw, bool bf16, uint4 signs, float scale, int lane, uint4& hi, uint4& lo) {
+  float v[8], am = 0.0f;
+  expand8(raw, bf16, v);
+  flip8(v, signs);
+  const XSigns sg(lane);
+  fwht128(v, sg);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    v[k] *= scale;
+    am = __builtin_fmaxf(am, __builtin_fabsf(v[k]));
+  }
+  am = __builtin_fmaxf(am, dpp_xor<1>(am));
+  am = __builtin_fmaxf(am, dpp_xor<2>(am));
+  am = __builtin_fmaxf(am, swz_xor4(am));
+  am = __builtin_fmaxf(am, dpp_xor<8>(am));
+  // its exponent, between -100 and 127
+  const int32_t e = min(max((int32_t)(__float_as_uint(am) >> 23), 27), 254) - 127;
+  const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+  two_terms(v[0] * up, v[1] * up, hi.x, lo.x);
+  two_terms(v[2] * up, v[3] * up, hi.y, lo.y);
+  two_terms(v[4] * up, v[5] * up, hi.z, lo.z);
+  two_terms(v[6] * up, v[7] * up, hi.w, lo.w);
+  return __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+}
+
+// A row's sum of a chunk, 16 lanes: to the join, or finished.
+__device__ __forceinline__ void tree_result(const hq_cache_attn_args& A, bool join, int64_t part, float M, float L, float* v,
+                                            const TreePlace& p, int32_t rows, int32_t from, int32_t head, int lane) {
+  const int c0 = (lane & 15) * 8;
+  if (!join) {
+    cache_finish(A, L, v, head, lane);
+    if (p.i < rows)
+      store8(A.out, ((int64_t)(from + p.i) * A.heads_q + (int64_t)head * A.group + p.head) * HQ_TILE + c0, A.out_bf16, v);
+  } else if (p.i < rows) {
+    store8(A.part_acc, part * HQ_TILE + c0, false, v);
+    if (c0 == 0) {
+      A.part_m[part] = M;
+      A.part_l[part] = L;
+    }
+  }
+}
+
 template <int FMT, int RT>
 constexpr int tree_wave_bytes() {
   constexpr int out = 16 * RT * kOPitch * (int)sizeof(float);
@@ -289,6 +417,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   constexpr int WAVES = HQ_CACHE_WAVES, ROWS = 16 * RT, WAVE = tree_wave_bytes<FMT, RT>();
   extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];  // a wave's ring after the other
   __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS], s_f[ROWS];
+  __shared__ TreeRow s_row[ROWS];
   // term t of row tile i lies in the second step of wave 2 i + t's ring until that is first
   // loaded, a wave's sums in its own ring at the end
   static_assert(16 * kQPitch * sizeof(uint16_t) <= R::STEP && 2 * RT <= WAVES, "");
@@ -326,14 +455,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
       qraw[i] = load_raw8(A.q, ((int64_t)(from + p.i) * A.heads_q + (int64_t)head * A.group + p.head) * HQ_TILE + c0, A.q_bf16);
   }
   const int32_t ctx = it.span.len - rows;
-  TreeRow row[RT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const TreePlace p(A, tile * ROWS + 16 * i + n);
-    const uint64_t mask = p.i < rows ? A.masks[from + p.i] : 0;
-    row[i].mask = rows < 64 ? mask & ((1ull << rows) - 1) : mask;
-    row[i].low = A.window ? ctx + __popcll(row[i].mask) - A.window : 0;
-  }
+  if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
   w.got();
   w.template enter<FMT, true>(A, lane);
   uint8_t* ring = s_ring + wave * WAVE;
@@ -342,37 +464,17 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
-    float qv[8];
-    expand8(qraw[i], A.q_bf16, qv);
-    flip8(qv, qd);
-    const XSigns sg(lane);
-    fwht128(qv, sg);
-    float am = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      qv[k] *= A.qscale;
-      am = __builtin_fmaxf(am, __builtin_fabsf(qv[k]));
-    }
-    am = __builtin_fmaxf(am, dpp_xor<1>(am));
-    am = __builtin_fmaxf(am, dpp_xor<2>(am));
-    am = __builtin_fmaxf(am, swz_xor4(am));
-    am = __builtin_fmaxf(am, dpp_xor<8>(am));
-    // its exponent, between -100 and 127
-    const int32_t e = min(max((int32_t)(__float_as_uint(am) >> 23), 27), 254) - 127;
-    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
     uint4 hi, lo;
-    two_terms(qv[0] * up, qv[1] * up, hi.x, lo.x);
-    two_terms(qv[2] * up, qv[3] * up, hi.y, lo.y);
-    two_terms(qv[4] * up, qv[5] * up, hi.z, lo.z);
-    two_terms(qv[6] * up, qv[7] * up, hi.w, lo.w);
+    const float f = tree_query(qraw[i], A.q_bf16, qd, A.qscale, lane, hi, lo);
     *(uint4*)(q_row(16 * i + grp, 0) + c0) = hi;
     *(uint4*)(q_row(16 * i + grp, 1) + c0) = lo;
-    if (n == 0) s_f[16 * i + grp] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+    if (n == 0) s_f[16 * i + grp] = f;
   }
   __syncthreads();
   // step s of the contraction takes dims 32 (l / 16) + 8 s + j in lane l (the codes
   // that the lane's one run of 32 holds)
   uint32_t q[RT][2][4][4];
+  float back[RT];  // 1 / the power of two that a row was moved by
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
 #pragma unroll
@@ -382,7 +484,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
         const uint4 x = *(const uint4*)(q_row(16 * i + n, t) + 32 * g + 8 * s);
         q[i][t][s][0] = x.x; q[i][t][s][1] = x.y; q[i][t][s][2] = x.z; q[i][t][s][3] = x.w;
       }
-    row[i].f = s_f[16 * i + n];
+    back[i] = s_f[16 * i + n];
   }
   __syncthreads();  // the queries' place is loaded over
 
@@ -421,7 +523,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       each |= here_at[h] + 16 > ctx || (here_at[h] < open && here_at[h] + 16 > A.sinks);
-    tree_step<FMT, RT>(cur, here, here_at, each, ctx, A.sinks, q, row, lane, z);
+    tree_step<FMT, RT>(cur, here, here_at, each, ctx, A.sinks, q, s_row, back, lane, z);
   }
   // ---- the waves' sums under one reference, one row per 16 lanes
 #pragma unroll
@@ -454,19 +556,395 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(f, o_row(x, at_row)[c0 + k], v[k]);
     }
-    if (it.n > 1) {
-      if (p.i >= rows) continue;
-      const int64_t part = (int64_t)blockIdx.x * ROWS + at_row;
-      store8(A.part_acc, part * HQ_TILE + c0, false, v);
-      if (n == 0) {
-        A.part_m[part] = M;
-        A.part_l[part] = L;
-      }
-      continue;
+    tree_result(A, it.n > 1, (int64_t)blockIdx.x * ROWS + at_row, M, L, v, p, rows, from, head, lane);
+  }
+}
+
+// ---- many rows
+// Trees of more than 32 rows of a KV head: the codes are turned into fp16 once per workgroup
+// and not once per wave.  A workgroup goes through its tokens in tiles of 64, two steps of 32;
+// two waves turn a step's keys each, two its values, into LDS in the order that the products'
+// operands are read in, a tile ahead of the products; the codes of the tile after it are on
+// their way in registers meanwhile.  Each wave has 32 rows: of a tile of 128 rows each wave
+// takes both steps, of one of 64 two waves share the rows and take a step each.
+constexpr int kTreeTile = 64;
+template <int FMT>
+struct TreeTile {
+  // keys: [step][half][contraction step][lane] 16 bytes; values: [step][dim in its group of 8]
+  // [lane] 16 bytes
+  static constexpr int V = kTreeTile * HQ_TILE * 2, KS = 2 * V, VS = KS + 4 * kTreeTile, SEEN = VS + 4 * kTreeTile;
+  static constexpr int BYTES = SEEN + 2 * 16 + 480;  // a multiple of 1 KB
+};
+
+// What a wave of the tile's loads holds: a step's keys or values of 32 tokens.
+template <int FMT>
+struct TreeLoads {
+  static constexpr int KW = FMT == kMx ? 4 : 8, VW = FMT == kMx ? 1 : 2;
+  uint32_t w[2][8];    // keys: half, words of lane's 32 codes (token lane % 16, run lane / 16);
+                       // values: half, VW words of each of four tokens (4 (lane / 16) + r, dims 8 (lane % 16) ..)
+  uint32_t scale[2];   // keys: half's token lane % 16; values: [0] token lane % 32
+  int32_t live[2];     // bits of tokens that anybody sees
+};
+
+// A wave's way over its halves of a workgroup's tiles.
+struct TreeWay {
+  const int32_t* table;
+  CacheSpan span;
+  int32_t gap, jump, head, last;  // last: the sequence's last block
+  int32_t id[2];                  // block ids of the next tile's halves, on their way
+  __device__ __forceinline__ int32_t real(int32_t t) const { return t < jump ? t : t + gap; }
+  __device__ __forceinline__ void ask(const hq_cache_attn_args& A, int32_t t) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) id[h] = table[min((int32_t)A.by_block.of((uint32_t)real(t + 16 * h)), last)];
+  }
+  // Starts the loads of the 32 tokens from t on, whose ids have been asked for, and asks for
+  // those of the tile behind.
+  template <int FMT, bool KEYS>
+  __device__ __forceinline__ void load(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, TreeLoads<FMT>& x) {
+    constexpr int RB = row_bytes<FMT>();
+    const uint8_t* codes = KEYS ? A.k_codes : A.v_codes;
+    const uint32_t* scales = (const uint32_t*)(KEYS ? A.k_scales : A.v_scales);
+    const int n = lane & 15, g = lane >> 4;
+    int64_t row[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t at = real(t + 16 * h), blk = (int32_t)readfirst((uint32_t)id[h]);
+      const bool in = t + 16 * h < end, bad = (uint32_t)blk >= (uint32_t)A.blocks;
+      if (KEYS && in && bad && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
+      x.live[h] = in && !bad ? (int32_t)span.bits(at) : 0;
+      // a half that nobody sees: the cache's first tokens
+      const int32_t off = at - (int32_t)A.by_block.of((uint32_t)at) * A.block_tokens;
+      row[h] = x.live[h] ? ((int64_t)blk * A.heads_kv + head) * A.block_tokens + off : 0;
     }
-    cache_finish(A, L, v, head, lane);
+    ask(A, t + kTreeTile);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* from = codes + row[h] * RB;
+      if constexpr (KEYS) {
+#pragma unroll
+        for (int i = 0; i < TreeLoads<FMT>::KW; i += 4) {
+          const uint4 v = *(const uint4*)(from + n * RB + g * (RB / 4) + 4 * i);
+          x.w[h][i] = v.x; x.w[h][i + 1] = v.y; x.w[h][i + 2] = v.z; x.w[h][i + 3] = v.w;
+        }
+        x.scale[h] = scales[row[h] + n];
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint8_t* at = from + (4 * g + r) * RB + n * (RB / 16);
+          if constexpr (FMT == kMx) {
+            x.w[h][r] = *(const uint32_t*)at;
+          } else {
+            const uint2 v = *(const uint2*)at;
+            x.w[h][2 * r] = v.x; x.w[h][2 * r + 1] = v.y;
+          }
+        }
+      }
+    }
+    if constexpr (!KEYS) x.scale[0] = x.scale[1] = scales[(lane & 16 ? row[1] : row[0]) + n];
+  }
+};
+
+__device__ __forceinline__ uint32_t largest_byte(uint32_t w) {
+  return max(max(w & 0xFFu, (w >> 8) & 0xFFu), max((w >> 16) & 0xFFu, w >> 24));
+}
+// Bits of a token's scale: MXFP4's is its largest block's.
+template <int FMT>
+__device__ __forceinline__ uint32_t token_scale(uint32_t w) {
+  if constexpr (FMT == kMx) {
+    const uint32_t x = largest_byte(w);
+    return x == 255u ? 0x7FC00000u : x << 23;
+  } else {
+    return __float_as_uint(__uint_as_float(w) * kCodeUnit<FMT>);
+  }
+}
+
+// The largest of lanes 0 .. 31's values, which lanes 32 on have too.
+__device__ __forceinline__ float half_wave_max(float x) {
+  x = __builtin_fmaxf(x, dpp_xor<1>(x));
+  x = __builtin_fmaxf(x, dpp_xor<2>(x));
+  x = __builtin_fmaxf(x, swz_xor4(x));
+  x = __builtin_fmaxf(x, dpp_xor<8>(x));
+  const v2u_t a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// A step's keys as fp16 into a tile.
+template <int FMT>
+__device__ __forceinline__ void turn_keys(const TreeLoads<FMT>& x, uint8_t* tile, int step, int lane) {
+  const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t scale = token_scale<FMT>(x.scale[h]);
+    const float f = FMT == kMx ? below_scale((x.scale[h] >> (8 * g)) & 0xFFu, __uint_as_float(scale)) : 1.0f;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      uint32_t o[4];
+      if constexpr (FMT == kMx) {
+        dims_of<FMT>(x.w[h][s], f, o);
+      } else {
+        dims_of<FMT>(x.w[h][2 * s], 1.0f, o);
+        dims_of<FMT>(x.w[h][2 * s + 1], 1.0f, o + 2);
+      }
+      *(uint4*)(tile + (((step * 2 + h) * 4 + s) * 64 + lane) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+    if (g == 0) *(uint32_t*)(tile + TreeTile<FMT>::KS + (step * 32 + 16 * h + n) * 4) = scale;
+  }
+}
+
+// A step's values as fp16 into a tile, their scales, and what the products go by: the largest
+// scale's lift, the tokens that anybody sees, whether one lift does.
+template <int FMT>
+__device__ __forceinline__ void turn_values(TreeLoads<FMT>& x, uint8_t* tile, int step, int lane) {
+  constexpr int VW = TreeLoads<FMT>::VW, D = 8 / VW;
+  const int n = lane & 15, g = lane >> 4;
+  uint32_t scale = token_scale<FMT>(x.scale[0]);
+  float f[2][4];
+  if constexpr (FMT == kMx) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int from = 16 * h + 4 * g + r;  // the lane that has the token's
+        const uint32_t w = (uint32_t)__shfl((int)x.scale[0], from, 64), of = (uint32_t)__shfl((int)scale, from, 64);
+        f[h][r] = below_scale((w >> (8 * (n >> 2))) & 0xFFu, __uint_as_float(of));
+      }
+  }
+  if ((x.live[0] & x.live[1]) != 0xFFFF) {
+    // tokens that nobody sees count as zeros (a stale code or scale may be a NaN)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (!((x.live[h] >> (4 * g + r)) & 1)) {
+#pragma unroll
+          for (int i = 0; i < VW; ++i) x.w[h][VW * r + i] = 0u;
+        }
+    if (!(((lane & 16 ? x.live[1] : x.live[0]) >> n) & 1)) scale = 0u;
+  }
+#pragma unroll
+  for (int w = 0; w < VW; ++w) {
+    uint32_t vf[D][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        uint32_t o[D];
+        tokens_of<FMT>(x.w[h][VW * r + w], x.w[h][VW * (r + 1) + w], FMT == kMx ? f[h][r] : 1.0f, FMT == kMx ? f[h][r + 1] : 1.0f, o);
+#pragma unroll
+        for (int d = 0; d < D; ++d) vf[d][2 * h + r / 2] = o[d];
+      }
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+      *(uint4*)(tile + TreeTile<FMT>::V + ((step * 8 + D * w + d) * 64 + lane) * 16) =
+          make_uint4(vf[d][0], vf[d][1], vf[d][2], vf[d][3]);
+  }
+  if (lane < 32) *(uint32_t*)(tile + TreeTile<FMT>::VS + (step * 32 + lane) * 4) = scale;
+  const float most = half_wave_max(__uint_as_float(scale)), least = -half_wave_max(-__uint_as_float(scale));
+  if (lane == 0)
+    *(uint4*)(tile + TreeTile<FMT>::SEEN + step * 16) =
+        make_uint4(__float_as_uint(lift_of(__float_as_uint(most))), (uint32_t)(x.live[0] | x.live[1] << 16),
+                   one_lift(__float_as_uint(least), __float_as_uint(most)), 0u);
+}
+
+// Everything that the workgroup wrote to LDS is there for all of it; loads from memory stay on their way.
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int FMT, int ROWS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_wide_kernel(hq_cache_attn_args A) {
+  using T = TreeTile<FMT>;
+  constexpr int RT = 2, RW = ROWS / 32, TW = 4 / RW;  // waves along the rows, along the tokens
+  extern __shared__ __attribute__((aligned(16))) uint8_t s_tile[];  // two tiles
+  __shared__ float s_m[TW][ROWS], s_l[TW][ROWS], s_f[ROWS];
+  __shared__ TreeRow s_row[ROWS];
+  static_assert(TW * ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
+  auto o_row = [&](int w, int row) { return (float*)s_tile + (w * ROWS + row) * kOPitch; };
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4, grp = tid >> 4;
+  const int wave = (int)readfirst((uint32_t)(tid >> 6)), rw = wave % RW, tw = wave / RW;
+  const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.units);
+  const int32_t unit = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.units);
+  const int32_t tile = unit / A.heads_kv, head = unit - tile * A.heads_kv, c0 = n * 8;
+  const CacheItem it = cache_item<kTree>(A, j, lane, blockIdx.x == 0 && wave == 0);
+  if (it.b < 0) return;
+  // what the join goes by
+  if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && unit == 0 && tid == 0)
+    A.parts[it.b] = {it.first, it.n};
+  const int32_t rows = it.span.rows, seen = it.span.seen();
+  if (tile * ROWS >= rows * A.group) return;  // none of this sequence's, or it has none at all
+  const int32_t from = A.starts[it.b];
+  const int32_t begin = (int32_t)((j - it.first) * it.chunk), end = begin + min(it.chunk, seen - begin);
+  TreeWay way;
+  way.table = A.table + (int64_t)it.b * A.max_blocks;
+  way.span = it.span;
+  way.gap = it.span.gap();
+  way.jump = way.gap ? it.span.turn() : 0x7FFFFFFF;
+  way.head = head;
+  way.last = (it.span.len - 1) / A.block_tokens;
+  TreeLoads<FMT> loads;
+  // waves 0 and 1 take the steps' keys, 2 and 3 their values
+  const int mine = wave & 1;
+  way.ask(A, begin + 32 * mine);
+  if (wave < 2)
+    way.template load<FMT, true>(A, begin + 32 * mine, end, lane, loads);
+  else
+    way.template load<FMT, false>(A, begin + 32 * mine, end, lane, loads);
+  const int32_t ctx = it.span.len - rows;
+  if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
+  // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each,
+  // [row tile][term][contraction step][lane] 16 bytes
+  const uint4 qd = sign_words(A.k_dsign16, head * HQ_TILE + c0);
+#pragma unroll 2
+  for (int i = 0; i < ROWS / 16; ++i) {
+    const TreePlace p(A, tile * ROWS + 16 * i + grp);
+    Raw8 raw = {};
     if (p.i < rows)
-      store8(A.out, ((int64_t)(from + p.i) * A.heads_q + (int64_t)head * A.group + p.head) * HQ_TILE + c0, A.out_bf16, v);
+      raw = load_raw8(A.q, ((int64_t)(from + p.i) * A.heads_q + (int64_t)head * A.group + p.head) * HQ_TILE + c0, A.q_bf16);
+    uint4 hi, lo;
+    const float f = tree_query(raw, A.q_bf16, qd, A.qscale, lane, hi, lo);
+    uint8_t* to = s_tile + i * 8192 + (n & 3) * 1024 + ((n >> 2) * 16 + grp) * 16;
+    *(uint4*)to = hi;
+    *(uint4*)(to + 4096) = lo;
+    if (n == 0) s_f[16 * i + grp] = f;
+  }
+  __syncthreads();
+  uint32_t q[RT][2][4][4];
+  float back[RT];  // 1 / the power of two that a row was moved by
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const uint4 x = *(const uint4*)(s_tile + (((2 * rw + i) * 2 + t) * 4 + s) * 1024 + lane * 16);
+        q[i][t][s][0] = x.x; q[i][t][s][1] = x.y; q[i][t][s][2] = x.z; q[i][t][s][3] = x.w;
+      }
+    back[i] = s_f[32 * rw + 16 * i + n];
+  }
+  __syncthreads();  // the queries' place is written over
+  TreeState z[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    z[i].m = -__builtin_inff();
+    z[i].l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[i].acc[k] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // from here on every row's window has begun
+  const int32_t open = A.window ? ctx + rows - A.window : 0;
+  const bool idle = tile * ROWS + 32 * rw >= rows * A.group;  // the wave has no rows
+  // the whole loop once for each side of the loads: with a choice in it their registers are
+  // moved, and waited for, in every tile
+  auto run = [&](auto side) {
+    constexpr bool KEYS = decltype(side)::value;
+    auto load = [&](int32_t t) { way.template load<FMT, KEYS>(A, t + 32 * mine, end, lane, loads); };
+    auto turn = [&](uint8_t* to) {
+      if constexpr (KEYS)
+        turn_keys<FMT>(loads, to, mine, lane);
+      else
+        turn_values<FMT>(loads, to, mine, lane);
+    };
+    turn(s_tile);
+    if (begin + kTreeTile < end) load(begin + kTreeTile);
+    tile_barrier();
+    uint8_t* at_tile = s_tile;
+    uint8_t* to_tile = s_tile + T::BYTES;
+    for (int32_t t = begin; t < end; t += kTreeTile) {
+      if (t + kTreeTile < end) {
+        turn(to_tile);
+        if (t + 2 * kTreeTile < end) load(t + 2 * kTreeTile);
+      }
+#pragma unroll 1
+      for (int step = TW == 1 ? 0 : tw; step < (TW == 1 ? 2 : tw + 1); ++step) {
+        const uint4 about = *(const uint4*)(at_tile + T::SEEN + step * 16);
+        const uint32_t all = readfirst(about.y);
+        const int32_t live[2] = {(int32_t)(all & 0xFFFFu), (int32_t)(all >> 16)};
+        if (all == 0 || idle) continue;
+        const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
+        bool each = all != 0xFFFFFFFFu || readfirst(about.z) == 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
+        v4_t c[RT][2];
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) c[i][h] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          uint4 a[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) a[h] = *(const uint4*)(at_tile + (((step * 2 + h) * 4 + s) * 64 + lane) * 16);
+#pragma unroll
+          for (int u = 1; u >= 0; --u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int i = 0; i < RT; ++i) c[i][h] = mfma_f16((const uint32_t*)&a[h], q[i][u][s], c[i][h]);
+        }
+        float ks[2][4], vs[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 x = *(const float4*)(at_tile + T::KS + (step * 32 + 16 * h + 4 * g) * 4);
+          const float4 y = *(const float4*)(at_tile + T::VS + (step * 32 + 16 * h + 4 * g) * 4);
+          ks[h][0] = x.x; ks[h][1] = x.y; ks[h][2] = x.z; ks[h][3] = x.w;
+          vs[h][0] = y.x; vs[h][1] = y.y; vs[h][2] = y.z; vs[h][3] = y.w;
+        }
+        uint32_t pt[RT][2][4];
+        tree_weights<RT>(c, ks, vs, each, __uint_as_float(readfirst(about.x)), live, at, ctx, A.sinks, s_row + 32 * rw, back, lane, z, pt);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint4 v = *(const uint4*)(at_tile + T::V + ((step * 8 + k) * 64 + lane) * 16);
+#pragma unroll
+          for (int u = 1; u >= 0; --u)
+#pragma unroll
+            for (int i = 0; i < RT; ++i) z[i].acc[k] = mfma_f16((const uint32_t*)&v, pt[i][u], z[i].acc[k]);
+        }
+      }
+      tile_barrier();
+      uint8_t* const x = at_tile;
+      at_tile = to_tile;
+      to_tile = x;
+    }
+  };
+  if (wave < 2)
+    run(std::true_type());
+  else
+    run(std::false_type());
+  // ---- the waves' sums under one reference, one row per 16 lanes
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    z[i].l = groups_sum(z[i].l);
+    const int at_row = 32 * rw + 16 * i + n;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* o = o_row(tw, at_row) + (4 * g + r) * 8;
+      *(float4*)o = make_float4(z[i].acc[0][r], z[i].acc[1][r], z[i].acc[2][r], z[i].acc[3][r]);
+      *(float4*)(o + 4) = make_float4(z[i].acc[4][r], z[i].acc[5][r], z[i].acc[6][r], z[i].acc[7][r]);
+    }
+    if (g == 0) {
+      s_m[tw][at_row] = z[i].m;
+      s_l[tw][at_row] = z[i].l;
+    }
+  }
+  __syncthreads();
+#pragma unroll 2
+  for (int i = 0; i < ROWS / 16; ++i) {
+    const int at_row = 16 * i + grp;
+    const TreePlace p(A, tile * ROWS + at_row);
+    float M = s_m[0][at_row], L = 0.0f, v[8] = {};
+#pragma unroll
+    for (int x = 1; x < TW; ++x) M = __builtin_fmaxf(M, s_m[x][at_row]);
+    const float ref = M == -__builtin_inff() ? 0.0f : M;
+#pragma unroll
+    for (int x = 0; x < TW; ++x) {
+      const float f = __builtin_amdgcn_exp2f(s_m[x][at_row] - ref);
+      L = __builtin_fmaf(f, s_l[x][at_row], L);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(f, o_row(x, at_row)[c0 + k], v[k]);
+    }
+    tree_result(A, it.n > 1, (int64_t)blockIdx.x * ROWS + at_row, M, L, v, p, rows, from, head, lane);
   }
 }
 
@@ -506,7 +984,7 @@ __global__ __launch_bounds__(256) void hq_cache_tree_join_kernel(hq_cache_attn_a
 }
 
 template <int FMT, int RT>
-int launch_tree(const hq_cache_attn_args& a, hipStream_t st) {
+int launch_narrow(const hq_cache_attn_args& a, hipStream_t st) {
   static hq_lds_granted granted;
   constexpr size_t lds = (size_t)HQ_CACHE_WAVES * tree_wave_bytes<FMT, RT>();
   if (const int e = hq_allow_lds((const void*)hq_cache_tree_kernel<FMT, RT>, lds, granted)) return e;
@@ -514,9 +992,23 @@ int launch_tree(const hq_cache_attn_args& a, hipStream_t st) {
   return 0;
 }
 
+template <int FMT, int ROWS>
+int launch_wide(const hq_cache_attn_args& a, hipStream_t st) {
+  static hq_lds_granted granted;
+  constexpr size_t lds = 2 * TreeTile<FMT>::BYTES;
+  if (const int e = hq_allow_lds((const void*)hq_cache_tree_wide_kernel<FMT, ROWS>, lds, granted)) return e;
+  hipLaunchKernelGGL((hq_cache_tree_wide_kernel<FMT, ROWS>), dim3((uint32_t)(a.items * a.units)), dim3(256), lds, st, a);
+  return 0;
+}
+
 template <int FMT>
 int launch_tree(const hq_cache_attn_args& a, hipStream_t st) {
-  return hq_tree_tile(a.max_rows * a.group) == 16 ? launch_tree<FMT, 1>(a, st) : launch_tree<FMT, 2>(a, st);
+  switch (hq_tree_tile((int64_t)a.max_rows * a.group)) {
+    case 16: return launch_narrow<FMT, 1>(a, st);
+    case 32: return launch_narrow<FMT, 2>(a, st);
+    case 64: return launch_wide<FMT, 64>(a, st);
+    default: return launch_wide<FMT, 128>(a, st);
+  }
 }
 
 }  // namespace

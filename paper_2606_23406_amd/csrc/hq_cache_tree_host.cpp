@@ -83,6 +83,7 @@ hq_status hq_cache_tree_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp,
   a.starts = starts;
   a.rows = (int32_t)rows;
   a.max_rows = max_tree;
+  a.by_block = hq_divide_by((uint32_t)k->block_tokens);
   a.units = (int32_t)s.units;
   a.items = s.items;
   a.joins = s.joins;

@@ -361,6 +361,7 @@ struct hq_cache_attn_args {
   const int32_t* starts;    // of trees: batch + 1 places in the rows
   const uint64_t* masks;    // of trees: ancestors, one per row
   int32_t rows, max_rows;   // of trees: rows of the call, of a sequence at most
+  hq_divisor by_block;      // of trees
 };
 
 // Tokens of the longest sequence that an attention looks at, those of the groups of 16 that
@@ -411,7 +412,7 @@ static inline int64_t hq_cache_joins(int64_t batch, int64_t heads_kv) {
 }
 
 // Rows of a tile of a tree attention, for so many of one KV head.
-static inline int32_t hq_tree_tile(int64_t rows) { return rows <= 16 ? 16 : 32; }
+static inline int32_t hq_tree_tile(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
 // RMS norm fused with the 8-bit activation prep.
 struct hq_norm_args {
