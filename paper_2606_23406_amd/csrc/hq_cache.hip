@@ -224,27 +224,32 @@ __global__ __launch_bounds__(kPlanThreads) void hq_cache_plan_kernel(hq_cache_at
     for (int i = 0; i < kPlanThreads / 64; ++i) x += s_sum[i];
     return x;
   };
-  auto seen = [&](int64_t i, bool tell) {
+  auto seen = [&](int64_t i, bool tell, int32_t& tiles) {
     const CacheSpan of = cache_span_of<MODE>(A, i, tell);
+    tiles = cache_tiles<MODE>(A, of.rows);
     return MODE == kAll ? of.len : of.seen();
   };
+  int32_t tiles = 1;
   int64_t total = 0;
-  for (int64_t i = tid; i < A.batch; i += kPlanThreads) total += seen(i, true);
+  for (int64_t i = tid; i < A.batch; i += kPlanThreads) {
+    const int64_t len = seen(i, true, tiles);
+    total += len * tiles;
+  }
   total = (int64_t)sum((uint64_t)total);
   // it counts chunks for few sequences only: at most one per thread
   static_assert(HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32 <= kPlanThreads, "");
-  const uint32_t chunk = cache_chunk(A, total, tid < A.batch ? seen(tid, false) : -1,
-                                     [&](uint32_t n) { return (int64_t)sum(n); });
+  const int32_t mine = tid < A.batch ? seen(tid, false, tiles) : -1;
+  const uint32_t chunk = cache_chunk(A, total, mine, tiles, [&](uint32_t n) { return (int64_t)sum(n); });
   uint64_t base = 0;  // items, and from bit 32 on split sequences, before these
   for (int64_t i0 = 0; i0 < A.batch; i0 += kPlanThreads) {
     const int64_t i = i0 + tid;
-    const uint32_t n = i < A.batch ? cache_parts(seen(i, false), chunk) : 0u, split = n > 1;
-    uint32_t items = n, splits = split;
+    const uint32_t n = i < A.batch ? cache_parts(seen(i, false, tiles), chunk) : 0u, split = n > 1;
+    uint32_t items = n * (uint32_t)tiles, splits = split;
     wave_scan_incl2(items, splits);
     __syncthreads();  // the last sums have been read
     if (lane == 63) s_sum[wave] = (uint64_t)splits << 32 | items;
     __syncthreads();
-    uint64_t at = base + ((uint64_t)(splits - split) << 32 | (items - n));
+    uint64_t at = base + ((uint64_t)(splits - split) << 32 | (items - n * (uint32_t)tiles));
     for (int x = 0; x < kPlanThreads / 64; ++x) {
       if (x < wave) at += s_sum[x];
       base += s_sum[x];
@@ -445,7 +450,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     return;
   }
   // the chunk's steps of 32 tokens shared out over the waves
-  const int32_t begin0 = (int32_t)((j - it.first) * it.chunk), tokens = min(it.chunk, seen - begin0);
+  const int32_t begin0 = (int32_t)(it.at * it.chunk), tokens = min(it.chunk, seen - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
   CacheWalk<MODE> w;

@@ -230,9 +230,19 @@ struct CacheItem {
   int32_t b;       // -1: behind the last item
   int32_t n;       // chunks of this sequence (an empty one has one, which writes its zeros)
   int32_t first;   // the sequence's first item
+  int32_t at;      // which of its chunks
+  int32_t tile;    // which of a tree's row tiles
   int32_t chunk;
   CacheSpan span;  // its tokens
 };
+
+// Row tiles of a sequence's tree, each with all its chunks; one for the other modes and for
+// none.
+template <int MODE>
+__device__ __forceinline__ int32_t cache_tiles(const hq_cache_attn_args& A, int32_t rows) {
+  if (MODE != kTree) return 1;
+  return max((rows * A.group + (1 << A.tile_shift) - 1) >> A.tile_shift, 1);
+}
 
 __device__ __forceinline__ uint32_t cache_parts(int32_t len, uint32_t chunk) {
   return len == 0 ? 1u : ((uint32_t)len + chunk - 1) / chunk;
@@ -245,12 +255,13 @@ __device__ __forceinline__ uint32_t cache_parts(int32_t len, uint32_t chunk) {
 // eighths until the chunks fit but for a few, to its double at most.  (24 sequences of
 // up to 6001 tokens, 8 KV heads in E4M3: 560 chunks of the even share take 51.7 us, 528 of
 // its 9 / 8 take 41.4.)  More sequences than that take several rounds in any case.
-// `total`: all tokens; `mine`: a lane's or thread's own sequence's, -1 without one; `sum`
-// adds a number over all of these.
+// `total`: all tokens, once for each row tile; `mine`: a lane's or thread's own sequence's, -1
+// without one, and its row tiles; `sum` adds a number over all of these.
 template <typename SUM>
-__device__ __forceinline__ uint32_t cache_chunk(const hq_cache_attn_args& A, int64_t total, int32_t mine, SUM sum) {
-  const int64_t even = (total * A.units + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
-  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.units;
+__device__ __forceinline__ uint32_t cache_chunk(const hq_cache_attn_args& A, int64_t total, int32_t mine, int32_t tiles,
+                                                SUM sum) {
+  const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
+  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.heads_kv;
   uint32_t chunk = HQ_CACHE_LEAST;
   for (int e = 8; e <= 16; ++e) {
     const int64_t c = min(((even * e >> 3) + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
@@ -258,7 +269,7 @@ __device__ __forceinline__ uint32_t cache_chunk(const hq_cache_attn_args& A, int
     if (A.batch > few) break;
     // about: a length a hair over a multiple may count as the multiple
     const float per = __builtin_amdgcn_rcpf((float)chunk) * 0.999999f;
-    if (sum(mine < 0 ? 0u : max(1u, (uint32_t)__builtin_ceilf((float)mine * per))) <= few) break;
+    if (sum(mine < 0 ? 0u : max(1u, (uint32_t)__builtin_ceilf((float)mine * per)) * (uint32_t)tiles) <= few) break;
   }
   return chunk;
 }
@@ -273,9 +284,13 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
   CacheItem it;
   it.b = -1;
   if (!A.join) {  // one chunk each
-    if (j >= A.batch) return it;
-    it.b = it.first = j;
+    const int32_t b = MODE == kTree ? j / A.max_tiles : j;
+    if (b >= A.batch) return it;
+    it.b = b;
+    it.first = j;
     it.n = 1;
+    it.at = 0;
+    it.tile = MODE == kTree ? j - b * A.max_tiles : 0;
     const CacheSpan s = cache_span_of<MODE>(A, it.b, true);
     it.span = {(int32_t)readfirst((uint32_t)s.len), (int32_t)readfirst((uint32_t)s.low),
                (int32_t)readfirst((uint32_t)s.sinks), (int32_t)readfirst((uint32_t)s.rows)};
@@ -295,7 +310,7 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     const hq_cache_of of = A.parts[lo];
     it.first = (int32_t)readfirst((uint32_t)of.first);
     it.n = (int32_t)readfirst((uint32_t)of.n);
-    if (j >= it.first + it.n) return it;
+    if (MODE != kTree && j >= it.first + it.n) return it;
     it.b = (int32_t)readfirst((uint32_t)lo);
     const CacheSpan s = cache_span_of<MODE>(A, it.b, false);
     it.span = {(int32_t)readfirst((uint32_t)s.len), (int32_t)readfirst((uint32_t)s.low),
@@ -305,19 +320,29 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     const bool in = lane < A.batch;
     const CacheSpan s = in ? cache_span_of<MODE>(A, lane, tell) : CacheSpan{-1, 0, 0, 0};
     const int32_t len = MODE == kAll ? s.len : s.seen();
-    int64_t total = max(len, 0);
+    const int32_t tiles = cache_tiles<MODE>(A, s.rows);
+    int64_t total = (int64_t)max(len, 0) * tiles;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
-    const uint32_t chunk = cache_chunk(A, total, len, [](uint32_t n) { return wave_total(n); });
+    const uint32_t chunk = cache_chunk(A, total, len, tiles, [](uint32_t n) { return wave_total(n); });
     const uint32_t n = in ? cache_parts(len, chunk) : 0u;
-    const int32_t incl = (int32_t)wave_scan_incl(n);
+    const int32_t incl = (int32_t)wave_scan_incl(n * (uint32_t)tiles);
     if (j >= __builtin_amdgcn_readlane(incl, 63)) return it;
     const int at = __popcll(__ballot(incl <= j));
     it.b = at;
     it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
-    it.first = __builtin_amdgcn_readlane(incl, at) - it.n;
+    it.first = __builtin_amdgcn_readlane(incl, at) - it.n * (int32_t)__builtin_amdgcn_readlane(tiles, at);
     it.span = cache_span<MODE>(A, __builtin_amdgcn_readlane(s.len, at),
                                MODE == kTree ? __builtin_amdgcn_readlane(s.rows, at) : 0);
+  }
+  if (MODE == kTree) {
+    const int32_t tiles = cache_tiles<MODE>(A, it.span.rows);
+    it.at = (j - it.first) / tiles;
+    it.tile = j - it.first - it.at * tiles;
+    if (it.at >= it.n) it.b = -1;  // behind the last sequence's
+  } else {
+    it.at = j - it.first;
+    it.tile = 0;
   }
   it.chunk = even_chunk(MODE == kAll ? it.span.len : it.span.seen(), it.n);
   return it;

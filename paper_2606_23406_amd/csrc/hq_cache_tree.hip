@@ -31,6 +31,12 @@ namespace {
 typedef _Float16 v2h_t __attribute__((ext_vector_type(2)));
 typedef _Float16 v8h16_t __attribute__((ext_vector_type(8)));
 
+typedef float v16_t __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ v16_t mfma_f16(const uint4& a, const uint32_t* b, v16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h16_t, a),
+                                                __builtin_bit_cast(v8h16_t, (v4w_t){b[0], b[1], b[2], b[3]}), c, 0, 0, 0);
+}
 __device__ __forceinline__ v4_t mfma_f16(const uint32_t* a, const uint32_t* b, v4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h16_t, (v4w_t){a[0], a[1], a[2], a[3]}),
                                                 __builtin_bit_cast(v8h16_t, (v4w_t){b[0], b[1], b[2], b[3]}), c, 0, 0, 0);
@@ -427,18 +433,17 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   auto o_row = [&](int w, int row) { return (float*)(s_ring + w * WAVE) + row * kOPitch; };
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4, grp = tid >> 4;
   const int wave = (int)readfirst((uint32_t)(tid >> 6));
-  const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.units);
-  const int32_t unit = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.units);
-  const int32_t tile = unit / A.heads_kv, head = unit - tile * A.heads_kv, c0 = n * 8;
+  const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.heads_kv), c0 = n * 8;
+  const int32_t head = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.heads_kv);
   const CacheItem it = cache_item<kTree>(A, j, lane, blockIdx.x == 0 && wave == 0);
   if (it.b < 0) return;
   // what the join goes by
-  if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && unit == 0 && tid == 0)
+  if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && head == 0 && tid == 0)
     A.parts[it.b] = {it.first, it.n};
-  const int32_t rows = it.span.rows, seen = it.span.seen();
+  const int32_t rows = it.span.rows, seen = it.span.seen(), tile = it.tile;
   if (tile * ROWS >= rows * A.group) return;  // none of this sequence's, or it has none at all
   const int32_t from = A.starts[it.b];
-  const int32_t begin0 = (int32_t)((j - it.first) * it.chunk), tokens = min(it.chunk, seen - begin0);
+  const int32_t begin0 = (int32_t)(it.at * it.chunk), tokens = min(it.chunk, seen - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
   CacheWalk<kTree> w;
@@ -567,11 +572,15 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
 // operands are read in, a tile ahead of the products; the codes of the tile after it are on
 // their way in registers meanwhile.  Each wave has 32 rows: of a tile of 128 rows each wave
 // takes both steps, of one of 64 two waves share the rows and take a step each.
+//
+// The products are 32 x 32 x 16: a step's scores are one tile C[token, row], in which lane l
+// holds tokens 8 q + 4 (l / 32) + r of row l % 32; with product t of the values contracting
+// tokens 16 t .. in the order 8 q' + 4 (l / 32) + r, lane by lane, they are its operand's.
 constexpr int kTreeTile = 64;
 template <int FMT>
 struct TreeTile {
-  // keys: [step][half][contraction step][lane] 16 bytes; values: [step][dim in its group of 8]
-  // [lane] 16 bytes
+  // keys: [step][contraction step][lane] 16 bytes, dims 8 (2 s + l / 32) ..;  values: [step][group
+  // of 32 dims][product][lane] 16 bytes, group d being dims 8 (l % 16) + 2 d + l / 16 % 2
   static constexpr int V = kTreeTile * HQ_TILE * 2, KS = 2 * V, VS = KS + 4 * kTreeTile, SEEN = VS + 4 * kTreeTile;
   static constexpr int BYTES = SEEN + 2 * 16 + 480;  // a multiple of 1 KB
 };
@@ -581,7 +590,8 @@ template <int FMT>
 struct TreeLoads {
   static constexpr int KW = FMT == kMx ? 4 : 8, VW = FMT == kMx ? 1 : 2;
   uint32_t w[2][8];    // keys: half, words of lane's 32 codes (token lane % 16, run lane / 16);
-                       // values: half, VW words of each of four tokens (4 (lane / 16) + r, dims 8 (lane % 16) ..)
+                       // values: VW words of each of the tokens 16 (lane / 32) + 4 (lane / 16 % 2) + 8 q + r,
+                       // dims 8 (lane % 16) ..
   uint32_t scale[2];   // keys: half's token lane % 16; values: [0] token lane % 32
   int32_t live[2];     // bits of tokens that anybody sees
 };
@@ -627,10 +637,15 @@ struct TreeWay {
           x.w[h][i] = v.x; x.w[h][i + 1] = v.y; x.w[h][i + 2] = v.z; x.w[h][i + 3] = v.w;
         }
         x.scale[h] = scales[row[h] + n];
-      } else {
+      }
+    }
+    if constexpr (!KEYS) {
+      const uint8_t* from = codes + (lane < 32 ? row[0] : row[1]) * RB + (g & 1) * 4 * RB + n * (RB / 16);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const uint8_t* at = from + (4 * g + r) * RB + n * (RB / 16);
+          const uint8_t* at = from + (8 * h + r) * RB;
           if constexpr (FMT == kMx) {
             x.w[h][r] = *(const uint32_t*)at;
           } else {
@@ -638,9 +653,8 @@ struct TreeWay {
             x.w[h][2 * r] = v.x; x.w[h][2 * r + 1] = v.y;
           }
         }
-      }
+      x.scale[0] = x.scale[1] = scales[(lane & 16 ? row[1] : row[0]) + n];
     }
-    if constexpr (!KEYS) x.scale[0] = x.scale[1] = scales[(lane & 16 ? row[1] : row[0]) + n];
   }
 };
 
@@ -685,7 +699,8 @@ __device__ __forceinline__ void turn_keys(const TreeLoads<FMT>& x, uint8_t* tile
         dims_of<FMT>(x.w[h][2 * s], 1.0f, o);
         dims_of<FMT>(x.w[h][2 * s + 1], 1.0f, o + 2);
       }
-      *(uint4*)(tile + (((step * 2 + h) * 4 + s) * 64 + lane) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+      // dims 8 (4 g + s) ..
+      *(uint4*)(tile + ((step * 8 + 2 * g + s / 2) * 64 + (s & 1) * 32 + 16 * h + n) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
     }
     if (g == 0) *(uint32_t*)(tile + TreeTile<FMT>::KS + (step * 32 + 16 * h + n) * 4) = scale;
   }
@@ -704,7 +719,7 @@ __device__ __forceinline__ void turn_values(TreeLoads<FMT>& x, uint8_t* tile, in
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int from = 16 * h + 4 * g + r;  // the lane that has the token's
+        const int from = 16 * (g >> 1) + 4 * (g & 1) + 8 * h + r;  // the lane that has the token's
         const uint32_t w = (uint32_t)__shfl((int)x.scale[0], from, 64), of = (uint32_t)__shfl((int)scale, from, 64);
         f[h][r] = below_scale((w >> (8 * (n >> 2))) & 0xFFu, __uint_as_float(of));
       }
@@ -715,7 +730,7 @@ __device__ __forceinline__ void turn_values(TreeLoads<FMT>& x, uint8_t* tile, in
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (!((x.live[h] >> (4 * g + r)) & 1)) {
+        if (!(((lane < 32 ? x.live[0] : x.live[1]) >> (4 * (g & 1) + 8 * h + r)) & 1)) {
 #pragma unroll
           for (int i = 0; i < VW; ++i) x.w[h][VW * r + i] = 0u;
         }
@@ -734,9 +749,11 @@ __device__ __forceinline__ void turn_values(TreeLoads<FMT>& x, uint8_t* tile, in
         for (int d = 0; d < D; ++d) vf[d][2 * h + r / 2] = o[d];
       }
 #pragma unroll
-    for (int d = 0; d < D; ++d)
-      *(uint4*)(tile + TreeTile<FMT>::V + ((step * 8 + D * w + d) * 64 + lane) * 16) =
+    for (int d = 0; d < D; ++d) {
+      const int j = D * w + d;  // dim 8 n + j
+      *(uint4*)(tile + TreeTile<FMT>::V + (((step * 4 + j / 2) * 2 + (g >> 1)) * 64 + (g & 1) * 32 + (j & 1) * 16 + n) * 16) =
           make_uint4(vf[d][0], vf[d][1], vf[d][2], vf[d][3]);
+    }
   }
   if (lane < 32) *(uint32_t*)(tile + TreeTile<FMT>::VS + (step * 32 + lane) * 4) = scale;
   const float most = half_wave_max(__uint_as_float(scale)), least = -half_wave_max(-__uint_as_float(scale));
@@ -744,6 +761,80 @@ __device__ __forceinline__ void turn_values(TreeLoads<FMT>& x, uint8_t* tile, in
     *(uint4*)(tile + TreeTile<FMT>::SEEN + step * 16) =
         make_uint4(__float_as_uint(lift_of(__float_as_uint(most))), (uint32_t)(x.live[0] | x.live[1] << 16),
                    one_lift(__float_as_uint(least), __float_as_uint(most)), 0u);
+}
+
+// What a wave carries over its tokens: a lane's row's reference and sum, its values' sum, acc[d][i]
+// dim 8 (8 (i / 4 % 2) + 4 (l / 32) + i % 4) + 2 d + i / 8.
+struct WideState {
+  float m, l;
+  v16_t acc[4];
+};
+
+// tree_weights of 32 tokens' scores in the 32 x 32 layout; ks and vs in LDS; pt: the terms of the
+// two products' operands.
+__device__ __forceinline__ void wide_weights(v16_t& c, const float* ks, const float* vs, bool each, float lift,
+                                             const int32_t (&live)[2], const int32_t (&at)[2], int32_t ctx, int32_t sinks,
+                                             const TreeRow* rows, float back, int lane, WideState& z, uint32_t (&pt)[2][2][4]) {
+  const int u = lane >> 5;
+  float top;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float4 k = *(const float4*)(ks + 8 * q + 4 * u);
+    c[4 * q] *= k.x; c[4 * q + 1] *= k.y; c[4 * q + 2] *= k.z; c[4 * q + 3] *= k.w;
+  }
+  if (each) {
+    const TreeRow row = rows[lane & 31];
+    top = -__builtin_inff();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t sees = (row.sees(at[h], ctx, sinks) & (uint32_t)live[h]) >> (4 * u);
+#pragma unroll
+      for (int q = 2 * h; q < 2 * h + 2; ++q) {
+        const float4 v = *(const float4*)(vs + 8 * q + 4 * u);
+        const float v4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          c[4 * q + r] = (sees >> (8 * (q & 1) + r)) & 1 ? c[4 * q + r] : -__builtin_inff();
+          top = __builtin_fmaxf(top, __builtin_fmaf(c[4 * q + r], back, lift_of(__float_as_uint(v4[r]))));
+        }
+      }
+    }
+  } else {
+    top = c[0];
+#pragma unroll
+    for (int k = 1; k < 16; ++k) top = __builtin_fmaxf(top, c[k]);
+    top = __builtin_fmaf(top, back, lift);
+  }
+  const v2u_t t = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+  top = __builtin_fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+  if (__ballot(top > z.m + kSlack)) {
+    // a row's own scores alone move it
+    const float mn = top > z.m + kSlack ? top : z.m;
+    const float alpha = __builtin_amdgcn_exp2f(z.m - (mn == -__builtin_inff() ? 0.0f : mn));
+    z.m = mn;
+    z.l *= alpha;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) z.acc[d] *= alpha;
+  }
+  const float ref = z.m == -__builtin_inff() ? 0.0f : z.m;  // nothing seen yet
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float4 v = *(const float4*)(vs + 8 * q + 4 * u);
+    float w[4] = {v.x, v.y, v.z, v.w};
+    if (each) {
+      // a scale that the row does not see may be a NaN
+#pragma unroll
+      for (int r = 0; r < 4; ++r) w[r] = c[4 * q + r] == -__builtin_inff() ? 0.0f : w[r];
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(c[4 * q + r], back, -ref));
+      z.l += e;
+      w[r] *= e;
+    }
+    two_terms(w[0], w[1], pt[0][q / 2][2 * (q & 1)], pt[1][q / 2][2 * (q & 1)]);
+    two_terms(w[2], w[3], pt[0][q / 2][2 * (q & 1) + 1], pt[1][q / 2][2 * (q & 1) + 1]);
+  }
 }
 
 // Everything that the workgroup wrote to LDS is there for all of it; loads from memory stay on their way.
@@ -756,26 +847,25 @@ __device__ __forceinline__ void tile_barrier() {
 template <int FMT, int ROWS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_wide_kernel(hq_cache_attn_args A) {
   using T = TreeTile<FMT>;
-  constexpr int RT = 2, RW = ROWS / 32, TW = 4 / RW;  // waves along the rows, along the tokens
+  constexpr int RW = ROWS / 32, TW = 4 / RW;  // waves along the rows, along the tokens
   extern __shared__ __attribute__((aligned(16))) uint8_t s_tile[];  // two tiles
   __shared__ float s_m[TW][ROWS], s_l[TW][ROWS], s_f[ROWS];
   __shared__ TreeRow s_row[ROWS];
   static_assert(TW * ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
   auto o_row = [&](int w, int row) { return (float*)s_tile + (w * ROWS + row) * kOPitch; };
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4, grp = tid >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4;
   const int wave = (int)readfirst((uint32_t)(tid >> 6)), rw = wave % RW, tw = wave / RW;
-  const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.units);
-  const int32_t unit = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.units);
-  const int32_t tile = unit / A.heads_kv, head = unit - tile * A.heads_kv, c0 = n * 8;
+  const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.heads_kv), c0 = n * 8;
+  const int32_t head = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.heads_kv);
   const CacheItem it = cache_item<kTree>(A, j, lane, blockIdx.x == 0 && wave == 0);
   if (it.b < 0) return;
   // what the join goes by
-  if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && unit == 0 && tid == 0)
+  if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && head == 0 && tid == 0)
     A.parts[it.b] = {it.first, it.n};
-  const int32_t rows = it.span.rows, seen = it.span.seen();
+  const int32_t rows = it.span.rows, seen = it.span.seen(), tile = it.tile;
   if (tile * ROWS >= rows * A.group) return;  // none of this sequence's, or it has none at all
   const int32_t from = A.starts[it.b];
-  const int32_t begin = (int32_t)((j - it.first) * it.chunk), end = begin + min(it.chunk, seen - begin);
+  const int32_t begin = (int32_t)(it.at * it.chunk), end = begin + min(it.chunk, seen - begin);
   TreeWay way;
   way.table = A.table + (int64_t)it.b * A.max_blocks;
   way.span = it.span;
@@ -794,44 +884,46 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   const int32_t ctx = it.span.len - rows;
   if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each,
-  // [row tile][term][contraction step][lane] 16 bytes
+  // [32 rows][term][contraction step][lane] 16 bytes; the next ones are on their way meanwhile
   const uint4 qd = sign_words(A.k_dsign16, head * HQ_TILE + c0);
-#pragma unroll 2
-  for (int i = 0; i < ROWS / 16; ++i) {
+  auto query = [&](int i) {
     const TreePlace p(A, tile * ROWS + 16 * i + grp);
     Raw8 raw = {};
-    if (p.i < rows)
+    if (i < ROWS / 16 && p.i < rows)
       raw = load_raw8(A.q, ((int64_t)(from + p.i) * A.heads_q + (int64_t)head * A.group + p.head) * HQ_TILE + c0, A.q_bf16);
+    return raw;
+  };
+  Raw8 raw0 = query(0), raw1 = query(1);
+#pragma unroll 1
+  for (int i = 0; i < ROWS / 16; ++i) {
+    const Raw8 raw = raw0;
+    raw0 = raw1;
+    raw1 = query(i + 2);
     uint4 hi, lo;
     const float f = tree_query(raw, A.q_bf16, qd, A.qscale, lane, hi, lo);
-    uint8_t* to = s_tile + i * 8192 + (n & 3) * 1024 + ((n >> 2) * 16 + grp) * 16;
+    uint8_t* to = s_tile + (i >> 1) * 16384 + (n >> 1) * 1024 + ((n & 1) * 32 + (i & 1) * 16 + grp) * 16;
     *(uint4*)to = hi;
-    *(uint4*)(to + 4096) = lo;
+    *(uint4*)(to + 8192) = lo;
     if (n == 0) s_f[16 * i + grp] = f;
   }
   __syncthreads();
-  uint32_t q[RT][2][4][4];
-  float back[RT];  // 1 / the power of two that a row was moved by
+  uint32_t q[2][8][4];
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const uint4 x = *(const uint4*)(s_tile + (((2 * rw + i) * 2 + t) * 4 + s) * 1024 + lane * 16);
-        q[i][t][s][0] = x.x; q[i][t][s][1] = x.y; q[i][t][s][2] = x.z; q[i][t][s][3] = x.w;
-      }
-    back[i] = s_f[32 * rw + 16 * i + n];
-  }
+    for (int s = 0; s < 8; ++s) {
+      const uint4 x = *(const uint4*)(s_tile + ((rw * 2 + t) * 8 + s) * 1024 + lane * 16);
+      q[t][s][0] = x.x; q[t][s][1] = x.y; q[t][s][2] = x.z; q[t][s][3] = x.w;
+    }
+  const float back = s_f[32 * rw + (lane & 31)];  // 1 / the power of two that the row was moved by
   __syncthreads();  // the queries' place is written over
-  TreeState z[RT];
+  WideState z;
+  z.m = -__builtin_inff();
+  z.l = 0.0f;
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    z[i].m = -__builtin_inff();
-    z[i].l = 0.0f;
+  for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z[i].acc[k] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  }
+    for (int k = 0; k < 16; ++k) z.acc[d][k] = 0.0f;
   // from here on every row's window has begun
   const int32_t open = A.window ? ctx + rows - A.window : 0;
   const bool idle = tile * ROWS + 32 * rw >= rows * A.group;  // the wave has no rows
@@ -866,41 +958,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
         bool each = all != 0xFFFFFFFFu || readfirst(about.z) == 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
-        v4_t c[RT][2];
+        v16_t c;
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+        for (int k = 0; k < 16; ++k) c[k] = 0.0f;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) c[i][h] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < 8; ++s) {
+          const uint4 a = *(const uint4*)(at_tile + ((step * 8 + s) * 64 + lane) * 16);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          uint4 a[2];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) a[h] = *(const uint4*)(at_tile + (((step * 2 + h) * 4 + s) * 64 + lane) * 16);
-#pragma unroll
-          for (int u = 1; u >= 0; --u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int i = 0; i < RT; ++i) c[i][h] = mfma_f16((const uint32_t*)&a[h], q[i][u][s], c[i][h]);
+          for (int t1 = 1; t1 >= 0; --t1) c = mfma_f16(a, q[t1][s], c);
         }
-        float ks[2][4], vs[2][4];
+        uint32_t pt[2][2][4];
+        wide_weights(c, (const float*)(at_tile + T::KS) + step * 32, (const float*)(at_tile + T::VS) + step * 32, each,
+                     __uint_as_float(readfirst(about.x)), live, at, ctx, A.sinks, s_row + 32 * rw, back, lane, z, pt);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float4 x = *(const float4*)(at_tile + T::KS + (step * 32 + 16 * h + 4 * g) * 4);
-          const float4 y = *(const float4*)(at_tile + T::VS + (step * 32 + 16 * h + 4 * g) * 4);
-          ks[h][0] = x.x; ks[h][1] = x.y; ks[h][2] = x.z; ks[h][3] = x.w;
-          vs[h][0] = y.x; vs[h][1] = y.y; vs[h][2] = y.z; vs[h][3] = y.w;
-        }
-        uint32_t pt[RT][2][4];
-        tree_weights<RT>(c, ks, vs, each, __uint_as_float(readfirst(about.x)), live, at, ctx, A.sinks, s_row + 32 * rw, back, lane, z, pt);
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint4 v = *(const uint4*)(at_tile + T::V + ((step * 8 + k) * 64 + lane) * 16);
+          for (int d = 0; d < 4; ++d) {
+            const uint4 v = *(const uint4*)(at_tile + T::V + (((step * 4 + d) * 2 + k) * 64 + lane) * 16);
 #pragma unroll
-          for (int u = 1; u >= 0; --u)
-#pragma unroll
-            for (int i = 0; i < RT; ++i) z[i].acc[k] = mfma_f16((const uint32_t*)&v, pt[i][u], z[i].acc[k]);
-        }
+            for (int t1 = 1; t1 >= 0; --t1) z.acc[d] = mfma_f16(v, pt[t1][k], z.acc[d]);
+          }
       }
       tile_barrier();
       uint8_t* const x = at_tile;
@@ -913,19 +990,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   else
     run(std::false_type());
   // ---- the waves' sums under one reference, one row per 16 lanes
+  {
+    const v2u_t l = __builtin_amdgcn_permlane32_swap(__float_as_uint(z.l), __float_as_uint(z.l), false, false);
+    const int u = lane >> 5, at_row = 32 * rw + (lane & 31);
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    z[i].l = groups_sum(z[i].l);
-    const int at_row = 32 * rw + 16 * i + n;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float* o = o_row(tw, at_row) + (4 * g + r) * 8;
-      *(float4*)o = make_float4(z[i].acc[0][r], z[i].acc[1][r], z[i].acc[2][r], z[i].acc[3][r]);
-      *(float4*)(o + 4) = make_float4(z[i].acc[4][r], z[i].acc[5][r], z[i].acc[6][r], z[i].acc[7][r]);
+    for (int k = 0; k < 8; ++k) {  // i / 4 % 2 = k / 4, i % 4 = k % 4
+      const int i = 4 * (k >> 2) + (k & 3);
+      float* o = o_row(tw, at_row) + (8 * (k >> 2) + 4 * u + (k & 3)) * 8;
+      *(float4*)o = make_float4(z.acc[0][i], z.acc[0][i + 8], z.acc[1][i], z.acc[1][i + 8]);
+      *(float4*)(o + 4) = make_float4(z.acc[2][i], z.acc[2][i + 8], z.acc[3][i], z.acc[3][i + 8]);
     }
-    if (g == 0) {
-      s_m[tw][at_row] = z[i].m;
-      s_l[tw][at_row] = z[i].l;
+    if (u == 0) {
+      s_m[tw][at_row] = z.m;
+      s_l[tw][at_row] = __uint_as_float(l[0]) + __uint_as_float(l[1]);
     }
   }
   __syncthreads();
@@ -964,8 +1041,8 @@ __global__ __launch_bounds__(256) void hq_cache_tree_join_kernel(hq_cache_attn_a
   const bool in = at < (uint32_t)rows * (uint32_t)A.heads_q;
   const uint32_t q = in ? at : 0u, i = q / (uint32_t)A.heads_q, hq = q - i * (uint32_t)A.heads_q, head = hq / (uint32_t)A.group;
   const uint32_t row = i * (uint32_t)A.group + hq - head * (uint32_t)A.group, tile = row / (uint32_t)tile_rows;
-  const int64_t part0 = ((int64_t)has.first * A.units + tile * (uint32_t)A.heads_kv + head) * tile_rows + (row - tile * (uint32_t)tile_rows);
-  const int64_t step = (int64_t)A.units * tile_rows;
+  const int64_t part0 = (((int64_t)has.first + tile) * A.heads_kv + head) * tile_rows + (row - tile * (uint32_t)tile_rows);
+  const int64_t step = (int64_t)cache_tiles<kTree>(A, rows) * A.heads_kv * tile_rows;
   float M = -__builtin_inff();
   for (int32_t x = 0; x < has.n; ++x) M = __builtin_fmaxf(M, A.part_m[part0 + x * step]);
   const float ref = M == -__builtin_inff() ? 0.0f : M;
@@ -988,7 +1065,7 @@ int launch_narrow(const hq_cache_attn_args& a, hipStream_t st) {
   static hq_lds_granted granted;
   constexpr size_t lds = (size_t)HQ_CACHE_WAVES * tree_wave_bytes<FMT, RT>();
   if (const int e = hq_allow_lds((const void*)hq_cache_tree_kernel<FMT, RT>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_tree_kernel<FMT, RT>), dim3((uint32_t)(a.items * a.units)), dim3(64 * HQ_CACHE_WAVES), lds, st, a);
+  hipLaunchKernelGGL((hq_cache_tree_kernel<FMT, RT>), dim3((uint32_t)(a.items * a.heads_kv)), dim3(64 * HQ_CACHE_WAVES), lds, st, a);
   return 0;
 }
 
@@ -997,7 +1074,7 @@ int launch_wide(const hq_cache_attn_args& a, hipStream_t st) {
   static hq_lds_granted granted;
   constexpr size_t lds = 2 * TreeTile<FMT>::BYTES;
   if (const int e = hq_allow_lds((const void*)hq_cache_tree_wide_kernel<FMT, ROWS>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_tree_wide_kernel<FMT, ROWS>), dim3((uint32_t)(a.items * a.units)), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((hq_cache_tree_wide_kernel<FMT, ROWS>), dim3((uint32_t)(a.items * a.heads_kv)), dim3(256), lds, st, a);
   return 0;
 }
 

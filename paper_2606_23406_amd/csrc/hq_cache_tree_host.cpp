@@ -12,27 +12,23 @@ bool sizes_ok(const hq_cache* k, int64_t batch, int32_t heads_q, int32_t max_blo
 }
 
 struct TreeSize {
-  int64_t seen, units, items, joins, parts;
+  int64_t seen, tile, tiles, items, joins, parts;
   size_t bytes;  // enough for the call, and never less for a larger one
 };
 
 TreeSize tree_size(int64_t batch, int32_t heads, int32_t group, int64_t max_tokens, int32_t max_tree, int32_t window,
                    int32_t sinks) {
   TreeSize s;
-  const int64_t rows = (int64_t)max_tree * group, tile = hq_tree_tile(rows);
+  const int64_t rows = (int64_t)max_tree * group;
+  s.tile = hq_tree_tile(rows);
+  s.tiles = (rows + s.tile - 1) / s.tile;
   s.seen = hq_cache_seen(max_tokens, window, sinks, max_tree);
-  s.units = (rows + tile - 1) / tile * heads;
-  s.items = hq_cache_items(batch, s.units, s.seen);
-  s.joins = hq_cache_joins(batch, s.units);
-  s.parts = s.items * s.units * tile;
-  // bounds on items * units and joins that do not fall as units grow
-  const int64_t chunks = (s.seen + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST * batch * s.units;
-  const int64_t even = batch * s.units + HQ_CACHE_WG_TARGET + s.units;
-  const int64_t listed = batch < HQ_CACHE_WG_TARGET + 1 ? batch : HQ_CACHE_WG_TARGET + 1;
-  s.bytes = s.seen <= HQ_CACHE_WHOLE
-                ? 0
-                : (size_t)((chunks < even ? chunks : even) * tile) * (HQ_TILE + 2) * sizeof(float) +
-                      (size_t)batch * sizeof(hq_cache_of) + (size_t)(listed + 1) * sizeof(int32_t);
+  s.items = hq_tree_items(batch, heads, s.seen, s.tiles);
+  s.joins = hq_cache_joins(batch, heads);
+  s.parts = s.items * heads * s.tile;
+  s.bytes = s.seen <= HQ_CACHE_WHOLE ? 0
+                                     : (size_t)s.parts * (HQ_TILE + 2) * sizeof(float) + (size_t)batch * sizeof(hq_cache_of) +
+                                           (size_t)(s.joins + 1) * sizeof(int32_t);
   return s;
 }
 
@@ -84,12 +80,13 @@ hq_status hq_cache_tree_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp,
   a.rows = (int32_t)rows;
   a.max_rows = max_tree;
   a.by_block = hq_divide_by((uint32_t)k->block_tokens);
-  a.units = (int32_t)s.units;
+  while (1 << a.tile_shift < s.tile) ++a.tile_shift;
+  a.max_tiles = (int32_t)s.tiles;
   a.items = s.items;
   a.joins = s.joins;
   a.join = s.seen > HQ_CACHE_WHOLE;
   // workgroups of both launches
-  if (s.units > kMaxGroups || s.items > kMaxGroups / s.units ||
+  if (s.items > kMaxGroups / k->heads ||
       s.joins * (((int64_t)max_tree * heads_q + 15) / 16) > kMaxGroups)
     return HQ_ERR_UNSUPPORTED;
   if (a.join && (!workspace || !aligned(workspace, 16) || ws_bytes < s.bytes)) return HQ_ERR_INVALID_ARG;

@@ -356,12 +356,12 @@ struct hq_cache_attn_args {
   int32_t join;             // a sequence may have several chunks
   int32_t q_bf16, out_bf16;
   float qscale;             // softmax scale times log2(e) / 128
-  int32_t units;            // workgroups per chunk: the KV heads, of a tree times its row tiles
   int32_t window, sinks;    // 0: every token
   const int32_t* starts;    // of trees: batch + 1 places in the rows
   const uint64_t* masks;    // of trees: ancestors, one per row
   int32_t rows, max_rows;   // of trees: rows of the call, of a sequence at most
   hq_divisor by_block;      // of trees
+  int32_t tile_shift, max_tiles;  // of trees: log2 of a tile's rows, tiles of max_rows
 };
 
 // Tokens of the longest sequence that an attention looks at, those of the groups of 16 that
@@ -396,6 +396,14 @@ static inline int64_t hq_cache_items(int64_t batch, int64_t heads_kv, int64_t ma
   const int64_t most = (max_tokens + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST;
   const int64_t even = HQ_CACHE_WG_TARGET / heads_kv + 1;
   return batch * most < batch + even ? batch * most : batch + even;
+}
+// The same of trees, whose chunks come once for each of a sequence's row tiles: a chunk is at
+// least total * heads_kv / HQ_CACHE_WG_TARGET with the total taken once per row tile.
+static inline int64_t hq_tree_items(int64_t batch, int64_t heads_kv, int64_t max_tokens, int64_t tiles) {
+  if (max_tokens <= HQ_CACHE_WHOLE) return batch * tiles;
+  const int64_t most = (max_tokens + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST * batch * tiles;
+  const int64_t even = batch * tiles + HQ_CACHE_WG_TARGET / heads_kv + 1;
+  return most < even ? most : even;
 }
 // Up to this many sequences every wave goes through all lengths, one per lane; the items
 // of more are planned by a launch before.
