@@ -416,11 +416,11 @@ constexpr int tree_wave_bytes() {
   return CacheRing<FMT>::WAVE > out ? CacheRing<FMT>::WAVE : out;
 }
 
-template <int FMT, int RT>
-__global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_kernel(
+template <int FMT, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_kernel(
     hq_cache_attn_args A) {
   using R = CacheRing<FMT>;
-  constexpr int WAVES = HQ_CACHE_WAVES, ROWS = 16 * RT, WAVE = tree_wave_bytes<FMT, RT>();
+  constexpr int ROWS = 16 * RT, WAVE = tree_wave_bytes<FMT, RT>();
   extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];  // a wave's ring after the other
   __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS], s_f[ROWS];
   __shared__ TreeRow s_row[ROWS];
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     const TreePlace p(A, tile * ROWS + 16 * i + grp);
-    if (p.i < rows)
+    if (grp < 16 && p.i < rows)
       qraw[i] = load_raw8(A.q, ((int64_t)(from + p.i) * A.heads_q + (int64_t)head * A.group + p.head) * HQ_TILE + c0, A.q_bf16);
   }
   const int32_t ctx = it.span.len - rows;
@@ -469,6 +469,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
+    if (grp >= 16) break;  // the last four of eight waves
     uint4 hi, lo;
     const float f = tree_query(qraw[i], A.q_bf16, qd, A.qscale, lane, hi, lo);
     *(uint4*)(q_row(16 * i + grp, 0) + c0) = hi;
@@ -546,6 +547,7 @@ __global__ __launch_bounds__(64 * HQ_CACHE_WAVES) __attribute__((amdgpu_waves_pe
     }
   }
   __syncthreads();
+  if (grp >= 16) return;
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     const int at_row = 16 * i + grp;
@@ -1060,12 +1062,12 @@ __global__ __launch_bounds__(256) void hq_cache_tree_join_kernel(hq_cache_attn_a
   if (in) store8(A.out, ((int64_t)(from + (int32_t)i) * A.heads_q + hq) * HQ_TILE + c0, A.out_bf16, v);
 }
 
-template <int FMT, int RT>
+template <int FMT, int RT, int WAVES>
 int launch_narrow(const hq_cache_attn_args& a, hipStream_t st) {
   static hq_lds_granted granted;
-  constexpr size_t lds = (size_t)HQ_CACHE_WAVES * tree_wave_bytes<FMT, RT>();
-  if (const int e = hq_allow_lds((const void*)hq_cache_tree_kernel<FMT, RT>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_tree_kernel<FMT, RT>), dim3((uint32_t)(a.items * a.heads_kv)), dim3(64 * HQ_CACHE_WAVES), lds, st, a);
+  constexpr size_t lds = (size_t)WAVES * tree_wave_bytes<FMT, RT>();
+  if (const int e = hq_allow_lds((const void*)hq_cache_tree_kernel<FMT, RT, WAVES>, lds, granted)) return e;
+  hipLaunchKernelGGL((hq_cache_tree_kernel<FMT, RT, WAVES>), dim3((uint32_t)(a.items * a.heads_kv)), dim3(64 * WAVES), lds, st, a);
   return 0;
 }
 
@@ -1080,10 +1082,12 @@ int launch_wide(const hq_cache_attn_args& a, hipStream_t st) {
 
 template <int FMT>
 int launch_tree(const hq_cache_attn_args& a, hipStream_t st) {
-  switch (hq_tree_tile((int64_t)a.max_rows * a.group)) {
-    case 16: return launch_narrow<FMT, 1>(a, st);
-    case 32: return launch_narrow<FMT, 2>(a, st);
-    case 64: return launch_wide<FMT, 64>(a, st);
+  switch (a.tile_shift) {
+    case 4:
+      // as the one-token attention, calls that leave CUs idle have eight waves share a chunk
+      return a.items * a.heads_kv <= 256 ? launch_narrow<FMT, 1, 2 * HQ_CACHE_WAVES>(a, st)
+                                         : launch_narrow<FMT, 1, HQ_CACHE_WAVES>(a, st);
+    case 5: return launch_narrow<FMT, 2, HQ_CACHE_WAVES>(a, st);
     default: return launch_wide<FMT, 128>(a, st);
   }
 }
@@ -1103,7 +1107,7 @@ int hq_launch_cache_tree(const hq_cache_attn_args& a, int format, void* stream) 
   if (a.join && a.joins) {
     const uint32_t per = ((uint32_t)a.max_rows * (uint32_t)a.heads_q + 15) / 16;
     hipLaunchKernelGGL(hq_cache_tree_join_kernel, dim3((uint32_t)a.joins * per), dim3(256), 0, st, a,
-                       hq_tree_tile(a.max_rows * a.group), per);
+                       1 << a.tile_shift, per);
   }
   return (int)hipGetLastError();
 }

@@ -20,14 +20,18 @@ TreeSize tree_size(int64_t batch, int32_t heads, int32_t group, int64_t max_toke
                    int32_t sinks) {
   TreeSize s;
   const int64_t rows = (int64_t)max_tree * group;
-  s.tile = hq_tree_tile(rows);
-  s.tiles = (rows + s.tile - 1) / s.tile;
   s.seen = hq_cache_seen(max_tokens, window, sinks, max_tree);
+  s.tile = hq_tree_tile(rows, batch * heads, s.seen);
+  s.tiles = (rows + s.tile - 1) / s.tile;
   s.items = hq_tree_items(batch, heads, s.seen, s.tiles);
   s.joins = hq_cache_joins(batch, heads);
   s.parts = s.items * heads * s.tile;
+  // a bound on the parts that does not fall from one rule's tiles to another's
+  const int64_t least = rows <= 16 ? 16 : 4 * rows < 3 * 128 ? 32 : 128, padded = (rows + least - 1) / least * least;
+  const int64_t most = (s.seen + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST * batch * heads * padded;
+  const int64_t even = batch * heads * padded + (HQ_CACHE_WG_TARGET + heads) * least, parts = most < even ? most : even;
   s.bytes = s.seen <= HQ_CACHE_WHOLE ? 0
-                                     : (size_t)s.parts * (HQ_TILE + 2) * sizeof(float) + (size_t)batch * sizeof(hq_cache_of) +
+                                     : (size_t)parts * (HQ_TILE + 2) * sizeof(float) + (size_t)batch * sizeof(hq_cache_of) +
                                            (size_t)(s.joins + 1) * sizeof(int32_t);
   return s;
 }
