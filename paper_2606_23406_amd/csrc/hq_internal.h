@@ -295,32 +295,39 @@ struct hq_rope_table_args {
   int32_t pairs;
   float factor;
 };
-// Rows turned by their positions.
-#define HQ_ROPE_HEADS 4   // head vectors of a lane group
+// Rows turned by their positions: a lane group takes `per` head vectors of a row, 4 where at
+// most a fifth of their places stay empty, else (of hq_rope) 2, of one head 1.
 struct hq_rope_args {
   hq_turns turn;
   const void* x;
   void* y;
   int64_t ldx, ldy;
   uint32_t tiles;         // rows * groups
-  int32_t heads, groups;  // groups = ceil(heads / HQ_ROPE_HEADS)
+  int32_t heads, per, groups;  // groups = ceil(heads / per)
   hq_divisor by_groups;
   int32_t x_bf16, y_bf16, transposed;
+  int32_t past;           // y is stored past the caches
 };
+// 4 of heads that fill it to four fifths.
+static inline int32_t hq_rope_per(int32_t heads, int32_t else_per) {
+  return 4 * ((heads + 3) / 4 * 4) <= 5 * heads ? 4 : else_per < heads ? else_per : heads;
+}
+// Bytes of turned rows from which they are stored past the caches, which cannot hold them until
+// they are read: 7800 rows of 20 heads in bf16 (40 MB) take 15.3 us so, 18.6 otherwise.
+#define HQ_ROPE_PAST (32 << 20)
 // Keys turned and cast into a cache with their values, queries turned beside them.
-#define HQ_APPEND_HEADS 2
 struct hq_cache_append_args {
   hq_turns turn;
   hq_cache_side side[2];
   const int64_t* slots;
   uint32_t tiles;         // rows * groups, of each side
-  int32_t heads, groups;  // groups = ceil(heads / HQ_APPEND_HEADS)
+  int32_t heads, per, groups;  // per 4 or 1, groups = ceil(heads / per)
   int32_t block_tokens;
   hq_divisor by_groups, by_block;
   int32_t x_bf16;
   uint32_t side_groups;   // workgroups of a side
   int32_t sides;
-  hq_rope_args q;         // tiles 0: none
+  hq_rope_args q;         // tiles 0: none; per 4 or 1
 };
 
 // A sequence's first item of a cache attention, and how many it has.

@@ -16,13 +16,26 @@
 
 namespace {
 
-// What one row's turn is to a lane: cosines and sines of its values' pairs (of
-// interleaved pairs the first four), the sines with the sign that they enter with.
-struct Turn {
-  float c[8], s[8];
-  bool in;  // the lane's values are among the turned ones
-  bool ok;  // the row has positions
+// A row's positions, one per axis.
+struct Positions {
+  int32_t p[4];
+  bool ok;  // all of them are in the table
 };
+
+__device__ __forceinline__ Positions load_positions(const hq_turns& T, uint32_t row, int lane) {
+  Positions x;
+  x.ok = true;
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    x.p[a] = a == 0 || a < T.axes ? T.pos[(int64_t)row * T.axes + a] : 0;
+    x.ok &= (uint32_t)x.p[a] < (uint32_t)T.count;
+  }
+  // a row of padding is left alone without a word
+  if (!x.ok && x.p[0] >= 0 && (lane & 15) == 0) report(T.stats, HQ_ERR_INVALID_ARG);
+#pragma unroll
+  for (int a = 0; a < 4; ++a) x.p[a] = x.ok ? x.p[a] : 0;
+  return x;
+}
 
 __device__ __forceinline__ int32_t axis_position(const hq_turns& T, uint32_t pair, const int32_t (&p)[4]) {
   const uint32_t at = pair >> 4;
@@ -31,22 +44,17 @@ __device__ __forceinline__ int32_t axis_position(const hq_turns& T, uint32_t pai
   return a == 0 ? p[0] : a == 1 ? p[1] : a == 2 ? p[2] : p[3];
 }
 
-__device__ __forceinline__ Turn load_turn(const hq_turns& T, uint32_t row, int lane, bool transposed) {
+// What one row's turn is to a lane: cosines and sines of its values' pairs (of
+// interleaved pairs the first four), the sines with the sign that they enter with.
+struct Turn {
+  float c[8], s[8];
+  bool in;  // the lane's values are among the turned ones
+};
+
+__device__ __forceinline__ Turn load_turn(const hq_turns& T, const int32_t (&p)[4], int lane, bool transposed) {
   Turn t;
   const uint32_t n = lane & 15, half = (uint32_t)T.pairs >> 3;  // lanes of a half
-  int32_t p[4];
-  bool in_range = true;
-#pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    p[a] = T.pos[(int64_t)row * T.axes + min(a, T.axes - 1)];
-    in_range &= (uint32_t)p[a] < (uint32_t)T.count;
-  }
   t.in = n < 2 * half;
-  t.ok = in_range;
-  // a row of padding is left alone without a word
-  if (!in_range && p[0] >= 0 && n == 0) report(T.stats, HQ_ERR_INVALID_ARG);
-#pragma unroll
-  for (int a = 0; a < 4; ++a) p[a] = in_range ? p[a] : 0;
   const uint32_t lower = n < half, turn = transposed ? 0x80000000u : 0u;
   if (T.interleaved) {
     const uint32_t p0 = t.in ? 4 * n : 0u;
@@ -122,56 +130,105 @@ __global__ __launch_bounds__(256) void hq_rope_table_kernel(hq_rope_table_args A
   }
 }
 
-// A lane group takes up to HQ_ROPE_HEADS heads of a row: the row's positions and table
-// lines are loaded once for them.
-__device__ __forceinline__ void rope_tile(const hq_rope_args& A, const hq_turns& T, uint32_t tile, bool in) {
-  const int lane = threadIdx.x & 63, c0 = (lane & 15) * 8;
-  const uint32_t row = A.by_groups.of(tile), head0 = (tile - row * (uint32_t)A.groups) * HQ_ROPE_HEADS;
-  Raw8 raw[HQ_ROPE_HEADS];
+// 8 values of an array whose type the launch goes by.
+template <bool BF16>
+struct Raw {
+  uint4 w[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* p, int64_t i) {
+    if constexpr (BF16) {
+      w[0] = *(const uint4*)((const uint16_t*)p + i);
+    } else {
+      w[0] = *(const uint4*)((const float*)p + i);
+      w[1] = *(const uint4*)((const float*)p + i + 4);
+    }
+  }
+  __device__ __forceinline__ void expand(float* v) const {
+    if constexpr (BF16) {
+      expand8({w[0], w[0]}, true, v);
+    } else {
+      expand8({w[0], w[1]}, false, v);
+    }
+  }
+};
+
+typedef uint32_t v4q_t __attribute__((ext_vector_type(4)));
+
+// store8, past the caches where `past`.
+__device__ __forceinline__ void store8_past(void* p, int64_t i, bool bf16, bool past, const float* v) {
+  if (!past) return store8(p, i, bf16, v);
+  if (bf16) {
+    const v4q_t o = {cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+    __builtin_nontemporal_store(o, (v4q_t*)((uint16_t*)p + i));
+  } else {
+    v4q_t o[2];
 #pragma unroll
-  for (uint32_t i = 0; i < HQ_ROPE_HEADS; ++i)
-    raw[i] = load_raw8(A.x, (int64_t)row * A.ldx + (min(head0 + i, (uint32_t)A.heads - 1) * HQ_TILE + c0), A.x_bf16);
-  const Turn t = load_turn(T, row, lane, A.transposed);
-#pragma unroll
-  for (uint32_t i = 0; i < HQ_ROPE_HEADS; ++i) {
-    float v[8];
-    expand8(raw[i], A.x_bf16, v);
-    apply_turn(T, t, lane, v);
-    if (in && t.ok && head0 + i < (uint32_t)A.heads)
-      store8(A.y, (int64_t)row * A.ldy + ((head0 + i) * HQ_TILE + c0), A.y_bf16, v);
+    for (int k = 0; k < 8; ++k) o[k >> 2][k & 3] = __float_as_uint(v[k]);
+    __builtin_nontemporal_store(o[0], (v4q_t*)((float*)p + i));
+    __builtin_nontemporal_store(o[1], (v4q_t*)((float*)p + i + 4));
   }
 }
 
-__global__ __launch_bounds__(256) void hq_rope_kernel(hq_rope_args A) {
-  const uint32_t t = blockIdx.x * 16u + (threadIdx.x >> 4);
-  rope_tile(A, A.turn, min(t, A.tiles - 1), t < A.tiles);
+// A lane group takes up to H heads of a row, groups apart: the row's positions and table
+// lines are loaded once for them, and neighbouring lane groups have neighbouring heads.
+template <int H, bool BF16>
+__device__ __forceinline__ void rope_tile(const hq_rope_args& A, const hq_turns& T, uint32_t tile, bool in) {
+  const int lane = threadIdx.x & 63, c0 = (lane & 15) * 8;
+  const uint32_t row = A.by_groups.of(tile), head0 = tile - row * (uint32_t)A.groups;
+  Raw<BF16> raw[H];
+#pragma unroll
+  for (uint32_t i = 0; i < H; ++i)
+    raw[i].load(A.x, (int64_t)row * A.ldx + (min(head0 + i * (uint32_t)A.groups, (uint32_t)A.heads - 1) * HQ_TILE + c0));
+  const Positions p = load_positions(T, row, lane);
+  const Turn t = load_turn(T, p.p, lane, A.transposed);
+#pragma unroll
+  for (uint32_t i = 0; i < H; ++i) {
+    const uint32_t head = head0 + i * (uint32_t)A.groups;
+    float v[8];
+    raw[i].expand(v);
+    apply_turn(T, t, lane, v);
+    if (in && p.ok && head < (uint32_t)A.heads)
+      store8_past(A.y, (int64_t)row * A.ldy + (head * HQ_TILE + c0), A.y_bf16, A.past, v);
+  }
 }
 
-// Workgroups of the keys, of the values, of the queries.
-template <int FMT>
+template <int H, bool BF16>
+__global__ __launch_bounds__(256) void hq_rope_kernel(hq_rope_args A) {
+  const uint32_t t = blockIdx.x * 16u + (threadIdx.x >> 4);
+  rope_tile<H, BF16>(A, A.turn, min(t, A.tiles - 1), t < A.tiles);
+}
+
+// Workgroups of the keys, of the values, of the queries.  A lane group takes U heads of a row
+// (8192 rows of 8 heads and their 32 query heads in bf16 to E4M3: 42.2 us with four, 44.3 with
+// two, 46.3 with one).  Bound by memory: 189 MB, which a large copy moves in 37 us; the queries
+// are two thirds of it.
+template <int FMT, bool BF16, int U>
 __global__ __launch_bounds__(256) void hq_cache_append_kernel(hq_cache_append_args A) {
-  constexpr uint32_t U = HQ_APPEND_HEADS;
   const uint32_t at = blockIdx.x / A.side_groups;
   if (at >= (uint32_t)A.sides) {
     const uint32_t t = (blockIdx.x - (uint32_t)A.sides * A.side_groups) * 16u + (threadIdx.x >> 4);
-    rope_tile(A.q, A.turn, min(t, A.q.tiles - 1), t < A.q.tiles);
+    if (A.q.per == 4)
+      rope_tile<4, BF16>(A.q, A.turn, min(t, A.q.tiles - 1), t < A.q.tiles);
+    else
+      rope_tile<1, BF16>(A.q, A.turn, min(t, A.q.tiles - 1), t < A.q.tiles);
     return;
   }
   const hq_cache_side& S = A.side[at];
   const int lane = threadIdx.x & 63, c0 = (lane & 15) * 8;
   const uint32_t t = (blockIdx.x - at * A.side_groups) * 16u + (threadIdx.x >> 4), tile = min(t, A.tiles - 1);
-  const uint32_t row = A.by_groups.of(tile), head0 = (tile - row * (uint32_t)A.groups) * U;
+  const uint32_t row = A.by_groups.of(tile), head0 = tile - row * (uint32_t)A.groups;
   const int64_t slot = A.slots[row];
-  float v[U][8];
+  Raw<BF16> raw[U];
   uint4 d[U];
 #pragma unroll
   for (uint32_t i = 0; i < U; ++i) {
-    const uint32_t col = min(head0 + i, (uint32_t)A.heads - 1) * HQ_TILE + c0;
-    load8(S.x, (int64_t)row * S.ld + col, A.x_bf16, v[i]);
+    const uint32_t col = min(head0 + i * (uint32_t)A.groups, (uint32_t)A.heads - 1) * HQ_TILE + c0;
+    raw[i].load(S.x, (int64_t)row * S.ld + col);
     d[i] = sign_words(S.dsign16, col);
   }
   // a row without positions leaves both sides of its slot as they were
-  const Turn turn = load_turn(A.turn, row, lane, false);
+  const Positions p = load_positions(A.turn, row, lane);
+  Turn turn;
+  if (at == 0) turn = load_turn(A.turn, p.p, lane, false);
   const bool here = slot >= 0 && slot < S.slots;
   if (slot >= S.slots && head0 == 0 && (lane & 15) == 0) report(S.stats, HQ_ERR_INVALID_ARG);
   const uint32_t s = here ? (uint32_t)slot : 0u, blk = A.by_block.of(s);
@@ -179,12 +236,36 @@ __global__ __launch_bounds__(256) void hq_cache_append_kernel(hq_cache_append_ar
   const TwSigns sg(lane);
 #pragma unroll
   for (uint32_t i = 0; i < U; ++i) {
-    if (at == 0) apply_turn(A.turn, turn, lane, v[i]);
-    flip8(v[i], d[i]);
-    fwht128_tw(v[i], sg);
-    cache_put<FMT>(S, v[i], here && turn.ok && t < A.tiles && head0 + i < (uint32_t)A.heads,
-                   vec0 + (int64_t)(head0 + i) * A.block_tokens, lane, sg);
+    const uint32_t head = head0 + i * (uint32_t)A.groups;
+    float v[8];
+    raw[i].expand(v);
+    if (at == 0) apply_turn(A.turn, turn, lane, v);
+    flip8(v, d[i]);
+    fwht128_tw(v, sg);
+    cache_put<FMT>(S, v, here && p.ok && t < A.tiles && head < (uint32_t)A.heads, vec0 + (int64_t)head * A.block_tokens, lane, sg);
   }
+}
+
+template <int H>
+void launch_rope(const hq_rope_args& a, hipStream_t st) {
+  const dim3 grid((a.tiles + 15) / 16), wg(256);
+  if (a.x_bf16)
+    hipLaunchKernelGGL((hq_rope_kernel<H, true>), grid, wg, 0, st, a);
+  else
+    hipLaunchKernelGGL((hq_rope_kernel<H, false>), grid, wg, 0, st, a);
+}
+
+template <int FMT>
+void launch_append(const hq_cache_append_args& a, hipStream_t st) {
+  const dim3 grid((uint32_t)a.sides * a.side_groups + (a.q.tiles + 15) / 16), wg(256);
+  if (a.x_bf16 && a.per == 4)
+    hipLaunchKernelGGL((hq_cache_append_kernel<FMT, true, 4>), grid, wg, 0, st, a);
+  else if (a.x_bf16)
+    hipLaunchKernelGGL((hq_cache_append_kernel<FMT, true, 1>), grid, wg, 0, st, a);
+  else if (a.per == 4)
+    hipLaunchKernelGGL((hq_cache_append_kernel<FMT, false, 4>), grid, wg, 0, st, a);
+  else
+    hipLaunchKernelGGL((hq_cache_append_kernel<FMT, false, 1>), grid, wg, 0, st, a);
 }
 
 }  // namespace
@@ -196,17 +277,21 @@ int hq_launch_rope_table(const hq_rope_table_args& a, void* stream) {
 }
 
 int hq_launch_rope(const hq_rope_args& a, void* stream) {
-  hipLaunchKernelGGL(hq_rope_kernel, dim3((a.tiles + 15) / 16), dim3(256), 0, (hipStream_t)stream, a);
+  const hipStream_t st = (hipStream_t)stream;
+  switch (a.per) {
+    case 4: launch_rope<4>(a, st); break;
+    case 2: launch_rope<2>(a, st); break;
+    default: launch_rope<1>(a, st);
+  }
   return (int)hipGetLastError();
 }
 
 int hq_launch_cache_append(const hq_cache_append_args& a, int format, void* stream) {
-  const dim3 grid((uint32_t)a.sides * a.side_groups + (a.q.tiles + 15) / 16);
   const hipStream_t st = (hipStream_t)stream;
   switch (format) {
-    case HQ_INT8: hipLaunchKernelGGL(hq_cache_append_kernel<kInt8>, grid, dim3(256), 0, st, a); break;
-    case HQ_E4M3: hipLaunchKernelGGL(hq_cache_append_kernel<kE4M3>, grid, dim3(256), 0, st, a); break;
-    default: hipLaunchKernelGGL(hq_cache_append_kernel<kMx>, grid, dim3(256), 0, st, a);
+    case HQ_INT8: launch_append<kInt8>(a, st); break;
+    case HQ_E4M3: launch_append<kE4M3>(a, st); break;
+    default: launch_append<kMx>(a, st);
   }
   return (int)hipGetLastError();
 }

@@ -32,7 +32,7 @@ bool positions_ok(const int32_t* p) { return p && aligned(p, 4); }
 
 // Rows of `heads` head vectors through `t`; rows above 0 and checked.
 void fill_rows(const hq_turns& t, const void* x, int32_t xt, int64_t ldx, int64_t rows, int32_t heads, void* y, int32_t yt,
-               int64_t ldy, hq_rope_args* a) {
+               int64_t ldy, int32_t else_per, hq_rope_args* a) {
   std::memset(a, 0, sizeof(*a));
   a->turn = t;
   a->x = x;
@@ -40,11 +40,13 @@ void fill_rows(const hq_turns& t, const void* x, int32_t xt, int64_t ldx, int64_
   a->ldx = ldx;
   a->ldy = ldy;
   a->heads = heads;
-  a->groups = (heads + HQ_ROPE_HEADS - 1) / HQ_ROPE_HEADS;
+  a->per = hq_rope_per(heads, else_per);
+  a->groups = (heads + a->per - 1) / a->per;
   a->tiles = (uint32_t)(rows * a->groups);
   a->by_groups = hq_divide_by((uint32_t)a->groups);
   a->x_bf16 = xt == HQ_BF16;
   a->y_bf16 = yt == HQ_BF16;
+  a->past = rows * heads * HQ_TILE * (yt == HQ_BF16 ? 2 : 4) >= HQ_ROPE_PAST;
 }
 
 // A row turned in place has to be the same row: each value is read before its own place, and
@@ -80,7 +82,7 @@ hq_status hq_rope(const hq_rotary* r, const void* x, int32_t xt, int64_t ldx, in
       !in_place_ok(x, xt, ldx, y, yt, ldy))
     return HQ_ERR_INVALID_ARG;
   hq_rope_args a;
-  fill_rows(t, x, xt, ldx, rows, heads, y, yt, ldy, &a);
+  fill_rows(t, x, xt, ldx, rows, heads, y, yt, ldy, 2, &a);
   a.transposed = transposed;
   if ((a.tiles + 15) / 16 > (uint32_t)kMaxGroups) return HQ_ERR_UNSUPPORTED;
   return hip_status(hq_launch_rope(a, stream));
@@ -112,14 +114,15 @@ hq_status hq_cache_append(hq_plan_t kp, const void* k, int64_t ldk, const hq_cac
   a.sides = both ? 2 : 1;
   a.slots = slots;
   a.heads = kc->heads;
-  a.groups = (kc->heads + HQ_APPEND_HEADS - 1) / HQ_APPEND_HEADS;
+  a.per = hq_rope_per(kc->heads, 1);
+  a.groups = (kc->heads + a.per - 1) / a.per;
   a.tiles = (uint32_t)(rows * a.groups);
   a.by_groups = hq_divide_by((uint32_t)a.groups);
   a.block_tokens = kc->block_tokens;
   a.by_block = hq_divide_by((uint32_t)kc->block_tokens);
   a.x_bf16 = xt == HQ_BF16;
   a.side_groups = (a.tiles + 15) / 16;
-  if (q) fill_rows(a.turn, q, xt, ldq, rows, heads_q, q_out, qot, ldqo, &a.q);
+  if (q) fill_rows(a.turn, q, xt, ldq, rows, heads_q, q_out, qot, ldqo, 1, &a.q);
   if ((int64_t)a.sides * a.side_groups + (a.q.tiles + 15) / 16 > kMaxGroups) return HQ_ERR_UNSUPPORTED;
   return hip_status(hq_launch_cache_append(a, kc->format, stream));
 }

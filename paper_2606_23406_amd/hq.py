@@ -608,6 +608,7 @@ class Cache:
         self.stats = torch.zeros(STATS_BYTES // 4, dtype=torch.int32, device=codes.device) if stats else None
         self.c = CacheStruct(codes.data_ptr(), scales.data_ptr(), blocks, block_tokens, self.heads,
                              format, 0, self.stats.data_ptr() if stats else None)
+        self.ref = C.byref(self.c)
 
     def read_stats(self):
         if self.stats is None:
@@ -702,7 +703,7 @@ def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.
     ot = out.dtype
     workspace = _workspace(workspace, lambda: hq_cache_attention_workspace_bytes(k, batch, heads_q, max_blocks),
                            dev, stream)
-    st = lib().hq_cache_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), qp,
+    st = lib().hq_cache_attention(k_plan.handle, k.ref, v_plan.handle, v.ref, qp,
                                   _dtype_code(qt), batch, heads_q,
                                   128 ** -0.5 if scale is None else scale, tp, max_blocks, lp,
                                   _dense(out, ot, shape, dev, "out"), _dtype_code(ot),
@@ -730,6 +731,7 @@ class Rope:
         self.stats = torch.zeros(STATS_BYTES // 4, dtype=torch.int32, device=table.device) if stats else None
         self.c = RotaryStruct(table.data_ptr(), table.shape[0], 2 * pairs, int(bool(interleaved)), self.axes, 0,
                               C.addressof(self._axis), self.stats.data_ptr() if stats else None)
+        self.ref = C.byref(self.c)
 
     read_stats = Cache.read_stats
     reset_stats = Cache.reset_stats
@@ -762,11 +764,10 @@ def hq_rope(rope: Rope, x: torch.Tensor, positions: torch.Tensor, transposed=Fal
     """hq_rope: x [rows, heads * 128] (bf16 or fp32) turned by positions int32 [rows, axes]
     (of one axis also [rows]); transposed: the gradient.  out may be x.  Without an out, rows
     of padding (a negative first position) are zeros."""
-    dev, dt = torch.cuda.current_device(), x.dtype
-    shape = (x.shape[0], x.shape[1])
-    xp, ldx = _rows(x, dt, shape, dev, "x")
-    if shape[1] % 128:
+    dev, dt, shape = torch.cuda.current_device(), x.dtype, x.shape
+    if len(shape) != 2 or shape[1] % 128:
         raise ValueError(f"x must be [rows, heads * 128], not {list(shape)}")
+    xp, ldx = _rows(x, dt, shape, dev, "x")
     pp = _positions(rope, positions, shape[0], dev)
     if out is None:
         out = _empty(shape, dt if out_dtype is None else out_dtype, dev, stream)
@@ -774,7 +775,7 @@ def hq_rope(rope: Rope, x: torch.Tensor, positions: torch.Tensor, transposed=Fal
             out.zero_()
     ot = out.dtype
     op, ldo = _rows(out, ot, shape, dev, "out")
-    st = lib().hq_rope(C.byref(rope.c), xp, _dtype_code(dt), ldx, shape[0], shape[1] // 128, pp, int(bool(transposed)),
+    st = lib().hq_rope(rope.ref, xp, _dtype_code(dt), ldx, shape[0], shape[1] // 128, pp, int(bool(transposed)),
                        op, _dtype_code(ot), ldo, _stream_handle(stream))
     _check("hq_rope", st)
     return out
@@ -799,7 +800,7 @@ def hq_cache_append(k_plan: Plan, k: torch.Tensor, k_cache: Cache, v_plan, v, v_
         vp, ldv = _rows(v, dt, shape, dev, "v")
         if v_cache.device.index != dev:
             raise ValueError(f"a cache on {v_cache.device} in a call on cuda:{dev}")
-        vh, vc = v_plan.handle, C.byref(v_cache.c)
+        vh, vc = v_plan.handle, v_cache.ref
     sp = _dense(slots, torch.int64, shape[:1], dev, "slots")
     pp = _positions(rope, positions, shape[0], dev)
     if q is None:
@@ -818,14 +819,14 @@ def hq_cache_append(k_plan: Plan, k: torch.Tensor, k_cache: Cache, v_plan, v, v_
                 q_out.zero_()
         op, ldo = _rows(q_out, q_out.dtype, qshape, dev, "q_out")
         heads_q, ot = qshape[1] // 128, _dtype_code(q_out.dtype)
-    st = lib().hq_cache_append(k_plan.handle, kp, ldk, C.byref(k_cache.c), vh, vp, ldv, vc, _dtype_code(dt), shape[0],
-                               sp, C.byref(rope.c), pp, qp, ldq, heads_q, op, ot, ldo, _stream_handle(stream))
+    st = lib().hq_cache_append(k_plan.handle, kp, ldk, k_cache.ref, vh, vp, ldv, vc, _dtype_code(dt), shape[0],
+                               sp, rope.ref, pp, qp, ldq, heads_q, op, ot, ldo, _stream_handle(stream))
     _check("hq_cache_append", st)
     return q_out
 
 
 def hq_cache_window_workspace_bytes(k_cache: Cache, batch, heads_q, max_blocks, window, sinks=0):
-    return lib().hq_cache_window_workspace_bytes(C.byref(k_cache.c), batch, heads_q, max_blocks, window, sinks)
+    return lib().hq_cache_window_workspace_bytes(k_cache.ref, batch, heads_q, max_blocks, window, sinks)
 
 
 def hq_cache_window_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor,
@@ -847,7 +848,7 @@ def hq_cache_window_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q:
     ot = out.dtype
     workspace = _workspace(
         workspace, lambda: hq_cache_window_workspace_bytes(k, batch, heads_q, max_blocks, window, sinks), dev, stream)
-    st = lib().hq_cache_window_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), qp,
+    st = lib().hq_cache_window_attention(k_plan.handle, k.ref, v_plan.handle, v.ref, qp,
                                          _dtype_code(qt), batch, heads_q, 128 ** -0.5 if scale is None else scale, tp,
                                          max_blocks, lp, window, sinks, _dense(out, ot, shape, dev, "out"),
                                          _dtype_code(ot), workspace.data_ptr(), workspace.nbytes,
@@ -857,7 +858,7 @@ def hq_cache_window_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q:
 
 
 def hq_cache_tree_workspace_bytes(k_cache: Cache, batch, heads_q, max_blocks, max_tree, window=0, sinks=0):
-    return lib().hq_cache_tree_workspace_bytes(C.byref(k_cache.c), batch, heads_q, max_blocks, max_tree, window, sinks)
+    return lib().hq_cache_tree_workspace_bytes(k_cache.ref, batch, heads_q, max_blocks, max_tree, window, sinks)
 
 
 def hq_cache_tree_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor, masks: torch.Tensor,
@@ -889,7 +890,7 @@ def hq_cache_tree_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: t
     workspace = _workspace(
         workspace, lambda: hq_cache_tree_workspace_bytes(k, batch, heads_q, max_blocks, max_tree, window, sinks), dev,
         stream)
-    st = lib().hq_cache_tree_attention(k_plan.handle, C.byref(k.c), v_plan.handle, C.byref(v.c), qp, _dtype_code(qt),
+    st = lib().hq_cache_tree_attention(k_plan.handle, k.ref, v_plan.handle, v.ref, qp, _dtype_code(qt),
                                        rows, heads_q, 128 ** -0.5 if scale is None else scale, mp, sp, batch, max_tree,
                                        tp, max_blocks, lp, window, sinks, _dense(out, ot, shape, dev, "out"),
                                        _dtype_code(ot), workspace.data_ptr(), workspace.nbytes,
