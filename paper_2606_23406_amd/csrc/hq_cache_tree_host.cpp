@@ -91,7 +91,7 @@ hq_status hq_cache_tree_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp,
   a.join = s.seen > HQ_CACHE_WHOLE;
   // workgroups of both launches
   if (s.items > kMaxGroups / k->heads ||
-      s.joins * (((int64_t)max_tree * heads_q + 15) / 16) > kMaxGroups)
+      s.joins * (((int64_t)max_tree * heads_q + 3) / 4) > kMaxGroups)
     return HQ_ERR_UNSUPPORTED;
   if (a.join && (!workspace || !aligned(workspace, 16) || ws_bytes < s.bytes)) return HQ_ERR_INVALID_ARG;
   if ((st = check_device(kp)) != HQ_OK || (st = check_device(vp)) != HQ_OK) return st;
