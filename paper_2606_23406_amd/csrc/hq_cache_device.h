@@ -188,7 +188,7 @@ constexpr int kAll = 0, kWindow = 1, kTree = 2;
 struct CacheSpan {
   int32_t len;         // 0: nothing
   int32_t low, sinks;  // sinks <= low
-  int32_t rows;        // drafted tokens
+  int32_t rows, from;  // drafted tokens, and the first one's row
   __device__ __forceinline__ int32_t turn() const { return (sinks + 15) & ~15; }
   __device__ __forceinline__ int32_t gap() const { return max((low & ~15) - turn(), 0); }
   __device__ __forceinline__ int32_t seen() const { return len - gap(); }
@@ -200,8 +200,8 @@ struct CacheSpan {
 };
 
 template <int MODE>
-__device__ __forceinline__ CacheSpan cache_span(const hq_cache_attn_args& A, int32_t len, int32_t rows) {
-  CacheSpan s = {len, 0, 0, rows};
+__device__ __forceinline__ CacheSpan cache_span(const hq_cache_attn_args& A, int32_t len, int32_t rows, int32_t from) {
+  CacheSpan s = {len, 0, 0, rows, from};
   if (MODE != kAll && A.window) {
     s.low = max(len - rows - A.window, 0);
     s.sinks = min(A.sinks, s.low);
@@ -212,9 +212,12 @@ __device__ __forceinline__ CacheSpan cache_span(const hq_cache_attn_args& A, int
 // Drafted tokens of sequence b (0 for the other modes).  Places that are out of order or range,
 // more tokens than the call's bound or than the sequence: reported, and none.
 template <int MODE>
-__device__ __forceinline__ int32_t cache_rows(const hq_cache_attn_args& A, int64_t b, int32_t len, bool tell) {
+__device__ __forceinline__ int32_t cache_rows(const hq_cache_attn_args& A, int64_t b, int32_t len, bool tell,
+                                              int32_t& from) {
+  from = 0;
   if (MODE != kTree) return 0;
-  const int32_t from = A.starts[b], to = A.starts[b + 1];
+  from = A.starts[b];
+  const int32_t to = A.starts[b + 1];
   const bool ok = from >= 0 && to >= from && to <= A.rows && to - from <= A.max_rows && to - from <= len;
   if (!ok && tell) report(A.stats, HQ_ERR_INVALID_ARG);
   return ok ? to - from : 0;
@@ -222,8 +225,9 @@ __device__ __forceinline__ int32_t cache_rows(const hq_cache_attn_args& A, int64
 
 template <int MODE>
 __device__ __forceinline__ CacheSpan cache_span_of(const hq_cache_attn_args& A, int64_t b, bool tell) {
-  const int32_t len = cache_len(A, b, tell), rows = cache_rows<MODE>(A, b, len, tell);
-  return cache_span<MODE>(A, MODE == kTree && rows == 0 ? 0 : len, rows);
+  int32_t from;
+  const int32_t len = cache_len(A, b, tell), rows = cache_rows<MODE>(A, b, len, tell, from);
+  return cache_span<MODE>(A, MODE == kTree && rows == 0 ? 0 : len, rows, from);
 }
 
 struct CacheItem {
@@ -293,7 +297,8 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.tile = MODE == kTree ? j - b * A.max_tiles : 0;
     const CacheSpan s = cache_span_of<MODE>(A, it.b, true);
     it.span = {(int32_t)readfirst((uint32_t)s.len), (int32_t)readfirst((uint32_t)s.low),
-               (int32_t)readfirst((uint32_t)s.sinks), (int32_t)readfirst((uint32_t)s.rows)};
+               (int32_t)readfirst((uint32_t)s.sinks), (int32_t)readfirst((uint32_t)s.rows),
+               (int32_t)readfirst((uint32_t)s.from)};
     it.chunk = HQ_CACHE_WHOLE;
     return it;
   }
@@ -314,11 +319,12 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.b = (int32_t)readfirst((uint32_t)lo);
     const CacheSpan s = cache_span_of<MODE>(A, it.b, false);
     it.span = {(int32_t)readfirst((uint32_t)s.len), (int32_t)readfirst((uint32_t)s.low),
-               (int32_t)readfirst((uint32_t)s.sinks), (int32_t)readfirst((uint32_t)s.rows)};
+               (int32_t)readfirst((uint32_t)s.sinks), (int32_t)readfirst((uint32_t)s.rows),
+               (int32_t)readfirst((uint32_t)s.from)};
   } else {
     static_assert(HQ_CACHE_UNPLANNED <= 64, "");
     const bool in = lane < A.batch;
-    const CacheSpan s = in ? cache_span_of<MODE>(A, lane, tell) : CacheSpan{-1, 0, 0, 0};
+    const CacheSpan s = in ? cache_span_of<MODE>(A, lane, tell) : CacheSpan{-1, 0, 0, 0, 0};
     const int32_t len = MODE == kAll ? s.len : s.seen();
     const int32_t tiles = cache_tiles<MODE>(A, s.rows);
     int64_t total = (int64_t)max(len, 0) * tiles;
@@ -333,7 +339,8 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     it.n = (int32_t)__builtin_amdgcn_readlane(n, at);
     it.first = __builtin_amdgcn_readlane(incl, at) - it.n * (int32_t)__builtin_amdgcn_readlane(tiles, at);
     it.span = cache_span<MODE>(A, __builtin_amdgcn_readlane(s.len, at),
-                               MODE == kTree ? __builtin_amdgcn_readlane(s.rows, at) : 0);
+                               MODE == kTree ? __builtin_amdgcn_readlane(s.rows, at) : 0,
+                               MODE == kTree ? __builtin_amdgcn_readlane(s.from, at) : 0);
   }
   if (MODE == kTree) {
     const int32_t tiles = cache_tiles<MODE>(A, it.span.rows);

@@ -442,7 +442,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     A.parts[it.b] = {it.first, it.n};
   const int32_t rows = it.span.rows, seen = it.span.seen(), tile = it.tile;
   if (tile * ROWS >= rows * A.group) return;  // none of this sequence's, or it has none at all
-  const int32_t from = A.starts[it.b];
+  const int32_t from = it.span.from;
   const int32_t begin0 = (int32_t)(it.at * it.chunk), tokens = min(it.chunk, seen - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
@@ -866,7 +866,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     A.parts[it.b] = {it.first, it.n};
   const int32_t rows = it.span.rows, seen = it.span.seen(), tile = it.tile;
   if (tile * ROWS >= rows * A.group) return;  // none of this sequence's, or it has none at all
-  const int32_t from = A.starts[it.b];
+  const int32_t from = it.span.from;
   const int32_t begin = (int32_t)(it.at * it.chunk), end = begin + min(it.chunk, seen - begin);
   TreeWay way;
   way.table = A.table + (int64_t)it.b * A.max_blocks;
