@@ -395,3 +395,46 @@ def test_a_drafted_step(hq, fmt, window, sinks):
         live = W.visible(n, window or n, sinks)[None]
         W.check(out[b:b + 1].cpu().numpy(), *W.attend(q[b:b + 1].float().cpu().numpy(), kv, vv, table[b].numpy(), live, bt, N ** -0.5,
                                                        heads, group))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_windows_of_many_long_sequences(hq, fmt):
+    """More sequences than a wave has lanes, split and joined, each looked at from its window on."""
+    rng = np.random.default_rng(20)
+    lens = np.maximum(rng.integers(-500, 3500, 90), 0)
+    lens[::5] = 3500
+    Case(hq, fmt, lens.tolist(), np.minimum(lens, rng.integers(0, 12, 90)).tolist(), 1, 4, 48, seed=20, pool=30, window=1500,
+         sinks=21, max_tree=12).check()
+
+
+@pytest.mark.parametrize("heads", [512, 600])
+def test_as_many_heads_as_workgroups(hq, heads):
+    """From 512 KV heads on no sequence is split, however long the table."""
+    Case(hq, "int8", [1100, 0, 1500, 3], [2, 0, 1, 3], heads, 1, 64, seed=heads, pool=12).check()
+
+
+def test_no_rows_and_no_sequences(hq):
+    c = Case(hq, "int8", [100, 30], [0, 0], 2, 2, 32, seed=21)
+    assert c.run().shape == (0, 4, N)
+    c = Case(hq, "int8", [100], [3], 2, 2, 32, seed=21)
+    empty = lambda *shape: torch.empty(shape, dtype=torch.int32, device="cuda")
+    out = torch.full((3, 4, N), 7.0, device="cuda")
+    hq.hq_cache_tree_attention(c.kp, c.kc, c.vp, c.vc, c.q.cuda(), W.mask_tensor(c.masks).cuda(), empty(1), 3, empty(0, 4), empty(0),
+                               out=out)
+    assert (out == 7).all()
+
+
+def test_two_calls_at_once(hq):
+    """Two calls on two streams over one cache, a workspace each."""
+    c = Case(hq, "int8", [3000, 1200], [30, 17], 4, 4, 64, seed=22)
+    want, streams, got = c.run(), [torch.cuda.Stream() for _ in range(2)], []
+    for _ in range(3):
+        torch.cuda.synchronize()
+        outs = [torch.empty_like(want) for _ in streams]
+        torch.cuda.synchronize()
+        for s, o in zip(streams, outs):
+            with torch.cuda.stream(s):
+                c.run(out=o)
+        torch.cuda.synchronize()
+        got += outs
+    assert all(torch.equal(o, want) for o in got)
