@@ -19,8 +19,6 @@
 // half as many products again and twice the instructions of cutting.)
 #include <hip/hip_runtime.h>
 
-#include <type_traits>
-
 #include "hq_cache_device.h"
 #include "hq_lds.h"
 
@@ -570,7 +568,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 // ---- many rows
 // Trees of more than 32 rows of a KV head: the codes are turned into fp16 once per workgroup
 // and not once per wave.  A workgroup goes through its tokens in tiles of 64, two steps of 32;
-// two waves turn a step's keys each, two its values, into LDS in the order that the products'
+// each wave turns the keys and values of 16 of them into LDS in the order that the products'
 // operands are read in, a tile ahead of the products; the codes of the tile after it are on
 // their way in registers meanwhile.  Each wave has 32 rows: of a tile of 128 rows each wave
 // takes both steps, of one of 64 two waves share the rows and take a step each.
@@ -584,79 +582,61 @@ struct TreeTile {
   // keys: [step][contraction step][lane] 16 bytes, dims 8 (2 s + l / 32) ..;  values: [step][group
   // of 32 dims][product][lane] 16 bytes, group d being dims 8 (l % 16) + 2 d + l / 16 % 2
   static constexpr int V = kTreeTile * HQ_TILE * 2, KS = 2 * V, VS = KS + 4 * kTreeTile, SEEN = VS + 4 * kTreeTile;
-  static constexpr int BYTES = SEEN + 2 * 16 + 480;  // a multiple of 1 KB
+  static constexpr int BYTES = SEEN + 4 * 16 + 448;  // a multiple of 1 KB
 };
 
-// What a wave of the tile's loads holds: a step's keys or values of 32 tokens.
+// A wave's 16 tokens of a tile on their way: lane l has 32 codes of key l % 16 (run l / 16) and 8
+// dims (8 (l % 16) ..) of the four values 8 (l / 32) + 4 (l / 16 % 2) + r.
 template <int FMT>
 struct TreeLoads {
   static constexpr int KW = FMT == kMx ? 4 : 8, VW = FMT == kMx ? 1 : 2;
-  uint32_t w[2][8];    // keys: half, words of lane's 32 codes (token lane % 16, run lane / 16);
-                       // values: VW words of each of the tokens 16 (lane / 32) + 4 (lane / 16 % 2) + 8 q + r,
-                       // dims 8 (lane % 16) ..
-  uint32_t scale[2];   // keys: half's token lane % 16; values: [0] token lane % 32
-  int32_t live[2];     // bits of tokens that anybody sees
+  uint32_t k[KW], v[4][VW];
+  uint32_t ks, vs;  // scales of token l % 16
+  int32_t live;     // bits of tokens that anybody sees
 };
 
-// A wave's way over its halves of a workgroup's tiles.
+// A wave's way over its tokens of a workgroup's tiles.
 struct TreeWay {
   const int32_t* table;
   CacheSpan span;
   int32_t gap, jump, head, last;  // last: the sequence's last block
-  int32_t id[2];                  // block ids of the next tile's halves, on their way
+  int32_t id;                     // the next tile's block, on its way
   __device__ __forceinline__ int32_t real(int32_t t) const { return t < jump ? t : t + gap; }
   __device__ __forceinline__ void ask(const hq_cache_attn_args& A, int32_t t) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) id[h] = table[min((int32_t)A.by_block.of((uint32_t)real(t + 16 * h)), last)];
+    id = table[min((int32_t)A.by_block.of((uint32_t)real(t)), last)];
   }
-  // Starts the loads of the 32 tokens from t on, whose ids have been asked for, and asks for
-  // those of the tile behind.
-  template <int FMT, bool KEYS>
+  // Starts the loads of the 16 tokens from t on, whose block has been asked for, and asks for
+  // that of the tile behind.
+  template <int FMT>
   __device__ __forceinline__ void load(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, TreeLoads<FMT>& x) {
     constexpr int RB = row_bytes<FMT>();
-    const uint8_t* codes = KEYS ? A.k_codes : A.v_codes;
-    const uint32_t* scales = (const uint32_t*)(KEYS ? A.k_scales : A.v_scales);
     const int n = lane & 15, g = lane >> 4;
-    int64_t row[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int32_t at = real(t + 16 * h), blk = (int32_t)readfirst((uint32_t)id[h]);
-      const bool in = t + 16 * h < end, bad = (uint32_t)blk >= (uint32_t)A.blocks;
-      if (KEYS && in && bad && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
-      x.live[h] = in && !bad ? (int32_t)span.bits(at) : 0;
-      // a half that nobody sees: the cache's first tokens
-      const int32_t off = at - (int32_t)A.by_block.of((uint32_t)at) * A.block_tokens;
-      row[h] = x.live[h] ? ((int64_t)blk * A.heads_kv + head) * A.block_tokens + off : 0;
-    }
+    const int32_t at = real(t), blk = (int32_t)readfirst((uint32_t)id);
+    const bool in = t < end, bad = (uint32_t)blk >= (uint32_t)A.blocks;
+    if (in && bad && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
+    x.live = in && !bad ? (int32_t)span.bits(at) : 0;
+    // 16 tokens that nobody sees: the cache's first ones
+    const int32_t off = at - (int32_t)A.by_block.of((uint32_t)at) * A.block_tokens;
+    const int64_t row = x.live ? ((int64_t)blk * A.heads_kv + head) * A.block_tokens + off : 0;
     ask(A, t + kTreeTile);
+    const uint8_t* k = A.k_codes + row * RB + n * RB + g * (RB / 4);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint8_t* from = codes + row[h] * RB;
-      if constexpr (KEYS) {
+    for (int i = 0; i < TreeLoads<FMT>::KW; i += 4) {
+      const uint4 w = *(const uint4*)(k + 4 * i);
+      x.k[i] = w.x; x.k[i + 1] = w.y; x.k[i + 2] = w.z; x.k[i + 3] = w.w;
+    }
+    const uint8_t* v = A.v_codes + row * RB + (8 * (g >> 1) + 4 * (g & 1)) * RB + n * (RB / 16);
 #pragma unroll
-        for (int i = 0; i < TreeLoads<FMT>::KW; i += 4) {
-          const uint4 v = *(const uint4*)(from + n * RB + g * (RB / 4) + 4 * i);
-          x.w[h][i] = v.x; x.w[h][i + 1] = v.y; x.w[h][i + 2] = v.z; x.w[h][i + 3] = v.w;
-        }
-        x.scale[h] = scales[row[h] + n];
+    for (int r = 0; r < 4; ++r) {
+      if constexpr (FMT == kMx) {
+        x.v[r][0] = *(const uint32_t*)(v + r * RB);
+      } else {
+        const uint2 w = *(const uint2*)(v + r * RB);
+        x.v[r][0] = w.x; x.v[r][1] = w.y;
       }
     }
-    if constexpr (!KEYS) {
-      const uint8_t* from = codes + (lane < 32 ? row[0] : row[1]) * RB + (g & 1) * 4 * RB + n * (RB / 16);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const uint8_t* at = from + (8 * h + r) * RB;
-          if constexpr (FMT == kMx) {
-            x.w[h][r] = *(const uint32_t*)at;
-          } else {
-            const uint2 v = *(const uint2*)at;
-            x.w[h][2 * r] = v.x; x.w[h][2 * r + 1] = v.y;
-          }
-        }
-      x.scale[0] = x.scale[1] = scales[(lane & 16 ? row[1] : row[0]) + n];
-    }
+    x.ks = ((const uint32_t*)A.k_scales)[row + n];
+    x.vs = ((const uint32_t*)A.v_scales)[row + n];
   }
 };
 
@@ -674,95 +654,81 @@ __device__ __forceinline__ uint32_t token_scale(uint32_t w) {
   }
 }
 
-// The largest of lanes 0 .. 31's values, which lanes 32 on have too.
-__device__ __forceinline__ float half_wave_max(float x) {
+// The largest of 16 neighbouring lanes' values.
+__device__ __forceinline__ float row_max(float x) {
   x = __builtin_fmaxf(x, dpp_xor<1>(x));
   x = __builtin_fmaxf(x, dpp_xor<2>(x));
   x = __builtin_fmaxf(x, swz_xor4(x));
-  x = __builtin_fmaxf(x, dpp_xor<8>(x));
-  const v2u_t a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __builtin_fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  return __builtin_fmaxf(x, dpp_xor<8>(x));
 }
 
-// A step's keys as fp16 into a tile.
+// The 16 tokens as fp16 into a tile, where they are its `group`-th, with their scales and what
+// the products go by: the value scales' largest and least, and the tokens that anybody sees.
 template <int FMT>
-__device__ __forceinline__ void turn_keys(const TreeLoads<FMT>& x, uint8_t* tile, int step, int lane) {
-  const int n = lane & 15, g = lane >> 4;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint32_t scale = token_scale<FMT>(x.scale[h]);
-    const float f = FMT == kMx ? below_scale((x.scale[h] >> (8 * g)) & 0xFFu, __uint_as_float(scale)) : 1.0f;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      uint32_t o[4];
-      if constexpr (FMT == kMx) {
-        dims_of<FMT>(x.w[h][s], f, o);
-      } else {
-        dims_of<FMT>(x.w[h][2 * s], 1.0f, o);
-        dims_of<FMT>(x.w[h][2 * s + 1], 1.0f, o + 2);
-      }
-      // dims 8 (4 g + s) ..
-      *(uint4*)(tile + ((step * 8 + 2 * g + s / 2) * 64 + (s & 1) * 32 + 16 * h + n) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
-    }
-    if (g == 0) *(uint32_t*)(tile + TreeTile<FMT>::KS + (step * 32 + 16 * h + n) * 4) = scale;
-  }
-}
-
-// A step's values as fp16 into a tile, their scales, and what the products go by: the largest
-// scale's lift, the tokens that anybody sees, whether one lift does.
-template <int FMT>
-__device__ __forceinline__ void turn_values(TreeLoads<FMT>& x, uint8_t* tile, int step, int lane) {
+__device__ __forceinline__ void turn(TreeLoads<FMT>& x, uint8_t* tile, int group, int lane) {
+  using T = TreeTile<FMT>;
   constexpr int VW = TreeLoads<FMT>::VW, D = 8 / VW;
-  const int n = lane & 15, g = lane >> 4;
-  uint32_t scale = token_scale<FMT>(x.scale[0]);
-  float f[2][4];
+  const int n = lane & 15, g = lane >> 4, step = group >> 1, h = group & 1;
+  const uint32_t ks = token_scale<FMT>(x.ks);
+  uint32_t vs = token_scale<FMT>(x.vs);
+  const float kf = FMT == kMx ? below_scale((x.ks >> (8 * g)) & 0xFFu, __uint_as_float(ks)) : 1.0f;
+  float vf[4] = {1.0f, 1.0f, 1.0f, 1.0f};
   if constexpr (FMT == kMx) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int from = 16 * (g >> 1) + 4 * (g & 1) + 8 * h + r;  // the lane that has the token's
-        const uint32_t w = (uint32_t)__shfl((int)x.scale[0], from, 64), of = (uint32_t)__shfl((int)scale, from, 64);
-        f[h][r] = below_scale((w >> (8 * (n >> 2))) & 0xFFu, __uint_as_float(of));
-      }
+    for (int r = 0; r < 4; ++r) {
+      const int from = 8 * (g >> 1) + 4 * (g & 1) + r;  // a lane that has the token's
+      const uint32_t w = (uint32_t)__shfl((int)x.vs, from, 64), of = (uint32_t)__shfl((int)vs, from, 64);
+      vf[r] = below_scale((w >> (8 * (n >> 2))) & 0xFFu, __uint_as_float(of));
+    }
   }
-  if ((x.live[0] & x.live[1]) != 0xFFFF) {
+  if (x.live != 0xFFFF) {
     // tokens that nobody sees count as zeros (a stale code or scale may be a NaN)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int r = 0; r < 4; ++r)
+      if (!((x.live >> (8 * (g >> 1) + 4 * (g & 1) + r)) & 1)) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (!(((lane < 32 ? x.live[0] : x.live[1]) >> (4 * (g & 1) + 8 * h + r)) & 1)) {
+        for (int i = 0; i < VW; ++i) x.v[r][i] = 0u;
+      }
+    if (!((x.live >> n) & 1)) vs = 0u;
+  }
 #pragma unroll
-          for (int i = 0; i < VW; ++i) x.w[h][VW * r + i] = 0u;
-        }
-    if (!(((lane & 16 ? x.live[1] : x.live[0]) >> n) & 1)) scale = 0u;
+  for (int s = 0; s < 4; ++s) {
+    uint32_t o[4];
+    if constexpr (FMT == kMx) {
+      dims_of<FMT>(x.k[s], kf, o);
+    } else {
+      dims_of<FMT>(x.k[2 * s], 1.0f, o);
+      dims_of<FMT>(x.k[2 * s + 1], 1.0f, o + 2);
+    }
+    // dims 8 (4 g + s) ..
+    *(uint4*)(tile + ((step * 8 + 2 * g + s / 2) * 64 + (s & 1) * 32 + 16 * h + n) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 #pragma unroll
   for (int w = 0; w < VW; ++w) {
-    uint32_t vf[D][4];
+    uint32_t o[2][D];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        uint32_t o[D];
-        tokens_of<FMT>(x.w[h][VW * r + w], x.w[h][VW * (r + 1) + w], FMT == kMx ? f[h][r] : 1.0f, FMT == kMx ? f[h][r + 1] : 1.0f, o);
-#pragma unroll
-        for (int d = 0; d < D; ++d) vf[d][2 * h + r / 2] = o[d];
-      }
+    for (int r = 0; r < 2; ++r) tokens_of<FMT>(x.v[2 * r][w], x.v[2 * r + 1][w], vf[2 * r], vf[2 * r + 1], o[r]);
 #pragma unroll
     for (int d = 0; d < D; ++d) {
       const int j = D * w + d;  // dim 8 n + j
-      *(uint4*)(tile + TreeTile<FMT>::V + (((step * 4 + j / 2) * 2 + (g >> 1)) * 64 + (g & 1) * 32 + (j & 1) * 16 + n) * 16) =
-          make_uint4(vf[d][0], vf[d][1], vf[d][2], vf[d][3]);
+      *(uint2*)(tile + T::V + (((step * 4 + j / 2) * 2 + h) * 64 + (g & 1) * 32 + (j & 1) * 16 + n) * 16 + (g >> 1) * 8) =
+          make_uint2(o[0][d], o[1][d]);
     }
   }
-  if (lane < 32) *(uint32_t*)(tile + TreeTile<FMT>::VS + (step * 32 + lane) * 4) = scale;
-  const float most = half_wave_max(__uint_as_float(scale)), least = -half_wave_max(-__uint_as_float(scale));
+  if (g == 0) {
+    *(uint32_t*)(tile + T::KS + (group * 16 + n) * 4) = ks;
+    *(uint32_t*)(tile + T::VS + (group * 16 + n) * 4) = vs;
+  }
+  const float most = row_max(__uint_as_float(vs)), least = -row_max(-__uint_as_float(vs));
   if (lane == 0)
-    *(uint4*)(tile + TreeTile<FMT>::SEEN + step * 16) =
-        make_uint4(__float_as_uint(lift_of(__float_as_uint(most))), (uint32_t)(x.live[0] | x.live[1] << 16),
-                   one_lift(__float_as_uint(least), __float_as_uint(most)), 0u);
+    *(uint4*)(tile + T::SEEN + group * 16) = make_uint4(__float_as_uint(most), __float_as_uint(least), (uint32_t)x.live, 0u);
+}
+
+// Everything that the workgroup wrote to LDS is there for all of it; loads from memory stay on their way.
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 // What a wave carries over its tokens: a lane's row's reference and sum, its values' sum, acc[d][i]
@@ -839,13 +805,6 @@ __device__ __forceinline__ void wide_weights(v16_t& c, const float* ks, const fl
   }
 }
 
-// Everything that the workgroup wrote to LDS is there for all of it; loads from memory stay on their way.
-__device__ __forceinline__ void tile_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 template <int FMT, int ROWS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_wide_kernel(hq_cache_attn_args A) {
   using T = TreeTile<FMT>;
@@ -876,13 +835,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   way.head = head;
   way.last = (it.span.len - 1) / A.block_tokens;
   TreeLoads<FMT> loads;
-  // waves 0 and 1 take the steps' keys, 2 and 3 their values
-  const int mine = wave & 1;
-  way.ask(A, begin + 32 * mine);
-  if (wave < 2)
-    way.template load<FMT, true>(A, begin + 32 * mine, end, lane, loads);
-  else
-    way.template load<FMT, false>(A, begin + 32 * mine, end, lane, loads);
+  way.ask(A, begin + 16 * wave);
+  way.template load<FMT>(A, begin + 16 * wave, end, lane, loads);
   const int32_t ctx = it.span.len - rows;
   if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each,
@@ -929,68 +883,53 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   // from here on every row's window has begun
   const int32_t open = A.window ? ctx + rows - A.window : 0;
   const bool idle = tile * ROWS + 32 * rw >= rows * A.group;  // the wave has no rows
-  // the whole loop once for each side of the loads: with a choice in it their registers are
-  // moved, and waited for, in every tile
-  auto run = [&](auto side) {
-    constexpr bool KEYS = decltype(side)::value;
-    auto load = [&](int32_t t) { way.template load<FMT, KEYS>(A, t + 32 * mine, end, lane, loads); };
-    auto turn = [&](uint8_t* to) {
-      if constexpr (KEYS)
-        turn_keys<FMT>(loads, to, mine, lane);
-      else
-        turn_values<FMT>(loads, to, mine, lane);
-    };
-    turn(s_tile);
-    if (begin + kTreeTile < end) load(begin + kTreeTile);
-    tile_barrier();
-    uint8_t* at_tile = s_tile;
-    uint8_t* to_tile = s_tile + T::BYTES;
-    for (int32_t t = begin; t < end; t += kTreeTile) {
-      if (t + kTreeTile < end) {
-        turn(to_tile);
-        if (t + 2 * kTreeTile < end) load(t + 2 * kTreeTile);
-      }
-#pragma unroll 1
-      for (int step = TW == 1 ? 0 : tw; step < (TW == 1 ? 2 : tw + 1); ++step) {
-        const uint4 about = *(const uint4*)(at_tile + T::SEEN + step * 16);
-        const uint32_t all = readfirst(about.y);
-        const int32_t live[2] = {(int32_t)(all & 0xFFFFu), (int32_t)(all >> 16)};
-        if (all == 0 || idle) continue;
-        const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
-        bool each = all != 0xFFFFFFFFu || readfirst(about.z) == 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
-        v16_t c;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) c[k] = 0.0f;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          const uint4 a = *(const uint4*)(at_tile + ((step * 8 + s) * 64 + lane) * 16);
-#pragma unroll
-          for (int t1 = 1; t1 >= 0; --t1) c = mfma_f16(a, q[t1][s], c);
-        }
-        uint32_t pt[2][2][4];
-        wide_weights(c, (const float*)(at_tile + T::KS) + step * 32, (const float*)(at_tile + T::VS) + step * 32, each,
-                     __uint_as_float(readfirst(about.x)), live, at, ctx, A.sinks, s_row + 32 * rw, back, lane, z, pt);
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const uint4 v = *(const uint4*)(at_tile + T::V + (((step * 4 + d) * 2 + k) * 64 + lane) * 16);
-#pragma unroll
-            for (int t1 = 1; t1 >= 0; --t1) z.acc[d] = mfma_f16(v, pt[t1][k], z.acc[d]);
-          }
-      }
-      tile_barrier();
-      uint8_t* const x = at_tile;
-      at_tile = to_tile;
-      to_tile = x;
+  turn<FMT>(loads, s_tile, wave, lane);
+  if (begin + kTreeTile < end) way.template load<FMT>(A, begin + kTreeTile + 16 * wave, end, lane, loads);
+  tile_barrier();
+  uint8_t* at_tile = s_tile;
+  uint8_t* to_tile = s_tile + T::BYTES;
+  for (int32_t t = begin; t < end; t += kTreeTile) {
+    if (t + kTreeTile < end) {
+      turn<FMT>(loads, to_tile, wave, lane);
+      if (t + 2 * kTreeTile < end) way.template load<FMT>(A, t + 2 * kTreeTile + 16 * wave, end, lane, loads);
     }
-  };
-  if (wave < 2)
-    run(std::true_type());
-  else
-    run(std::false_type());
+#pragma unroll 1
+    for (int step = TW == 1 ? 0 : tw; step < (TW == 1 ? 2 : tw + 1); ++step) {
+      const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32), about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
+      const int32_t live[2] = {(int32_t)readfirst(about0.z), (int32_t)readfirst(about1.z)};
+      if ((live[0] | live[1]) == 0 || idle) continue;
+      // the largest and least value scale: not negative, so ordered as their bits are
+      const uint32_t most = max(readfirst(about0.x), readfirst(about1.x)), least = min(readfirst(about0.y), readfirst(about1.y));
+      const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
+      bool each = (live[0] & live[1]) != 0xFFFF || !one_lift(least, most);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
+      v16_t c;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) c[k] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const uint4 a = *(const uint4*)(at_tile + ((step * 8 + s) * 64 + lane) * 16);
+#pragma unroll
+        for (int t1 = 1; t1 >= 0; --t1) c = mfma_f16(a, q[t1][s], c);
+      }
+      uint32_t pt[2][2][4];
+      wide_weights(c, (const float*)(at_tile + T::KS) + step * 32, (const float*)(at_tile + T::VS) + step * 32, each,
+                   lift_of(most), live, at, ctx, A.sinks, s_row + 32 * rw, back, lane, z, pt);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const uint4 v = *(const uint4*)(at_tile + T::V + (((step * 4 + d) * 2 + k) * 64 + lane) * 16);
+#pragma unroll
+          for (int t1 = 1; t1 >= 0; --t1) z.acc[d] = mfma_f16(v, pt[t1][k], z.acc[d]);
+        }
+    }
+    tile_barrier();
+    uint8_t* const x = at_tile;
+    at_tile = to_tile;
+    to_tile = x;
+  }
   // ---- the waves' sums under one reference, one row per 16 lanes
   {
     const v2u_t l = __builtin_amdgcn_permlane32_swap(__float_as_uint(z.l), __float_as_uint(z.l), false, false);
