@@ -619,24 +619,29 @@ struct TreeWay {
     const int32_t off = at - (int32_t)A.by_block.of((uint32_t)at) * A.block_tokens;
     const int64_t row = x.live ? ((int64_t)blk * A.heads_kv + head) * A.block_tokens + off : 0;
     ask(A, t + kTreeTile);
-    const uint8_t* k = A.k_codes + row * RB + n * RB + g * (RB / 4);
+    // scalar bases and lane offsets: addresses per lane would live through the whole loop
+    auto base = [&](const void* p, int64_t bytes) {
+      const uint64_t a = (uint64_t)p + bytes;
+      return (const uint8_t*)((uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a));
+    };
+    const uint8_t *k = base(A.k_codes, row * RB), *v = base(A.v_codes, row * RB);
+    const uint32_t lk = n * RB + g * (RB / 4), lv = (8 * (g >> 1) + 4 * (g & 1)) * RB + n * (RB / 16);
 #pragma unroll
     for (int i = 0; i < TreeLoads<FMT>::KW; i += 4) {
-      const uint4 w = *(const uint4*)(k + 4 * i);
+      const uint4 w = *(const uint4*)(k + (lk + 4 * i));
       x.k[i] = w.x; x.k[i + 1] = w.y; x.k[i + 2] = w.z; x.k[i + 3] = w.w;
     }
-    const uint8_t* v = A.v_codes + row * RB + (8 * (g >> 1) + 4 * (g & 1)) * RB + n * (RB / 16);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       if constexpr (FMT == kMx) {
-        x.v[r][0] = *(const uint32_t*)(v + r * RB);
+        x.v[r][0] = *(const uint32_t*)(v + (lv + r * RB));
       } else {
-        const uint2 w = *(const uint2*)(v + r * RB);
+        const uint2 w = *(const uint2*)(v + (lv + r * RB));
         x.v[r][0] = w.x; x.v[r][1] = w.y;
       }
     }
-    x.ks = ((const uint32_t*)A.k_scales)[row + n];
-    x.vs = ((const uint32_t*)A.v_scales)[row + n];
+    x.ks = *(const uint32_t*)(base(A.k_scales, row * 4) + 4 * (uint32_t)n);
+    x.vs = *(const uint32_t*)(base(A.v_scales, row * 4) + 4 * (uint32_t)n);
   }
 };
 
