@@ -12,11 +12,20 @@
 // Both products run on the matrix cores in fp16, which holds every code of the three formats
 // exactly (MXFP4's with its block's scale relative to the token's largest).  A query row is
 // moved to [2^14, 2^15) by a power of two and enters as two fp16 terms, cut off: 11 + 11 bits
-// of the row's largest value.  So do the weights: a row's reference is the largest score plus
-// the power of two of the token's value scale, so that a weight times that scale lies below
-// 2^15, and what two terms cut off, 2^-21 of it, is below 2^-21 of the largest term that the
-// row sums.  Scores, references and sums are fp32.  (Three bf16 terms hold all 24 bits, for
-// half as many products again and twice the instructions of cutting.)
+// of the row's largest value.  So do a weight times its token's value scale: a row's reference
+// (TreeState, kSlack) keeps that product below 2^15 and its row's largest at 2^1 or more, so
+// that two terms, 22 bits of a product or 2^-24 of it, whichever is coarser, cut off no more
+// than 2^-21 of the largest.  Scores, references and sums are fp32.  (Three bf16 terms hold all
+// 24 bits, for half as many products again and twice the instructions of cutting.)
+//
+// What bounds it: a row and token take 2 x 2 x 2 x 128 operations of the matrix cores and some
+// 8 instructions for 16 of them of a lane's softmax, two terms included.  Of two waves on a SIMD
+// the products of one hide a seventh of the other's vector instructions (4 products of
+// 16 x 16 x 32 beside 16 fma: 97 ns for both waves, 64 and 49 alone), so the time is nearly
+// their sum: of 198 us for 8 sequences of 8192 tokens, 64 rows, 8 KV heads of 4, int8, 39 lay
+// before, behind and between the loops (11 the join); without the loads 150 were left, without
+// the softmax 123, without the second product 129.  (The codes' bytes take 29 us at a copy's
+// rate, the two terms' products 116 at that of a large matrix product.)
 #include <hip/hip_runtime.h>
 
 #include "hq_cache_device.h"
@@ -566,17 +575,17 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 }
 
 // ---- many rows
-// Trees of more than 32 rows of a KV head: the codes are turned into fp16 once per workgroup
-// and not once per wave.  A workgroup goes through its tokens in tiles of 64, two steps of 32;
-// each wave turns the keys and values of 16 of them into LDS in the order that the products'
-// operands are read in, a tile ahead of the products; the codes of the tile after it are on
-// their way in registers meanwhile.  Each wave has 32 rows: of a tile of 128 rows each wave
-// takes both steps, of one of 64 two waves share the rows and take a step each.
+// Tiles of 128 rows of a KV head, 32 of each wave: the codes are turned into fp16 once per
+// workgroup and not once per wave.  A workgroup goes through its tokens in tiles of 64, two
+// steps of 32; each wave turns the keys and values of 16 of them into LDS in the order that the
+// products' operands are read in, a tile ahead of the products; the codes of the tile after it
+// are on their way in registers meanwhile.  (8 sequences of 8192 tokens and 64 rows, groups of 4:
+// 191 us, and 221 in tiles of 32 rows, whose waves each turn what they read.)
 //
 // The products are 32 x 32 x 16: a step's scores are one tile C[token, row], in which lane l
 // holds tokens 8 q + 4 (l / 32) + r of row l % 32; with product t of the values contracting
 // tokens 16 t .. in the order 8 q' + 4 (l / 32) + r, lane by lane, they are its operand's.
-constexpr int kTreeTile = 64;
+constexpr int kTreeTile = 64, kWideRows = 128;
 template <int FMT>
 struct TreeTile {
   // keys: [step][contraction step][lane] 16 bytes, dims 8 (2 s + l / 32) ..;  values: [step][group
@@ -810,17 +819,17 @@ __device__ __forceinline__ void wide_weights(v16_t& c, const float* ks, const fl
   }
 }
 
-template <int FMT, int ROWS>
+template <int FMT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_wide_kernel(hq_cache_attn_args A) {
   using T = TreeTile<FMT>;
-  constexpr int RW = ROWS / 32, TW = 4 / RW;  // waves along the rows, along the tokens
+  constexpr int ROWS = kWideRows;
   extern __shared__ __attribute__((aligned(16))) uint8_t s_tile[];  // two tiles
-  __shared__ float s_m[TW][ROWS], s_l[TW][ROWS], s_f[ROWS];
+  __shared__ float s_m[ROWS], s_l[ROWS], s_f[ROWS];
   __shared__ TreeRow s_row[ROWS];
-  static_assert(TW * ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
-  auto o_row = [&](int w, int row) { return (float*)s_tile + (w * ROWS + row) * kOPitch; };
+  static_assert(ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
+  auto o_row = [&](int row) { return (float*)s_tile + row * kOPitch; };
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4;
-  const int wave = (int)readfirst((uint32_t)(tid >> 6)), rw = wave % RW, tw = wave / RW;
+  const int wave = (int)readfirst((uint32_t)(tid >> 6));
   const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.heads_kv), c0 = n * 8;
   const int32_t head = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.heads_kv);
   const CacheItem it = cache_item<kTree>(A, j, lane, blockIdx.x == 0 && wave == 0);
@@ -873,10 +882,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      const uint4 x = *(const uint4*)(s_tile + ((rw * 2 + t) * 8 + s) * 1024 + lane * 16);
+      const uint4 x = *(const uint4*)(s_tile + ((wave * 2 + t) * 8 + s) * 1024 + lane * 16);
       q[t][s][0] = x.x; q[t][s][1] = x.y; q[t][s][2] = x.z; q[t][s][3] = x.w;
     }
-  const float back = s_f[32 * rw + (lane & 31)];  // 1 / the power of two that the row was moved by
+  const float back = s_f[32 * wave + (lane & 31)];  // 1 / the power of two that the row was moved by
   __syncthreads();  // the queries' place is written over
   WideState z;
   z.m = -__builtin_inff();
@@ -887,7 +896,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     for (int k = 0; k < 16; ++k) z.acc[d][k] = 0.0f;
   // from here on every row's window has begun
   const int32_t open = A.window ? ctx + rows - A.window : 0;
-  const bool idle = tile * ROWS + 32 * rw >= rows * A.group;  // the wave has no rows
+  const bool idle = tile * ROWS + 32 * wave >= rows * A.group;  // the wave has no rows
   turn<FMT>(loads, s_tile, wave, lane);
   if (begin + kTreeTile < end) way.template load<FMT>(A, begin + kTreeTile + 16 * wave, end, lane, loads);
   tile_barrier();
@@ -899,7 +908,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       if (t + 2 * kTreeTile < end) way.template load<FMT>(A, t + 2 * kTreeTile + 16 * wave, end, lane, loads);
     }
 #pragma unroll 1
-    for (int step = TW == 1 ? 0 : tw; step < (TW == 1 ? 2 : tw + 1); ++step) {
+    for (int step = 0; step < 2; ++step) {
       const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32), about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
       const int32_t live[2] = {(int32_t)readfirst(about0.z), (int32_t)readfirst(about1.z)};
       if ((live[0] | live[1]) == 0 || idle) continue;
@@ -920,7 +929,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       }
       uint32_t pt[2][2][4];
       wide_weights(c, (const float*)(at_tile + T::KS) + step * 32, (const float*)(at_tile + T::VS) + step * 32, each,
-                   lift_of(most), live, at, ctx, A.sinks, s_row + 32 * rw, back, lane, z, pt);
+                   lift_of(most), live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, z, pt);
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -935,20 +944,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     at_tile = to_tile;
     to_tile = x;
   }
-  // ---- the waves' sums under one reference, one row per 16 lanes
+  // ---- the sums, one row per 16 lanes
   {
     const v2u_t l = __builtin_amdgcn_permlane32_swap(__float_as_uint(z.l), __float_as_uint(z.l), false, false);
-    const int u = lane >> 5, at_row = 32 * rw + (lane & 31);
+    const int u = lane >> 5, at_row = 32 * wave + (lane & 31);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {  // i / 4 % 2 = k / 4, i % 4 = k % 4
       const int i = 4 * (k >> 2) + (k & 3);
-      float* o = o_row(tw, at_row) + (8 * (k >> 2) + 4 * u + (k & 3)) * 8;
+      float* o = o_row(at_row) + (8 * (k >> 2) + 4 * u + (k & 3)) * 8;
       *(float4*)o = make_float4(z.acc[0][i], z.acc[0][i + 8], z.acc[1][i], z.acc[1][i + 8]);
       *(float4*)(o + 4) = make_float4(z.acc[2][i], z.acc[2][i + 8], z.acc[3][i], z.acc[3][i + 8]);
     }
     if (u == 0) {
-      s_m[tw][at_row] = z.m;
-      s_l[tw][at_row] = __uint_as_float(l[0]) + __uint_as_float(l[1]);
+      s_m[at_row] = z.m;
+      s_l[at_row] = __uint_as_float(l[0]) + __uint_as_float(l[1]);
     }
   }
   __syncthreads();
@@ -956,18 +965,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   for (int i = 0; i < ROWS / 16; ++i) {
     const int at_row = 16 * i + grp;
     const TreePlace p(A, tile * ROWS + at_row);
-    float M = s_m[0][at_row], L = 0.0f, v[8] = {};
-#pragma unroll
-    for (int x = 1; x < TW; ++x) M = __builtin_fmaxf(M, s_m[x][at_row]);
-    const float ref = M == -__builtin_inff() ? 0.0f : M;
-#pragma unroll
-    for (int x = 0; x < TW; ++x) {
-      const float f = __builtin_amdgcn_exp2f(s_m[x][at_row] - ref);
-      L = __builtin_fmaf(f, s_l[x][at_row], L);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(f, o_row(x, at_row)[c0 + k], v[k]);
-    }
-    tree_result(A, it.n > 1, (int64_t)blockIdx.x * ROWS + at_row, M, L, v, p, rows, from, head, lane);
+    float v[8];
+    load8(o_row(at_row), c0, false, v);
+    tree_result(A, it.n > 1, (int64_t)blockIdx.x * ROWS + at_row, s_m[at_row], s_l[at_row], v, p, rows, from, head, lane);
   }
 }
 
@@ -1040,12 +1040,12 @@ int launch_narrow(const hq_cache_attn_args& a, hipStream_t st) {
   return 0;
 }
 
-template <int FMT, int ROWS>
+template <int FMT>
 int launch_wide(const hq_cache_attn_args& a, hipStream_t st) {
   static hq_lds_granted granted;
   constexpr size_t lds = 2 * TreeTile<FMT>::BYTES;
-  if (const int e = hq_allow_lds((const void*)hq_cache_tree_wide_kernel<FMT, ROWS>, lds, granted)) return e;
-  hipLaunchKernelGGL((hq_cache_tree_wide_kernel<FMT, ROWS>), dim3((uint32_t)(a.items * a.heads_kv)), dim3(256), lds, st, a);
+  if (const int e = hq_allow_lds((const void*)hq_cache_tree_wide_kernel<FMT>, lds, granted)) return e;
+  hipLaunchKernelGGL((hq_cache_tree_wide_kernel<FMT>), dim3((uint32_t)(a.items * a.heads_kv)), dim3(256), lds, st, a);
   return 0;
 }
 
@@ -1057,7 +1057,7 @@ int launch_tree(const hq_cache_attn_args& a, hipStream_t st) {
       return a.items * a.heads_kv <= 256 ? launch_narrow<FMT, 1, 2 * HQ_CACHE_WAVES>(a, st)
                                          : launch_narrow<FMT, 1, HQ_CACHE_WAVES>(a, st);
     case 5: return launch_narrow<FMT, 2, HQ_CACHE_WAVES>(a, st);
-    default: return launch_wide<FMT, 128>(a, st);
+    default: return launch_wide<FMT>(a, st);
   }
 }
 
