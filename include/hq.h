@@ -641,14 +641,16 @@ hq_status hq_cache_window_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan
  *                sinks); may be null where that is 0.  Overlapping calls need one each.
  * k, v, block_table, scale and the rest as hq_cache_attention.  Scores and sums are fp32; the
  * queries (in the stored coordinates) enter the products with 22 bits of the row's largest
- * value, the weights with 22 bits of the row's largest term: each term is off by at most 2^-21
- * of the largest.  Results repeat bit for bit.  Infinities or NaN come out where a score times
- * 2^22 or the attended tokens' |y| of one coordinate together pass 3.4e38.  An E4M3 code that
- * is a NaN (hq_cache_write stores none) makes every row of its sequence NaN; a NaN scale the
+ * value, a weight times its token's value scale with 22 bits or 2^-21 of the row's largest such
+ * product, whichever is coarser.  Results repeat bit for bit.  Infinities or NaN come out where a
+ * score passes 3.4e38 or an attended key's |y| 2^95; value scales below 2^-96 lose low bits and
+ * below 2^-118 all.  An E4M3 code that is a NaN (hq_cache_write stores none) makes every row of
+ * its sequence NaN; a NaN scale the
  * rows that see its token.
  * Device-side, in k->stats (HQ_ERR_INVALID_ARG): lengths and block ids as hq_cache_attention;
  * a sequence whose starts fall, leave 0 .. rows or hold more rows than max_tree or than its
- * tokens is left out, its rows as they were.  Host errors: HQ_ERR_INVALID_ARG,
+ * tokens is left out, its rows as they were.  Starts that rise everywhere give each row to one
+ * sequence; of two that share rows either one's results are written.  Host errors: HQ_ERR_INVALID_ARG,
  * HQ_ERR_UNSUPPORTED, HQ_ERR_HIP.
  * hq_cache_tree_workspace_bytes -- 0 for invalid arguments, and never less for a larger batch,
  * heads_q, max_blocks, max_tree, window (0 the largest) or sinks. */

@@ -1,6 +1,7 @@
 // gfx950 kernels of the fixed-rate key-value cache: rows cast into slots
 // (hq_cache_write), read back (hq_cache_read), and one query token per sequence
-// attending over a paged cache (hq_cache_attention).
+// attending over a paged cache (hq_cache_attention), or over the last tokens and the first
+// ones of it (hq_cache_window_attention, the same kernel with other tokens to go through).
 //
 // A stored head vector is the cast of y = H D x (H the 128-point Sylvester
 // matrix, D the plan's signs of the head's columns): int8 or E4M3 codes c with one

@@ -308,7 +308,9 @@ struct hq_rope_args {
   int32_t x_bf16, y_bf16, transposed;
   int32_t past;           // y is stored past the caches
 };
-// 4 of heads that fill it to four fifths.
+// Heads of a row that a lane group takes: 4 where the heads fill it to four fifths.  7800 rows of 20
+// heads, bf16, 15.9 us with four, 19.3 with two, 27.5 with one; 8000 of 16 from fp32 to bf16 22.7,
+// 21.7 and 23.2; eight were slower (18.7 for the first).
 static inline int32_t hq_rope_per(int32_t heads, int32_t else_per) {
   return 4 * ((heads + 3) / 4 * 4) <= 5 * heads ? 4 : else_per < heads ? else_per : heads;
 }

@@ -170,6 +170,9 @@ __device__ __forceinline__ void store8_past(void* p, int64_t i, bool bf16, bool 
 
 // A lane group takes up to H heads of a row, groups apart: the row's positions and table
 // lines are loaded once for them, and neighbouring lane groups have neighbouring heads.
+// Bound by memory: 7800 rows of 20 heads in bf16, 84 MB with the table's lines, take 15.5 us,
+// at a large copy's rate 16.4 (some of the rows are in the last cache).  16 rows of 32 heads: a
+// launch and one chain of two loads, position and then table, 4.6 us on the GPU.
 template <int H, bool BF16>
 __device__ __forceinline__ void rope_tile(const hq_rope_args& A, const hq_turns& T, uint32_t tile, bool in) {
   const int lane = threadIdx.x & 63, c0 = (lane & 15) * 8;
