@@ -468,8 +468,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   w.got();
   w.template enter<FMT, true>(A, lane);
   uint8_t* ring = s_ring + wave * R::WAVE;
-  int32_t live[2], next[2] = {0, 0}, at[2];
-  if (begin < end) w.template fetch<FMT>(A, begin, end, lane, ring, live, at);
+  int32_t live[2], next[2] = {0, 0};
+  if (begin < end) w.template fetch<FMT>(A, begin, end, lane, ring, live);
   // ---- the query into the cache's coordinates, as three bf16 terms
   if (grp < HEADS) {
     float qv[8];
@@ -509,7 +509,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   z.l = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) z.acc[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  if (begin + 32 < end) w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP, next, at);
+  if (begin + 32 < end) w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP, next);
   int32_t slot = 0;
   for (int32_t t = begin; t < end; t += 32) {
     // the loads of this step are done when at most the next step's are not
@@ -524,7 +524,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     live[1] = next[1];
     if (t + 64 < end) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
-      w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next, at);
+      w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next);
     }
     slot ^= 1;
     cache_step<FMT, C, MODE>(cur, here, q, lane, z);

@@ -265,7 +265,7 @@ template <typename SUM>
 __device__ __forceinline__ uint32_t cache_chunk(const hq_cache_attn_args& A, int64_t total, int32_t mine, int32_t tiles,
                                                 SUM sum) {
   const int64_t even = (total * A.heads_kv + HQ_CACHE_WG_TARGET - 1) / HQ_CACHE_WG_TARGET;
-  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / A.heads_kv;
+  const int64_t few = (HQ_CACHE_WG_TARGET + HQ_CACHE_WG_TARGET / 32) / (uint32_t)A.heads_kv;
   uint32_t chunk = HQ_CACHE_LEAST;
   for (int e = 8; e <= 16; ++e) {
     const int64_t c = min(((even * e >> 3) + kStep - 1) & -(int64_t)kStep, (int64_t)1 << 30);
@@ -327,9 +327,11 @@ __device__ __forceinline__ CacheItem cache_item(const hq_cache_attn_args& A, int
     const CacheSpan s = in ? cache_span_of<MODE>(A, lane, tell) : CacheSpan{-1, 0, 0, 0, 0};
     const int32_t len = MODE == kAll ? s.len : s.seen();
     const int32_t tiles = cache_tiles<MODE>(A, s.rows);
-    int64_t total = (int64_t)max(len, 0) * tiles;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
+    const uint64_t of = (uint64_t)max(len, 0) * (uint32_t)tiles;  // below 2^37
+    uint32_t sum0 = (uint32_t)of & 0xFFFFu, sum1 = (uint32_t)(of >> 16);
+    wave_scan_incl2(sum0, sum1);
+    const int64_t total =
+        ((int64_t)__builtin_amdgcn_readlane(sum1, 63) << 16) + (uint32_t)__builtin_amdgcn_readlane(sum0, 63);
     const uint32_t chunk = cache_chunk(A, total, len, tiles, [](uint32_t n) { return wave_total(n); });
     const uint32_t n = in ? cache_parts(len, chunk) : 0u;
     const int32_t incl = (int32_t)wave_scan_incl(n * (uint32_t)tiles);
@@ -458,10 +460,10 @@ struct CacheWalk {
   }
   // Starts the loads of the 32 tokens from t on into `step` (LDS) and moves the walk
   // past them; live[h]: tokens of each half to attend to, of kAll their number, else one bit
-  // each; at[h] (not of kAll): a half's first token.
+  // each.
   template <int FMT>
   __device__ __forceinline__ void fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step,
-                                        int32_t (&live)[2], int32_t (&at)[2]) {
+                                        int32_t (&live)[2]) {
     using R = CacheRing<FMT>;
     constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
     const uint32_t row_in = lane / CPR, chunk = lane % CPR;
@@ -485,8 +487,8 @@ struct CacheWalk {
       if constexpr (MODE == kAll) {
         live[h] = bad ? 0 : min(max(end - t - 16 * h, 0), 16);
       } else {
-        at[h] = t + 16 * h + (blk > before ? gap : 0);
-        live[h] = bad || t + 16 * h >= end ? 0 : (int32_t)span.bits(at[h]);
+        // told to be the same in every lane: the loads' scalar offsets go by it
+        live[h] = (int32_t)readfirst(bad || t + 16 * h >= end ? 0u : span.bits(t + 16 * h + (blk > before ? gap : 0)));
       }
       const uint32_t place = live[h] ? off : 0;
       off += 16;

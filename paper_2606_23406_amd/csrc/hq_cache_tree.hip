@@ -155,6 +155,95 @@ __device__ __forceinline__ void tree_take(uint8_t* step, int lane, TreeStep<FMT>
   }
 }
 
+// A scalar base for lane offsets: addresses per lane would live through the whole loop.
+__device__ __forceinline__ const uint8_t* uniform(const void* p, int64_t bytes) {
+  const uint64_t a = (uint64_t)p + bytes;
+  return (const uint8_t*)((uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a));
+}
+typedef __attribute__((address_space(1))) const void glb_void;
+
+// A wave's way over its tokens, through the ring of the one-token attention.  Next to the products
+// every instruction of a wave counts, scalar ones too (a wave issues one in some 7 cycles): a
+// half's place is formed from its token by a multiplication, with no state from half to half but
+// the ids of the 64 blocks from `first` on, one a lane, and what a step's masks go by is formed
+// when one is needed.  (The one-token attention's way, which keeps buffers of its block: 24
+// uneven trees in MXFP4 73.5 us.)
+struct TreeWalk {
+  const int32_t* table;
+  CacheSpan span;
+  int32_t gap, jump, head, last;  // last: the sequence's last block
+  int32_t ctx, open, sinks;       // all rows see [0, sinks) and [open, ctx)
+  int32_t first, ids;
+  int64_t stride, offset;         // vectors of a block, those before the head's
+  __device__ __forceinline__ void start(const hq_cache_attn_args& A, const CacheItem& it, int32_t of) {
+    table = A.table + (int64_t)it.b * A.max_blocks;
+    span = it.span;
+    gap = span.gap();
+    jump = gap ? span.turn() : 0x7FFFFFFF;
+    head = of;
+    last = (span.len - 1) / A.block_tokens;
+    ctx = span.len - span.rows;
+    open = A.window ? ctx + span.rows - A.window : 0;
+    sinks = A.sinks;
+    stride = (int64_t)A.heads_kv * A.block_tokens;
+    offset = (int64_t)of * A.block_tokens;
+  }
+  __device__ __forceinline__ int32_t real(int32_t t) const { return t < jump ? t : t + gap; }
+  __device__ __forceinline__ int32_t block(const hq_cache_attn_args& A, int32_t at) const {
+    return min((int32_t)A.by_block.of((uint32_t)at), last);
+  }
+  __device__ __forceinline__ void ask(int32_t blk, int lane) {
+    first = blk;
+    ids = table[min(blk + lane, last)];
+  }
+  __device__ __forceinline__ void got() { asm volatile("" : "+v"(ids)); }
+  // Starts the loads of the 32 tokens from t on into `step`.  Returns 1 + 2 + 4 where all rows see
+  // all of them, else 2 and 4 for the halves with tokens at all; one without loads the cache's
+  // first ones.
+  template <int FMT>
+  __device__ __forceinline__ uint32_t fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step) {
+    using R = CacheRing<FMT>;
+    constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
+    const uint32_t row_in = lane / CPR, chunk = lane % CPR;
+    const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16, token = (lane & 15) * 4;
+    uint32_t all = 1, some = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t at = real(t + 16 * h), blk = block(A, at);
+      if (blk - first >= 64) {
+        ask(blk, lane);
+        got();
+      }
+      const int32_t id = __builtin_amdgcn_readlane(ids, blk - first);
+      const bool in = t + 16 * h < end, ok = in && (uint32_t)id < (uint32_t)A.blocks;
+      if (in && !ok && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
+      if (!ok || at + 16 > ctx || (at < open && at + 16 > sinks)) all = 0;
+      if (ok) some |= 2u << h;
+      const int64_t row = ok ? id * stride + offset + (at - blk * A.block_tokens) : 0;
+      uint8_t* to = step + h * R::HALF;
+      const uint8_t *k = uniform(A.k_codes, row * R::RB), *v = uniform(A.v_codes, row * R::RB);
+      glb_void *const kl = (glb_void*)(k + from), *const vl = (glb_void*)(v + from);
+      __builtin_amdgcn_global_load_lds(kl, (lds_void*)to, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(vl, (lds_void*)(to + R::V), 16, 0, 0);
+      if constexpr (RPL < 16) {  // the offset moves both places
+        __builtin_amdgcn_global_load_lds(kl, (lds_void*)to, 16, 1024, 0);
+        __builtin_amdgcn_global_load_lds(vl, (lds_void*)(to + R::V), 16, 1024, 0);
+      }
+      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.k_scales, row * 4) + token), (lds_void*)(to + R::SCALES), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.v_scales, row * 4) + token), (lds_void*)(to + R::SCALES + 256), 4, 0, 0);
+    }
+    return all | some;
+  }
+  // Of the 32 tokens from t on: each half's first and the bits of those that anybody sees.
+  __device__ __forceinline__ void about(int32_t t, uint32_t seen, int32_t (&live)[2], int32_t (&at)[2]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      at[h] = real(t + 16 * h);
+      live[h] = (seen >> h) & 2 ? (int32_t)span.bits(at[h]) : 0;
+    }
+  }
+};
+
 // What a row sees, in LDS: only steps that some row does not see some token of look at it.
 struct TreeRow {
   uint64_t mask;  // ancestors
@@ -198,9 +287,9 @@ __device__ __forceinline__ bool one_lift(uint32_t least, uint32_t most) { return
 // with one for each of two ways the compiler keeps the accumulators twice.
 template <int RT>
 __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)[2][4], const float (&vs)[2][4], bool each,
-                                             float lift, const int32_t (&live)[2], const int32_t (&at)[2], int32_t ctx,
-                                             int32_t sinks, const TreeRow* rows, const float (&back)[RT], int lane,
-                                             TreeState (&z)[RT], uint32_t (&pt)[RT][2][4]) {
+                                             float lift, const TreeWalk& w, int32_t t, uint32_t seen, const TreeRow* rows,
+                                             const float (&back)[RT], int lane, TreeState (&z)[RT],
+                                             uint32_t (&pt)[RT][2][4]) {
   const int g = lane >> 4;
   float top[RT];
   bool more = false;
@@ -212,13 +301,15 @@ __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)
       for (int r = 0; r < 4; ++r) c[i][h][r] *= ks[h][r];
   }
   if (each) {
+    int32_t live[2], at[2];
+    w.about(t, seen, live, at);
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
       const TreeRow row = rows[16 * i + (lane & 15)];
       top[i] = -__builtin_inff();
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t sees = (row.sees(at[h], ctx, sinks) & (uint32_t)live[h]) >> (4 * g);
+        const uint32_t sees = (row.sees(at[h], w.ctx, w.sinks) & (uint32_t)live[h]) >> (4 * g);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           c[i][h][r] = (sees >> r) & 1 ? c[i][h][r] : -__builtin_inff();
@@ -282,13 +373,16 @@ __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)
   }
 }
 
-// One step: 32 tokens.  `each`: some row does not see some token.
+// One step: the 32 tokens from t on, of which `seen` is what TreeWalk::fetch returned.
 template <int FMT, int RT>
-__device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const int32_t (&live)[2], const int32_t (&at)[2], bool each,
-                                          int32_t ctx, int32_t sinks, const uint32_t (&q)[RT][2][4][4],
-                                          const TreeRow* rows, const float (&back)[RT], int lane, TreeState (&z)[RT]) {
+__device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const TreeWalk& w, int32_t t, uint32_t seen,
+                                          const uint32_t (&q)[RT][2][4][4], const TreeRow* rows, const float (&back)[RT],
+                                          int lane, TreeState (&z)[RT]) {
   const int g = lane >> 4;
+  bool each = !(seen & 1);  // some row does not see some token
   if (each) {
+    int32_t live[2], at[2];
+    w.about(t, seen, live, at);
     // tokens that nobody sees: their value codes count as zeros (a stale code may be a NaN)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -333,7 +427,7 @@ __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const int32_t (&li
         for (int i = 0; i < RT; ++i) c[i][h] = mfma_f16(a[h], q[i][t][s], c[i][h]);
   }
   uint32_t pt[RT][2][4];
-  tree_weights<RT>(c, cur.ks, cur.vs, each, lift_of(hi), live, at, ctx, sinks, rows, back, lane, z, pt);
+  tree_weights<RT>(c, cur.ks, cur.vs, each, lift_of(hi), w, t, seen, rows, back, lane, z, pt);
   // value codes: per word the tokens' pairs of each of its dims
 #pragma unroll
   for (int w = 0; w < CacheStep<FMT>::VW; ++w) {
@@ -453,11 +547,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   const int32_t begin0 = (int32_t)(it.at * it.chunk), tokens = min(it.chunk, seen - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
-  CacheWalk<kTree> w;
-  w.table = A.table + (int64_t)it.b * A.max_blocks;
-  w.head = head;
-  w.start(A, it.span, begin);
-  w.ask(lane);
+  TreeWalk w;
+  w.start(A, it, head);
+  w.ask(w.block(A, w.real(begin)), lane);
   Raw8 qraw[RT] = {};
   const uint4 qd = sign_words(A.k_dsign16, head * HQ_TILE + c0);
 #pragma unroll
@@ -466,13 +558,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     if (grp < 16 && p.i < rows)
       qraw[i] = load_raw8(A.q, ((int64_t)(from + p.i) * A.heads_q + (int64_t)head * A.group + p.head) * HQ_TILE + c0, A.q_bf16);
   }
-  const int32_t ctx = it.span.len - rows;
-  if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
+  if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, w.ctx);
   w.got();
-  w.template enter<FMT, true>(A, lane);
   uint8_t* ring = s_ring + wave * WAVE;
-  int32_t live[2], at[2], next[2] = {0, 0}, next_at[2] = {0, 0};
-  if (begin < end) w.template fetch<FMT>(A, begin, end, lane, ring, live, at);
+  uint32_t sees = 0, next = 0;
+  if (begin < end) sees = w.template fetch<FMT>(A, begin, end, lane, ring);
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
@@ -509,9 +599,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
     for (int k = 0; k < 8; ++k) z[i].acc[k] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
   }
-  // from here on every row's window has begun
-  const int32_t open = A.window ? ctx + rows - A.window : 0;
-  if (begin + 32 < end) w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP, next, next_at);
+  if (begin + 32 < end) next = w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP);
   int32_t slot = 0;
   for (int32_t t = begin; t < end; t += 32) {
     // the loads of this step are done when at most the next step's are not
@@ -521,22 +609,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     TreeStep<FMT> cur;
     tree_take<FMT>(ring + slot * R::STEP, lane, cur);
-    const int32_t here[2] = {live[0], live[1]}, here_at[2] = {at[0], at[1]};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      live[h] = next[h];
-      at[h] = next_at[h];
-    }
+    const uint32_t here = sees;
+    sees = next;
     if (t + 64 < end) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
-      w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next, next_at);
+      next = w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP);
     }
     slot ^= 1;
-    bool each = (here[0] & here[1]) != 0xFFFF;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      each |= here_at[h] + 16 > ctx || (here_at[h] < open && here_at[h] + 16 > A.sinks);
-    tree_step<FMT, RT>(cur, here, here_at, each, ctx, A.sinks, q, s_row, back, lane, z);
+    tree_step<FMT, RT>(cur, w, t, here, q, s_row, back, lane, z);
   }
   // ---- the waves' sums under one reference, one row per 16 lanes
 #pragma unroll
@@ -628,12 +708,7 @@ struct TreeWay {
     const int32_t off = at - (int32_t)A.by_block.of((uint32_t)at) * A.block_tokens;
     const int64_t row = x.live ? ((int64_t)blk * A.heads_kv + head) * A.block_tokens + off : 0;
     ask(A, t + kTreeTile);
-    // scalar bases and lane offsets: addresses per lane would live through the whole loop
-    auto base = [&](const void* p, int64_t bytes) {
-      const uint64_t a = (uint64_t)p + bytes;
-      return (const uint8_t*)((uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a));
-    };
-    const uint8_t *k = base(A.k_codes, row * RB), *v = base(A.v_codes, row * RB);
+    const uint8_t *k = uniform(A.k_codes, row * RB), *v = uniform(A.v_codes, row * RB);
     const uint32_t lk = n * RB + g * (RB / 4), lv = (8 * (g >> 1) + 4 * (g & 1)) * RB + n * (RB / 16);
 #pragma unroll
     for (int i = 0; i < TreeLoads<FMT>::KW; i += 4) {
@@ -649,8 +724,8 @@ struct TreeWay {
         x.v[r][0] = w.x; x.v[r][1] = w.y;
       }
     }
-    x.ks = *(const uint32_t*)(base(A.k_scales, row * 4) + 4 * (uint32_t)n);
-    x.vs = *(const uint32_t*)(base(A.v_scales, row * 4) + 4 * (uint32_t)n);
+    x.ks = *(const uint32_t*)(uniform(A.k_scales, row * 4) + 4 * (uint32_t)n);
+    x.vs = *(const uint32_t*)(uniform(A.v_scales, row * 4) + 4 * (uint32_t)n);
   }
 };
 
