@@ -552,9 +552,12 @@ __device__ __forceinline__ void cache_finish(const hq_cache_attn_args& A, float 
   const float inv = L == 0.0f ? 0.0f : 1.0f / (L * 128.0f);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] *= inv;
-  const XSigns sg(lane);
-  fwht128(v, sg);
-  flip8(v, sign_words(A.v_dsign16, head * HQ_TILE + (lane & 15) * 8));
+  const TwSigns sg(lane);
+  fwht128_tw(v, sg);
+  uint4 d = sign_words(A.v_dsign16, head * HQ_TILE + (lane & 15) * 8);
+  const uint32_t sigma = sg.sigma | sg.sigma >> 16;
+  d.x ^= sigma; d.y ^= sigma; d.z ^= sigma; d.w ^= sigma;
+  flip8(v, d);
 }
 
 }  // namespace

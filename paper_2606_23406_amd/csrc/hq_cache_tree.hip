@@ -155,6 +155,29 @@ __device__ __forceinline__ void tree_take(uint8_t* step, int lane, TreeStep<FMT>
   }
 }
 
+// Of two waves of a SIMD the one that is further behind goes first, by quarters of their ways: else
+// the older one does throughout, and the younger one's rest runs alone.  (8 sequences of 8192
+// tokens and 64 rows: the loops of the first workgroups of the CUs 137 us and of the second 158,
+// so 146 and 157; 175.3 us a call to 173.7, 24 uneven trees in MXFP4 72.0 to 70.2.)
+struct Behind {
+  int32_t left, next, quarter;
+  __device__ __forceinline__ void start(int32_t begin, int32_t of) {
+    left = 4;
+    next = begin;
+    quarter = of;
+  }
+  __device__ __forceinline__ void at(int32_t t, int32_t end) {
+    if (t != next) return;
+    switch (--left) {
+      case 3: __builtin_amdgcn_s_setprio(3); break;
+      case 2: __builtin_amdgcn_s_setprio(2); break;
+      case 1: __builtin_amdgcn_s_setprio(1); break;
+      default: __builtin_amdgcn_s_setprio(0);
+    }
+    next = left && quarter ? t + quarter : end;
+  }
+};
+
 // A scalar base for lane offsets: addresses per lane would live through the whole loop.
 __device__ __forceinline__ const uint8_t* uniform(const void* p, int64_t bytes) {
   const uint64_t a = (uint64_t)p + bytes;
@@ -455,7 +478,7 @@ __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const TreeWalk& w,
 struct TreePlace {
   int32_t i, head;  // i: of the tree, at or past its end where the tile has none
   __device__ __forceinline__ TreePlace(const hq_cache_attn_args& A, int32_t row) {
-    i = row / A.group;
+    i = (int32_t)A.by_group.of((uint32_t)row);
     head = row - i * A.group;
   }
 };
@@ -469,12 +492,13 @@ __device__ __forceinline__ TreeRow tree_row(const hq_cache_attn_args& A, int32_t
 
 // 8 values a lane of a query in the cache's coordinates, moved by a power of two so that the
 // largest of its 128 lies in [2^14, 2^15), as two terms; returns 1 / that power.
-__device__ __forceinline__ float tree_query(const Raw8& raw, bool bf16, uint4 signs, float scale, int lane, uint4& hi, uint4& lo) {
+__device__ __forceinline__ float tree_query(const Raw8& raw, bool bf16, uint4 signs, float scale, const TwSigns& sg,
+                                            uint4& hi, uint4& lo) {
   float v[8], am = 0.0f;
   expand8(raw, bf16, v);
   flip8(v, signs);
-  const XSigns sg(lane);
-  fwht128(v, sg);
+  fwht128_tw(v, sg);
+  scale = xor_sign(scale, sg.sigma);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     v[k] *= scale;
@@ -564,11 +588,12 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   uint32_t sees = 0, next = 0;
   if (begin < end) sees = w.template fetch<FMT>(A, begin, end, lane, ring);
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each
+  const TwSigns sg(lane);
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     if (grp >= 16) break;  // the last four of eight waves
     uint4 hi, lo;
-    const float f = tree_query(qraw[i], A.q_bf16, qd, A.qscale, lane, hi, lo);
+    const float f = tree_query(qraw[i], A.q_bf16, qd, A.qscale, sg, hi, lo);
     *(uint4*)(q_row(16 * i + grp, 0) + c0) = hi;
     *(uint4*)(q_row(16 * i + grp, 1) + c0) = lo;
     if (n == 0) s_f[16 * i + grp] = f;
@@ -601,7 +626,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   }
   if (begin + 32 < end) next = w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP);
   int32_t slot = 0;
+  Behind first;
+  first.start(begin, (end - begin) / 128 * 32);
   for (int32_t t = begin; t < end; t += 32) {
+    first.at(t, end);
     // the loads of this step are done when at most the next step's are not
     if (t + 32 < end)
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
@@ -939,13 +967,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     return raw;
   };
   Raw8 raw0 = query(0), raw1 = query(1);
+  const TwSigns sg(lane);
 #pragma unroll 1
   for (int i = 0; i < ROWS / 16; ++i) {
     const Raw8 raw = raw0;
     raw0 = raw1;
     raw1 = query(i + 2);
     uint4 hi, lo;
-    const float f = tree_query(raw, A.q_bf16, qd, A.qscale, lane, hi, lo);
+    const float f = tree_query(raw, A.q_bf16, qd, A.qscale, sg, hi, lo);
     uint8_t* to = s_tile + (i >> 1) * 16384 + (n >> 1) * 1024 + ((n & 1) * 32 + (i & 1) * 16 + grp) * 16;
     *(uint4*)to = hi;
     *(uint4*)(to + 8192) = lo;
@@ -977,7 +1006,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   tile_barrier();
   uint8_t* at_tile = s_tile;
   uint8_t* to_tile = s_tile + T::BYTES;
+  Behind first;
+  first.start(begin, (end - begin) / (4 * kTreeTile) * kTreeTile);
   for (int32_t t = begin; t < end; t += kTreeTile) {
+    first.at(t, end);
     if (t + kTreeTile < end) {
       turn<FMT>(loads, to_tile, wave, lane);
       if (t + 2 * kTreeTile < end) way.template load<FMT>(A, t + 2 * kTreeTile + 16 * wave, end, lane, loads);
@@ -1049,7 +1081,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
 // Joins the chunks of a row under one reference, in order, and moves the result back: a wave
 // per row of a split sequence, 16 lanes for every fourth chunk, whose first four are loaded
 // together.  (16 chunks of 32 rows: 11.6 us with 16 lanes for all of a row's chunks.)
-__global__ __launch_bounds__(256) void hq_cache_tree_join_kernel(hq_cache_attn_args A, int32_t tile_rows, uint32_t per) {
+__global__ __launch_bounds__(256) void hq_cache_tree_join_kernel(hq_cache_attn_args A, uint32_t per) {
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4, c0 = n * 8;
   int64_t b = blockIdx.x / per;
   const uint32_t at = readfirst((blockIdx.x - (uint32_t)b * per) * 4 + (tid >> 6));  // query head of a drafted token
@@ -1061,10 +1093,10 @@ __global__ __launch_bounds__(256) void hq_cache_tree_join_kernel(hq_cache_attn_a
   if (has.n == 1) return;  // already whole
   const int32_t from = A.starts[b], rows = A.starts[b + 1] - from;
   if (at >= (uint32_t)rows * (uint32_t)A.heads_q) return;
-  const uint32_t i = at / (uint32_t)A.heads_q, hq = at - i * (uint32_t)A.heads_q, head = hq / (uint32_t)A.group;
-  const uint32_t row = i * (uint32_t)A.group + hq - head * (uint32_t)A.group, tile = row / (uint32_t)tile_rows;
-  const int64_t part0 = (((int64_t)has.first + tile) * A.heads_kv + head) * tile_rows + (row - tile * (uint32_t)tile_rows);
-  const int64_t step = (int64_t)cache_tiles<kTree>(A, rows) * A.heads_kv * tile_rows;
+  const uint32_t i = at / (uint32_t)A.heads_q, hq = at - i * (uint32_t)A.heads_q, head = A.by_group.of(hq);
+  const uint32_t row = i * (uint32_t)A.group + hq - head * (uint32_t)A.group, tile = row >> A.tile_shift;
+  const int64_t part0 = ((((int64_t)has.first + tile) * A.heads_kv + head) << A.tile_shift) + (row - (tile << A.tile_shift));
+  const int64_t step = (int64_t)cache_tiles<kTree>(A, rows) * A.heads_kv << A.tile_shift;
   float M = -__builtin_inff(), m[4], l[4], a[4][8];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -1150,8 +1182,7 @@ int hq_launch_cache_tree(const hq_cache_attn_args& a, int format, void* stream) 
   if (e) return e;
   if (a.join && a.joins) {
     const uint32_t per = ((uint32_t)a.max_rows * (uint32_t)a.heads_q + 3) / 4;
-    hipLaunchKernelGGL(hq_cache_tree_join_kernel, dim3((uint32_t)a.joins * per), dim3(256), 0, st, a,
-                       1 << a.tile_shift, per);
+    hipLaunchKernelGGL(hq_cache_tree_join_kernel, dim3((uint32_t)a.joins * per), dim3(256), 0, st, a, per);
   }
   return (int)hipGetLastError();
 }
