@@ -12,6 +12,8 @@
 // tokens of a block are one run of memory.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "hq_cache_device.h"
 #include "hq_lds.h"
 
@@ -278,13 +280,13 @@ struct CacheState {
 template <int C>
 constexpr int products() { return C == 4 ? 1 : C == 2 ? 2 : 3; }
 
-template <int FMT, int C, int MODE>
-__device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const int32_t (&live)[2],
+template <int FMT, int C, typename WALK>
+__device__ __forceinline__ void cache_step(CacheStep<FMT>& cur, const WALK& w, int32_t t, const typename WALK::Look& look,
                                            const uint32_t (&q)[products<C>()][4][4], int lane, CacheState& z) {
   constexpr int T = products<C>();
   const int n = lane & 15, g = lane >> 4;
-  const bool cut = MODE == kAll ? live[0] + live[1] < 32 : (live[0] & live[1]) != 0xFFFF;
-  auto dead = [&](int h, int r) { return MODE == kAll ? 4 * g + r >= live[h] : !((live[h] >> (4 * g + r)) & 1); };
+  const bool cut = w.cut(look);
+  auto dead = [&](int h, int r) { return w.dead(look, t, h, 4 * g + r); };
   if (cut) {
     // stale or absent tokens: their value codes count as zeros (their weight is
     // zero, but a stale code or scale may be a NaN)
@@ -454,12 +456,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   const int32_t begin0 = (int32_t)(it.at * it.chunk), tokens = min(it.chunk, seen - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
-  CacheWalk<MODE> w;
-  w.table = A.table + (int64_t)it.b * A.max_blocks;
-  w.head = head;
-  w.start(A, it.span, begin);
+  using Walk = std::conditional_t<MODE == kAll, CacheWalk, SpanWalk>;
+  Walk w;
+  w.start(A, it, head, begin);
   if (A.join || MODE != kAll) {
-    w.ask(lane);
+    w.ask(A, begin, lane);
     if (A.join) load_query(it.b);
   } else {
     w.first = 0;
@@ -468,8 +469,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   w.got();
   w.template enter<FMT, true>(A, lane);
   uint8_t* ring = s_ring + wave * R::WAVE;
-  int32_t live[2], next[2] = {0, 0};
-  if (begin < end) w.template fetch<FMT>(A, begin, end, lane, ring, live);
+  typename Walk::Look sees = {}, next = {};
+  if (begin < end) sees = w.template fetch<FMT>(A, begin, end, lane, ring);
   // ---- the query into the cache's coordinates, as three bf16 terms
   if (grp < HEADS) {
     float qv[8];
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   z.l = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) z.acc[i] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  if (begin + 32 < end) w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP, next);
+  if (begin + 32 < end) next = w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP);
   int32_t slot = 0;
   for (int32_t t = begin; t < end; t += 32) {
     // the loads of this step are done when at most the next step's are not
@@ -519,15 +520,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     CacheStep<FMT> cur;
     cache_take<FMT>(ring + slot * R::STEP, lane, cur);
-    const int32_t here[2] = {live[0], live[1]};
-    live[0] = next[0];
-    live[1] = next[1];
+    const typename Walk::Look here = sees;
+    sees = next;
     if (t + 64 < end) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
-      w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP, next);
+      next = w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP);
     }
     slot ^= 1;
-    cache_step<FMT, C, MODE>(cur, here, q, lane, z);
+    cache_step<FMT, C>(cur, w, t, here, q, lane, z);
   }
   z.l = groups_sum(z.l);
   // ---- the waves' sums under one maximum, one head per 16 lanes

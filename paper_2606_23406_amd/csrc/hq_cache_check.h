@@ -111,6 +111,7 @@ hq_status attention_args(const hq_plan_s* kp, const hq_cache* k, const hq_plan_s
   a->group = (int32_t)group;
   a->max_blocks = max_blocks;
   a->block_tokens = k->block_tokens;
+  a->by_block = hq_divide_by((uint32_t)k->block_tokens);
   // no sequence is longer than 2^30 tokens, so no larger window or number of sinks differs
   a->window = window < 1 << 30 ? window : 1 << 30;
   a->sinks = sinks < 1 << 30 ? sinks : 1 << 30;

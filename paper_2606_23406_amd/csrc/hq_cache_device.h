@@ -393,52 +393,33 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t run_of(const void* p, int64_t 
   return __builtin_amdgcn_make_buffer_rsrc((void*)u, 0, bytes, 0x00020000);
 }
 
-// Where a wave stands in its sequence: token off of block blk of the table row, and
-// that block's head as buffers.  The ids of 64 blocks ahead are one per lane, so that
-// following the table costs a lane read and not a load that the next loads' addresses
-// wait for.  Blocks are numbered along the way: of a window, those of the sinks up to
-// `before`, then those of the window, `skip` further on in the table row.
-template <int MODE>
+// Where a wave stands in its sequence, all of whose tokens it goes through: token off of block blk
+// of the table row, and that block's head as buffers.  The ids of 64 blocks ahead are one per
+// lane, so that following the table costs a lane read and not a load that the next loads'
+// addresses wait for.
 struct CacheWalk {
+  // What a fetch returns of its two halves: tokens of each to attend to.
+  struct Look {
+    int32_t live[2];
+  };
   const int32_t* table;
-  int32_t last;  // the way's last block
+  int32_t last;  // the sequence's last block
   int32_t head, blk, off;
   int32_t first, ids;  // lane l: block first + l
   __amdgpu_buffer_rsrc_t k, v, ks, vs;
   bool bad;  // the block lies outside the cache: its buffers are empty
-  CacheSpan span;
-  int32_t jump, before, skip, to_off, gap;
-  // To token `begin` of the way.
-  __device__ __forceinline__ void start(const hq_cache_attn_args& A, const CacheSpan& s, int32_t begin) {
-    const int32_t bt = A.block_tokens;
-    last = (s.len - 1) / bt;
-    if constexpr (MODE == kAll) {
-      blk = min(begin / bt, last);
-      off = begin - blk * bt;
-    } else {
-      span = s;
-      gap = s.gap();
-      before = 0x7FFFFFFF;
-      jump = -1;
-      skip = to_off = 0;
-      if (gap) {
-        jump = s.turn();
-        const int32_t to = (jump + gap) / bt;
-        to_off = jump + gap - to * bt;
-        before = (jump + bt - 1) / bt - 1;
-        skip = to - before - 1;
-        last -= skip;
-      }
-      const int32_t real = gap && begin >= jump ? begin + gap : begin, at = real / bt;
-      blk = min(real == begin ? at : at - skip, last);
-      off = real - at * bt;
-    }
+  // To token `begin`.
+  __device__ __forceinline__ void start(const hq_cache_attn_args& A, const CacheItem& it, int32_t of, int32_t begin) {
+    table = A.table + (int64_t)it.b * A.max_blocks;
+    head = of;
+    last = (it.span.len - 1) / A.block_tokens;
+    blk = min(begin / A.block_tokens, last);
+    off = begin - blk * A.block_tokens;
   }
+  __device__ __forceinline__ void ask(const hq_cache_attn_args&, int32_t, int lane) { ask(lane); }
   __device__ __forceinline__ void ask(int lane) {
     first = blk;
-    int32_t x = min(blk + lane, last);
-    if (MODE != kAll) x += x > before ? skip : 0;
-    ids = table[x];
+    ids = table[min(blk + lane, last)];
   }
   // the wait for it stands here: at its uses it would wait for the tokens in flight
   __device__ __forceinline__ void got() { asm volatile("" : "+v"(ids)); }
@@ -459,38 +440,26 @@ struct CacheWalk {
     vs = run_of(A.v_scales, row * 4, n * 4);
   }
   // Starts the loads of the 32 tokens from t on into `step` (LDS) and moves the walk
-  // past them; live[h]: tokens of each half to attend to, of kAll their number, else one bit
-  // each.
+  // past them.
   template <int FMT>
-  __device__ __forceinline__ void fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step,
-                                        int32_t (&live)[2]) {
+  __device__ __forceinline__ Look fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step) {
     using R = CacheRing<FMT>;
     constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
     const uint32_t row_in = lane / CPR, chunk = lane % CPR;
     const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16;
+    Look look;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (t + 16 * h < end) {
-        if (MODE != kAll && t + 16 * h == jump && blk <= before) {
-          off = to_off;
-          ++blk;
-          enter<FMT, false>(A, lane);
-        } else if (off == A.block_tokens) {  // 16 divides a block
-          off = 0;
-          ++blk;
-          enter<FMT, false>(A, lane);
-        }
+      if (t + 16 * h < end && off == A.block_tokens) {  // 16 divides a block
+        off = 0;
+        ++blk;
+        enter<FMT, false>(A, lane);
       }
       // a half behind the end loads its block's first tokens, one of a block outside the
       // cache nothing (its buffers are empty), so that a step is always the same loads;
       // nothing reads them
-      if constexpr (MODE == kAll) {
-        live[h] = bad ? 0 : min(max(end - t - 16 * h, 0), 16);
-      } else {
-        // told to be the same in every lane: the loads' scalar offsets go by it
-        live[h] = (int32_t)readfirst(bad || t + 16 * h >= end ? 0u : span.bits(t + 16 * h + (blk > before ? gap : 0)));
-      }
-      const uint32_t place = live[h] ? off : 0;
+      look.live[h] = bad ? 0 : min(max(end - t - 16 * h, 0), 16);
+      const uint32_t place = look.live[h] ? off : 0;
       off += 16;
       uint8_t* to = step + h * R::HALF;
 #pragma unroll
@@ -502,6 +471,108 @@ struct CacheWalk {
       const uint32_t token = (lane & 15) * 4;  // four times over
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_void*)(to + R::SCALES), 4, token, place * 4, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_void*)(to + R::SCALES + 256), 4, token, place * 4, 0, 0);
+    }
+    return look;
+  }
+  __device__ __forceinline__ bool cut(const Look& x) const { return x.live[0] + x.live[1] < 32; }
+  __device__ __forceinline__ bool dead(const Look& x, int32_t, int h, int32_t i) const { return i >= x.live[h]; }
+};
+
+// A scalar base for lane offsets: addresses per lane would live through the whole loop.
+__device__ __forceinline__ const uint8_t* uniform(const void* p, int64_t bytes) {
+  const uint64_t a = (uint64_t)p + bytes;
+  return (const uint8_t*)((uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a));
+}
+typedef __attribute__((address_space(1))) const void glb_void;
+
+// The same of a window or a tree, some of whose tokens are left out.  A half's place is formed from its token by a multiplication, with
+// no state from half to half but the ids of the 64 blocks from `first` on, one a lane, so that
+// following the table costs a lane read and not a load that the next loads' addresses wait for.
+// Every instruction counts, scalar ones too (a wave issues one in some 7 cycles): what a step's
+// masks go by is formed when one is needed.  (Windows of 300 tokens 9.1 us, 9.5 with buffers of a
+// block and a window's state; whole sequences are bound by memory and take 1 to 3 % longer so.)
+struct SpanWalk {
+  using Look = uint32_t;  // what a fetch returns
+  const int32_t* table;
+  CacheSpan span;
+  int32_t gap, jump, head, last;  // last: the sequence's last block
+  int32_t ctx, open, sinks;       // all rows see [0, sinks) and [open, ctx)
+  int32_t first, ids;
+  int64_t stride, offset;         // vectors of a block, those before the head's
+  __device__ __forceinline__ void start(const hq_cache_attn_args& A, const CacheItem& it, int32_t of, int32_t) {
+    table = A.table + (int64_t)it.b * A.max_blocks;
+    span = it.span;
+    gap = span.gap();
+    jump = gap ? span.turn() : 0x7FFFFFFF;
+    head = of;
+    last = (span.len - 1) / A.block_tokens;
+    ctx = span.len - span.rows;
+    open = A.window ? ctx + span.rows - A.window : 0;
+    sinks = A.sinks;
+    stride = (int64_t)A.heads_kv * A.block_tokens;
+    offset = (int64_t)of * A.block_tokens;
+  }
+  __device__ __forceinline__ int32_t real(int32_t t) const { return t < jump ? t : t + gap; }
+  __device__ __forceinline__ int32_t block(const hq_cache_attn_args& A, int32_t at) const {
+    return min((int32_t)A.by_block.of((uint32_t)at), last);
+  }
+  __device__ __forceinline__ void ask(const hq_cache_attn_args& A, int32_t begin, int lane) {
+    ask(block(A, real(begin)), lane);
+  }
+  __device__ __forceinline__ void ask(int32_t blk, int lane) {
+    first = blk;
+    ids = table[min(blk + lane, last)];
+  }
+  __device__ __forceinline__ void got() { asm volatile("" : "+v"(ids)); }
+  template <int FMT, bool>
+  __device__ __forceinline__ void enter(const hq_cache_attn_args&, int) {}
+  // Starts the loads of the 32 tokens from t on into `step`.  Returns 1 + 2 + 4 where all rows see
+  // all of them, else 2 and 4 for the halves with tokens at all; one without loads the cache's
+  // first ones.
+  template <int FMT>
+  __device__ __forceinline__ Look fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step) {
+    using R = CacheRing<FMT>;
+    constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
+    const uint32_t row_in = lane / CPR, chunk = lane % CPR;
+    const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16, token = (lane & 15) * 4;
+    uint32_t all = 1, some = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t at = real(t + 16 * h), blk = block(A, at);
+      if (blk - first >= 64) {
+        ask(blk, lane);
+        got();
+      }
+      const int32_t id = __builtin_amdgcn_readlane(ids, blk - first);
+      const bool in = t + 16 * h < end, ok = in && (uint32_t)id < (uint32_t)A.blocks;
+      if (in && !ok && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
+      if (!ok || at + 16 > ctx || (at < open && at + 16 > sinks)) all = 0;
+      if (ok) some |= 2u << h;
+      const int64_t row = ok ? id * stride + offset + (at - blk * A.block_tokens) : 0;
+      uint8_t* to = step + h * R::HALF;
+      const uint8_t *k = uniform(A.k_codes, row * R::RB), *v = uniform(A.v_codes, row * R::RB);
+      glb_void *const kl = (glb_void*)(k + from), *const vl = (glb_void*)(v + from);
+      __builtin_amdgcn_global_load_lds(kl, (lds_void*)to, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(vl, (lds_void*)(to + R::V), 16, 0, 0);
+      if constexpr (RPL < 16) {  // the offset moves both places
+        __builtin_amdgcn_global_load_lds(kl, (lds_void*)to, 16, 1024, 0);
+        __builtin_amdgcn_global_load_lds(vl, (lds_void*)(to + R::V), 16, 1024, 0);
+      }
+      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.k_scales, row * 4) + token), (lds_void*)(to + R::SCALES), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.v_scales, row * 4) + token), (lds_void*)(to + R::SCALES + 256), 4, 0, 0);
+    }
+    return all | some;
+  }
+  __device__ __forceinline__ bool cut(Look seen) const { return !(seen & 1); }
+  __device__ __forceinline__ bool dead(Look seen, int32_t t, int h, int32_t i) const {
+    return !((seen >> h) & 2) || !((span.bits(real(t + 16 * h)) >> i) & 1);
+  }
+  // Of the 32 tokens from t on: each half's first and the bits of those that anybody sees.
+  __device__ __forceinline__ void about(int32_t t, uint32_t seen, int32_t (&live)[2], int32_t (&at)[2]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      at[h] = real(t + 16 * h);
+      live[h] = (seen >> h) & 2 ? (int32_t)span.bits(at[h]) : 0;
     }
   }
 };

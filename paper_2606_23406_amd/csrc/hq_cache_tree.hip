@@ -178,95 +178,6 @@ struct Behind {
   }
 };
 
-// A scalar base for lane offsets: addresses per lane would live through the whole loop.
-__device__ __forceinline__ const uint8_t* uniform(const void* p, int64_t bytes) {
-  const uint64_t a = (uint64_t)p + bytes;
-  return (const uint8_t*)((uint64_t)readfirst((uint32_t)(a >> 32)) << 32 | readfirst((uint32_t)a));
-}
-typedef __attribute__((address_space(1))) const void glb_void;
-
-// A wave's way over its tokens, through the ring of the one-token attention.  Next to the products
-// every instruction of a wave counts, scalar ones too (a wave issues one in some 7 cycles): a
-// half's place is formed from its token by a multiplication, with no state from half to half but
-// the ids of the 64 blocks from `first` on, one a lane, and what a step's masks go by is formed
-// when one is needed.  (The one-token attention's way, which keeps buffers of its block: 24
-// uneven trees in MXFP4 73.5 us.)
-struct TreeWalk {
-  const int32_t* table;
-  CacheSpan span;
-  int32_t gap, jump, head, last;  // last: the sequence's last block
-  int32_t ctx, open, sinks;       // all rows see [0, sinks) and [open, ctx)
-  int32_t first, ids;
-  int64_t stride, offset;         // vectors of a block, those before the head's
-  __device__ __forceinline__ void start(const hq_cache_attn_args& A, const CacheItem& it, int32_t of) {
-    table = A.table + (int64_t)it.b * A.max_blocks;
-    span = it.span;
-    gap = span.gap();
-    jump = gap ? span.turn() : 0x7FFFFFFF;
-    head = of;
-    last = (span.len - 1) / A.block_tokens;
-    ctx = span.len - span.rows;
-    open = A.window ? ctx + span.rows - A.window : 0;
-    sinks = A.sinks;
-    stride = (int64_t)A.heads_kv * A.block_tokens;
-    offset = (int64_t)of * A.block_tokens;
-  }
-  __device__ __forceinline__ int32_t real(int32_t t) const { return t < jump ? t : t + gap; }
-  __device__ __forceinline__ int32_t block(const hq_cache_attn_args& A, int32_t at) const {
-    return min((int32_t)A.by_block.of((uint32_t)at), last);
-  }
-  __device__ __forceinline__ void ask(int32_t blk, int lane) {
-    first = blk;
-    ids = table[min(blk + lane, last)];
-  }
-  __device__ __forceinline__ void got() { asm volatile("" : "+v"(ids)); }
-  // Starts the loads of the 32 tokens from t on into `step`.  Returns 1 + 2 + 4 where all rows see
-  // all of them, else 2 and 4 for the halves with tokens at all; one without loads the cache's
-  // first ones.
-  template <int FMT>
-  __device__ __forceinline__ uint32_t fetch(const hq_cache_attn_args& A, int32_t t, int32_t end, int lane, uint8_t* step) {
-    using R = CacheRing<FMT>;
-    constexpr uint32_t RPL = 1024 / R::RB, CPR = R::RB / 16;  // rows of a load, chunks of a row
-    const uint32_t row_in = lane / CPR, chunk = lane % CPR;
-    const uint32_t from = row_in * R::RB + (chunk ^ R::swizzle(row_in)) * 16, token = (lane & 15) * 4;
-    uint32_t all = 1, some = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int32_t at = real(t + 16 * h), blk = block(A, at);
-      if (blk - first >= 64) {
-        ask(blk, lane);
-        got();
-      }
-      const int32_t id = __builtin_amdgcn_readlane(ids, blk - first);
-      const bool in = t + 16 * h < end, ok = in && (uint32_t)id < (uint32_t)A.blocks;
-      if (in && !ok && head == 0 && lane == 0) report(A.stats, HQ_ERR_INVALID_ARG);
-      if (!ok || at + 16 > ctx || (at < open && at + 16 > sinks)) all = 0;
-      if (ok) some |= 2u << h;
-      const int64_t row = ok ? id * stride + offset + (at - blk * A.block_tokens) : 0;
-      uint8_t* to = step + h * R::HALF;
-      const uint8_t *k = uniform(A.k_codes, row * R::RB), *v = uniform(A.v_codes, row * R::RB);
-      glb_void *const kl = (glb_void*)(k + from), *const vl = (glb_void*)(v + from);
-      __builtin_amdgcn_global_load_lds(kl, (lds_void*)to, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(vl, (lds_void*)(to + R::V), 16, 0, 0);
-      if constexpr (RPL < 16) {  // the offset moves both places
-        __builtin_amdgcn_global_load_lds(kl, (lds_void*)to, 16, 1024, 0);
-        __builtin_amdgcn_global_load_lds(vl, (lds_void*)(to + R::V), 16, 1024, 0);
-      }
-      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.k_scales, row * 4) + token), (lds_void*)(to + R::SCALES), 4, 0, 0);
-      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.v_scales, row * 4) + token), (lds_void*)(to + R::SCALES + 256), 4, 0, 0);
-    }
-    return all | some;
-  }
-  // Of the 32 tokens from t on: each half's first and the bits of those that anybody sees.
-  __device__ __forceinline__ void about(int32_t t, uint32_t seen, int32_t (&live)[2], int32_t (&at)[2]) const {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      at[h] = real(t + 16 * h);
-      live[h] = (seen >> h) & 2 ? (int32_t)span.bits(at[h]) : 0;
-    }
-  }
-};
-
 // What a row sees, in LDS: only steps that some row does not see some token of look at it.
 struct TreeRow {
   uint64_t mask;  // ancestors
@@ -310,7 +221,7 @@ __device__ __forceinline__ bool one_lift(uint32_t least, uint32_t most) { return
 // with one for each of two ways the compiler keeps the accumulators twice.
 template <int RT>
 __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)[2][4], const float (&vs)[2][4], bool each,
-                                             float lift, const TreeWalk& w, int32_t t, uint32_t seen, const TreeRow* rows,
+                                             float lift, const SpanWalk& w, int32_t t, uint32_t seen, const TreeRow* rows,
                                              const float (&back)[RT], int lane, TreeState (&z)[RT],
                                              uint32_t (&pt)[RT][2][4]) {
   const int g = lane >> 4;
@@ -396,9 +307,9 @@ __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)
   }
 }
 
-// One step: the 32 tokens from t on, of which `seen` is what TreeWalk::fetch returned.
+// One step: the 32 tokens from t on, of which `seen` is what SpanWalk::fetch returned.
 template <int FMT, int RT>
-__device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const TreeWalk& w, int32_t t, uint32_t seen,
+__device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const SpanWalk& w, int32_t t, uint32_t seen,
                                           const uint32_t (&q)[RT][2][4][4], const TreeRow* rows, const float (&back)[RT],
                                           int lane, TreeState (&z)[RT]) {
   const int g = lane >> 4;
@@ -571,9 +482,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   const int32_t begin0 = (int32_t)(it.at * it.chunk), tokens = min(it.chunk, seen - begin0);
   const int32_t per = (tokens + 32 * WAVES - 1) / (32 * WAVES) * 32;
   const int32_t end = begin0 + min(tokens, (wave + 1) * per), begin = min(begin0 + wave * per, end);
-  TreeWalk w;
-  w.start(A, it, head);
-  w.ask(w.block(A, w.real(begin)), lane);
+  SpanWalk w;
+  w.start(A, it, head, begin);
+  w.ask(A, begin, lane);
   Raw8 qraw[RT] = {};
   const uint4 qd = sign_words(A.k_dsign16, head * HQ_TILE + c0);
 #pragma unroll

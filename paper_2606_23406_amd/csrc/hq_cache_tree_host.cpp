@@ -83,7 +83,6 @@ hq_status hq_cache_tree_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp,
   a.starts = starts;
   a.rows = (int32_t)rows;
   a.max_rows = max_tree;
-  a.by_block = hq_divide_by((uint32_t)k->block_tokens);
   a.by_group = hq_divide_by((uint32_t)a.group);
   while (1 << a.tile_shift < s.tile) ++a.tile_shift;
   a.max_tiles = (int32_t)s.tiles;

@@ -369,7 +369,7 @@ struct hq_cache_attn_args {
   const int32_t* starts;    // of trees: batch + 1 places in the rows
   const uint64_t* masks;    // of trees: ancestors, one per row
   int32_t rows, max_rows;   // of trees: rows of the call, of a sequence at most
-  hq_divisor by_block, by_group;  // of trees
+  hq_divisor by_block, by_group;  // by_group: of trees
   int32_t tile_shift, max_tiles;  // of trees: log2 of a tile's rows, tiles of max_rows
 };
 
