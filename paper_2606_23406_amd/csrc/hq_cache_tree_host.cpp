@@ -16,17 +16,19 @@ struct TreeSize {
   size_t bytes;  // enough for the call, and never less for a larger one
 };
 
-TreeSize tree_size(int64_t batch, int32_t heads, int32_t group, int64_t max_tokens, int32_t max_tree, int32_t window,
-                   int32_t sinks) {
+// `all`: drafted tokens of all sequences.
+TreeSize tree_size(int64_t batch, int64_t all, int32_t heads, int32_t group, int64_t max_tokens, int32_t max_tree,
+                   int32_t window, int32_t sinks) {
   TreeSize s;
   const int64_t rows = (int64_t)max_tree * group;
   s.seen = hq_cache_seen(max_tokens, window, sinks, max_tree);
-  s.tile = hq_tree_tile(rows, batch * heads, s.seen);
+  if (all > batch * max_tree) all = batch * max_tree;  // some are of no sequence
+  s.tile = hq_tree_tile(rows, all * group, batch, heads, s.seen);
   s.tiles = (rows + s.tile - 1) / s.tile;
   s.items = hq_tree_items(batch, heads, s.seen, s.tiles);
   s.joins = hq_cache_joins(batch, heads);
   s.parts = s.items * heads * s.tile;
-  // a bound on the parts that does not fall from one rule's tiles to another's
+  // a bound on the parts that does not fall from one rule's tiles to another's, nor go by `all`
   const int64_t least = rows <= 16 ? 16 : 4 * rows < 3 * 128 ? 32 : 128, padded = (rows + least - 1) / least * least;
   const int64_t most = (s.seen + HQ_CACHE_LEAST - 1) / HQ_CACHE_LEAST * batch * heads * padded;
   const int64_t even = batch * heads * padded + (HQ_CACHE_WG_TARGET + heads) * least, parts = most < even ? most : even;
@@ -62,7 +64,9 @@ hq_status hq_cache_window_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t v
 size_t hq_cache_tree_workspace_bytes(const hq_cache* k, int64_t batch, int32_t heads_q, int32_t max_blocks,
                                      int32_t max_tree, int32_t window, int32_t sinks) {
   if (!sizes_ok(k, batch, heads_q, max_blocks, window, sinks) || max_tree <= 0 || max_tree > 64) return 0;
-  return tree_size(batch, k->heads, heads_q / k->heads, (int64_t)max_blocks * k->block_tokens, max_tree, window, sinks).bytes;
+  return tree_size(batch, batch * max_tree, k->heads, heads_q / k->heads, (int64_t)max_blocks * k->block_tokens, max_tree,
+                   window, sinks)
+      .bytes;
 }
 
 hq_status hq_cache_tree_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp, const hq_cache* v, const void* q,
@@ -78,7 +82,8 @@ hq_status hq_cache_tree_attention(hq_plan_t kp, const hq_cache* k, hq_plan_t vp,
                                 sinks, out, ot, &a, &run);
   if (st != HQ_OK || !run) return st;
   if (!masks || !aligned(masks, 8) || !starts || !aligned(starts, 4)) return HQ_ERR_INVALID_ARG;
-  const TreeSize s = tree_size(batch, k->heads, a.group, (int64_t)max_blocks * k->block_tokens, max_tree, window, sinks);
+  const TreeSize s =
+      tree_size(batch, rows, k->heads, a.group, (int64_t)max_blocks * k->block_tokens, max_tree, window, sinks);
   a.masks = masks;
   a.starts = starts;
   a.rows = (int32_t)rows;

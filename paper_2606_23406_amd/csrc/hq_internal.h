@@ -428,25 +428,26 @@ static inline int64_t hq_cache_joins(int64_t batch, int64_t heads_kv) {
   return batch <= HQ_CACHE_UNPLANNED || batch < even ? batch : even;
 }
 
-// Rows of a tile of a tree attention, for so many rows of one KV head in each of `heads` heads of
-// all sequences together (HQ_TREE_* in workgroups, measured below):
+// Rows of a tile of a tree attention, for up to so many rows of one KV head in each of `batch`
+// sequences, `all` of them together, and `heads` KV heads (HQ_TREE_* in workgroups):
 //   16   up to 16 rows, and where sequences are not split while that gives at most HQ_TREE_SMALL
 //        workgroups: a call that leaves CUs idle is as long as its longest wave
 //   128  the codes turned into fp16 once for all of a workgroup's waves: where the tiles are
 //        three quarters full and fill the chip, which chunks do for split sequences
 //   32   else
-// 8 KV heads of 4, us: 16 sequences of 500 tokens and 8 rows each 13.0 in tiles of 16, 17.3 of
-// 32; 4 of 1000 and 32 17.4 and 26.1; 16 of 8192 and 8 97 and 78.  8 of 8192 tokens and 64 rows
-// 197 in tiles of 128, 221 of 32; 64 of 1000 and 16, groups of 8, 107 and 130; but 8 of 1000 and
-// 25 (256 workgroups of 128 rows) 73 and 34.
+// 8 KV heads of 4, int8, us: 16 sequences of 500 tokens and 8 rows each 12.1 in tiles of 16, 15.7 of
+// 32; 4 of 1000 and 32 14.5 and 23.4; 16 of 8192 and 8 86 and 69.  8 of 8192 tokens and 64 rows
+// 181 in tiles of 128, 195 of 32; 64 of 1000 and 16, groups of 8, 102 and 122; but 8 of 1000 and
+// 25 (256 workgroups of 128 rows) 65 and 23, and 24 of up to 6001 and up to 48, groups of 16, which
+// fill tiles of 128 by half, 227 and 199.
 #define HQ_TREE_SMALL 256
 #define HQ_TREE_WIDE 512
 #define HQ_TREE_WIDE_SPLIT 128
-static inline int32_t hq_tree_tile(int64_t rows, int64_t heads, int64_t seen) {
+static inline int32_t hq_tree_tile(int64_t rows, int64_t all, int64_t batch, int64_t heads, int64_t seen) {
   const bool split = seen > HQ_CACHE_WHOLE;
-  if (rows <= 16 || (!split && (rows + 15) / 16 * heads <= HQ_TREE_SMALL)) return 16;
-  const int64_t wide = (rows + 127) / 128;
-  return 4 * rows >= 3 * 128 * wide && wide * heads >= (split ? HQ_TREE_WIDE_SPLIT : HQ_TREE_WIDE) ? 128 : 32;
+  if (rows <= 16 || (!split && (rows + 15) / 16 * batch * heads <= HQ_TREE_SMALL)) return 16;
+  const int64_t wide = (rows + 127) / 128 * batch;
+  return 4 * all >= 3 * 128 * wide && wide * heads >= (split ? HQ_TREE_WIDE_SPLIT : HQ_TREE_WIDE) ? 128 : 32;
 }
 
 // RMS norm fused with the 8-bit activation prep.
