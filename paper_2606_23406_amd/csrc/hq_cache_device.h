@@ -485,10 +485,9 @@ __device__ __forceinline__ const uint8_t* uniform(const void* p, int64_t bytes) 
 }
 typedef __attribute__((address_space(1))) const void glb_void;
 
-// The same of a window or a tree, some of whose tokens are left out.  A half's place is formed from its token by a multiplication, with
-// no state from half to half but the ids of the 64 blocks from `first` on, one a lane, so that
-// following the table costs a lane read and not a load that the next loads' addresses wait for.
-// Every instruction counts, scalar ones too (a wave issues one in some 7 cycles): what a step's
+// The same of a window or a tree, some of whose tokens are left out.  A half's place is formed
+// from its token by a multiplication, with no state from half to half but the block ids.  Every
+// instruction counts, scalar ones too (a wave issues one in some 7 cycles): what a step's
 // masks go by is formed when one is needed.  (Windows of 300 tokens 9.1 us, 9.5 with buffers of a
 // block and a window's state; whole sequences are bound by memory and take 1 to 3 % longer so.)
 struct SpanWalk {
@@ -558,8 +557,9 @@ struct SpanWalk {
         __builtin_amdgcn_global_load_lds(kl, (lds_void*)to, 16, 1024, 0);
         __builtin_amdgcn_global_load_lds(vl, (lds_void*)(to + R::V), 16, 1024, 0);
       }
-      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.k_scales, row * 4) + token), (lds_void*)(to + R::SCALES), 4, 0, 0);
-      __builtin_amdgcn_global_load_lds((glb_void*)(uniform(A.v_scales, row * 4) + token), (lds_void*)(to + R::SCALES + 256), 4, 0, 0);
+      const uint8_t *ks = uniform(A.k_scales, row * 4), *vs = uniform(A.v_scales, row * 4);
+      __builtin_amdgcn_global_load_lds((glb_void*)(ks + token), (lds_void*)(to + R::SCALES), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((glb_void*)(vs + token), (lds_void*)(to + R::SCALES + 256), 4, 0, 0);
     }
     return all | some;
   }

@@ -18,11 +18,11 @@
 // than 2^-21 of the largest.  Scores, references and sums are fp32.  (Three bf16 terms hold all
 // 24 bits, for half as many products again and twice the instructions of cutting.)
 //
-// What bounds it: a row and token take 2 x 2 x 2 x 128 operations of the matrix cores and some
-// 8 instructions for 16 of them of a lane's softmax, two terms included.  Of two waves on a SIMD
-// the products of one hide a seventh of the other's vector instructions (4 products of
-// 16 x 16 x 32 beside 16 fma: 97 ns for both waves, 64 and 49 alone), so the time is nearly
-// their sum: of 198 us for 8 sequences of 8192 tokens, 64 rows, 8 KV heads of 4, int8, 39 lay
+// What bounds it: a row and token take 2 x 2 x 2 x 128 operations of the matrix cores, and a
+// lane's 16 of them some 8 instructions each for their softmax, two terms included.  Of two waves
+// on a SIMD the products of one hide a seventh of the other's vector instructions (4 products of
+// 16 x 16 x 32 beside 16 fma: 97 ns for both waves, 64 and 49 alone), so the time is nearly their
+// sum: of 198 us for 8 sequences of 8192 tokens, 64 rows, 8 KV heads of 4, int8 (182 since), 39 lay
 // before, behind and between the loops (11 the join); without the loads 150 were left, without
 // the softmax 123, without the second product 129.  (The codes' bytes take 29 us at a copy's
 // rate, the two terms' products 116 at that of a large matrix product.)
@@ -452,6 +452,9 @@ constexpr int tree_wave_bytes() {
   return CacheRing<FMT>::WAVE > out ? CacheRing<FMT>::WAVE : out;
 }
 
+// Tiles of 16 RT rows: every wave has all of them and its own tokens.  (24 uneven trees in MXFP4,
+// groups of 7: 70 us; the longest wave goes through 22 steps, some 5400 cycles each with two waves
+// a SIMD.  1 x 777 tokens 11.7 us: four steps and the chain around them.)
 template <int FMT, int RT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_kernel(
     hq_cache_attn_args A) {
@@ -599,7 +602,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 // steps of 32; each wave turns the keys and values of 16 of them into LDS in the order that the
 // products' operands are read in, a tile ahead of the products; the codes of the tile after it
 // are on their way in registers meanwhile.  (8 sequences of 8192 tokens and 64 rows, groups of 4:
-// 191 us, and 221 in tiles of 32 rows, whose waves each turn what they read.)
+// 181 us, and 195 in tiles of 32 rows, whose waves each turn what they read.  Tiles of 256 rows,
+// eight waves of one workgroup a CU, took 177, but uneven trees 299 where these took 221.)
 //
 // The products are 32 x 32 x 16: a step's scores are one tile C[token, row], in which lane l
 // holds tokens 8 q + 4 (l / 32) + r of row l % 32; with product t of the values contracting
@@ -927,11 +931,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     }
 #pragma unroll 1
     for (int step = 0; step < 2; ++step) {
-      const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32), about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
+      const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32);
+      const uint4 about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
       const int32_t live[2] = {(int32_t)readfirst(about0.z), (int32_t)readfirst(about1.z)};
       if ((live[0] | live[1]) == 0 || idle) continue;
       // the largest and least value scale: not negative, so ordered as their bits are
-      const uint32_t most = max(readfirst(about0.x), readfirst(about1.x)), least = min(readfirst(about0.y), readfirst(about1.y));
+      const uint32_t most = max(readfirst(about0.x), readfirst(about1.x));
+      const uint32_t least = min(readfirst(about0.y), readfirst(about1.y));
       const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
       bool each = (live[0] & live[1]) != 0xFFFF || !one_lift(least, most);
 #pragma unroll
