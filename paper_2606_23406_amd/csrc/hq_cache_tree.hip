@@ -126,11 +126,16 @@ __device__ __forceinline__ void tree_take(uint8_t* step, int lane, TreeStep<FMT>
   using R = CacheRing<FMT>;
   const uint32_t n = lane & 15, g = lane >> 4;
   if constexpr (FMT == kMx) {
-    // one lane per token and side: its scale as fp32 into the place of the bytes' first copy
+    // one lane per token and side: its scale as fp32 into the place of the bytes' first copy.  A
+    // wave's LDS operations keep their order, so the fence costs no wait: it holds the compiler
+    // from moving the lanes' reads of each other's scales above the writes
     uint8_t* at = step + ((lane >> 4) & 1) * R::HALF + R::SCALES + (lane >> 5) * 256 + n * 4;
     const uint32_t w = *(const uint32_t*)at;
     const uint32_t x = max(max(w & 0xFFu, (w >> 8) & 0xFFu), max((w >> 16) & 0xFFu, w >> 24));
-    *(uint32_t*)(at + 64) = x == 255u ? 0x7FC00000u : x << 23;
+    *(float*)(at + 64) = __uint_as_float(x == 255u ? 0x7FC00000u : x << 23);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
   }
   cache_take<FMT>(step, lane, s);
 #pragma unroll
