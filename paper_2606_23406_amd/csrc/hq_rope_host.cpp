@@ -98,10 +98,11 @@ hq_status hq_cache_append(hq_plan_t kp, const void* k, int64_t ldk, const hq_cac
   std::memset(&a, 0, sizeof(a));
   if ((st = fill_turns(r, positions, &a.turn)) != HQ_OK) return st;
   const bool both = vc != nullptr;
-  if (!float_type(xt) || rows < 0 || heads_q < 0 || (!q != !q_out) || (!q != !heads_q) || (q && !float_type(qot)))
-    return HQ_ERR_INVALID_ARG;
-  if (heads_q > 1 << 21 || rows > kMaxTiles / kc->heads || (q && rows > kMaxTiles / heads_q)) return HQ_ERR_UNSUPPORTED;
-  if (rows == 0) return HQ_OK;
+  if (!float_type(xt) || rows < 0 || heads_q < 0 || (heads_q && !float_type(qot))) return HQ_ERR_INVALID_ARG;
+  if (heads_q > 1 << 21 || rows > kMaxTiles / kc->heads || (heads_q && rows > kMaxTiles / heads_q))
+    return HQ_ERR_UNSUPPORTED;
+  if (rows == 0) return HQ_OK;  // no rows need no addresses
+  if ((!q != !q_out) || (!q != !heads_q)) return HQ_ERR_INVALID_ARG;
   const int64_t width = (int64_t)kc->heads * HQ_TILE, width_q = (int64_t)heads_q * HQ_TILE;
   if (!slots || !aligned(slots, 8) || !positions_ok(positions) || !rows_ok(k, xt, ldk, width) ||
       (both && !rows_ok(v, xt, ldv, width)))
