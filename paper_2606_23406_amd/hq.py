@@ -715,9 +715,10 @@ def hq_cache_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.
 class Rope:
     """Rotary positions (hq_rotary): `table` fp32 [positions, 2, dims / 2] (hq_rope_table
     makes one), the axis of each pair (a list of dims / 2 numbers; None: one axis), pairs
-    (i, i + dims / 2) or, interleaved, (2 i, 2 i + 1)."""
+    (i, i + dims / 2) or, interleaved, (2 i, 2 i + 1).  axes: positions of a row, 1 to 4 (by
+    default as many as the pairs use)."""
 
-    def __init__(self, table: torch.Tensor, interleaved=False, axis=None, stats=True):
+    def __init__(self, table: torch.Tensor, interleaved=False, axis=None, stats=True, axes=None):
         if table.dim() != 3 or table.shape[1] != 2 or table.dtype != torch.float32 or not table.is_contiguous() \
                 or not table.is_cuda:
             raise ValueError("table must be a contiguous fp32 device tensor [positions, 2, dims / 2]")
@@ -726,7 +727,9 @@ class Rope:
         if len(axis) != pairs or not all(0 <= a < 4 for a in axis):
             raise ValueError(f"axis must be {pairs} numbers from 0 to 3")
         self.table, self.axis, self.device = table, axis, table.device
-        self.axes = max(axis, default=0) + 1
+        self.axes = max(axis, default=0) + 1 if axes is None else int(axes)
+        if not max(axis, default=0) < self.axes <= 4:
+            raise ValueError(f"{self.axes} axes for pairs of axis {max(axis, default=0)}")
         self._axis = (C.c_uint8 * pairs)(*axis)
         self.stats = torch.zeros(STATS_BYTES // 4, dtype=torch.int32, device=table.device) if stats else None
         self.c = RotaryStruct(table.data_ptr(), table.shape[0], 2 * pairs, int(bool(interleaved)), self.axes, 0,
