@@ -828,8 +828,14 @@ def hq_cache_append(k_plan: Plan, k: torch.Tensor, k_cache: Cache, v_plan, v, v_
     return q_out
 
 
+def _tokens(n):
+    """A number of tokens for an int32 argument, which would keep a larger one's low bits: no sequence
+    has more than 2^30."""
+    return n if -1 <= n < 1 << 30 else 1 << 30 if n > 0 else -1
+
+
 def hq_cache_window_workspace_bytes(k_cache: Cache, batch, heads_q, max_blocks, window, sinks=0):
-    return lib().hq_cache_window_workspace_bytes(k_cache.ref, batch, heads_q, max_blocks, window, sinks)
+    return lib().hq_cache_window_workspace_bytes(k_cache.ref, batch, heads_q, max_blocks, _tokens(window), _tokens(sinks))
 
 
 def hq_cache_window_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor,
@@ -853,7 +859,8 @@ def hq_cache_window_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q:
         workspace, lambda: hq_cache_window_workspace_bytes(k, batch, heads_q, max_blocks, window, sinks), dev, stream)
     st = lib().hq_cache_window_attention(k_plan.handle, k.ref, v_plan.handle, v.ref, qp,
                                          _dtype_code(qt), batch, heads_q, 128 ** -0.5 if scale is None else scale, tp,
-                                         max_blocks, lp, window, sinks, _dense(out, ot, shape, dev, "out"),
+                                         max_blocks, lp, _tokens(window), _tokens(sinks),
+                                         _dense(out, ot, shape, dev, "out"),
                                          _dtype_code(ot), workspace.data_ptr(), workspace.nbytes,
                                          _stream_handle(stream))
     _check("hq_cache_window_attention", st)
@@ -861,7 +868,8 @@ def hq_cache_window_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q:
 
 
 def hq_cache_tree_workspace_bytes(k_cache: Cache, batch, heads_q, max_blocks, max_tree, window=0, sinks=0):
-    return lib().hq_cache_tree_workspace_bytes(k_cache.ref, batch, heads_q, max_blocks, max_tree, window, sinks)
+    return lib().hq_cache_tree_workspace_bytes(k_cache.ref, batch, heads_q, max_blocks, max_tree, _tokens(window),
+                                               _tokens(sinks))
 
 
 def hq_cache_tree_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: torch.Tensor, masks: torch.Tensor,
@@ -895,8 +903,8 @@ def hq_cache_tree_attention(k_plan: Plan, k: Cache, v_plan: Plan, v: Cache, q: t
         stream)
     st = lib().hq_cache_tree_attention(k_plan.handle, k.ref, v_plan.handle, v.ref, qp, _dtype_code(qt),
                                        rows, heads_q, 128 ** -0.5 if scale is None else scale, mp, sp, batch, max_tree,
-                                       tp, max_blocks, lp, window, sinks, _dense(out, ot, shape, dev, "out"),
-                                       _dtype_code(ot), workspace.data_ptr(), workspace.nbytes,
+                                       tp, max_blocks, lp, _tokens(window), _tokens(sinks),
+                                       _dense(out, ot, shape, dev, "out"), _dtype_code(ot), workspace.data_ptr(), workspace.nbytes,
                                        _stream_handle(stream))
     _check("hq_cache_tree_attention", st)
     return out
