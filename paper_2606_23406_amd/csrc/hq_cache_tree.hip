@@ -216,6 +216,11 @@ __device__ __forceinline__ float lift_of(uint32_t scale_bits) {
   return max((float)((int32_t)((scale_bits >> 23) & 0xFFu) - (126 + 8)), -94.0f);
 }
 
+// 2^x of a reference's move, x <= 0, as its root: a sum of weights takes it in two steps.  Zero vectors
+// have weights of up to 2^94 under their references, beside a value scale of 2^k others of 2^-k:
+// in one step what is left of the first would be 0 from k = 33 on.
+__device__ __forceinline__ float half_move(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
+
 // Whether one lift, the largest scale's, does for tokens whose scales lie between these: the
 // largest product of a row is then at least 2^1.
 __device__ __forceinline__ bool one_lift(uint32_t least, uint32_t most) { return (least >> 23) + 6 >= most >> 23; }
@@ -275,9 +280,9 @@ __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)
     for (int i = 0; i < RT; ++i) {
       // a row's own scores alone move it
       const float mn = top[i] > z[i].m + kSlack ? top[i] : z[i].m;
-      const float alpha = __builtin_amdgcn_exp2f(z[i].m - (mn == -__builtin_inff() ? 0.0f : mn));
+      const float root = half_move(z[i].m - (mn == -__builtin_inff() ? 0.0f : mn)), alpha = root * root;
       z[i].m = mn;
-      z[i].l *= alpha;
+      z[i].l = z[i].l * root * root;
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[i].acc[j] *= alpha;
     }
@@ -592,8 +597,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     const float ref = M == -__builtin_inff() ? 0.0f : M;
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) {
-      const float f = __builtin_amdgcn_exp2f(s_m[x][at_row] - ref);
-      L = __builtin_fmaf(f, s_l[x][at_row], L);
+      const float root = half_move(s_m[x][at_row] - ref), f = root * root;
+      L = __builtin_fmaf(root, root * s_l[x][at_row], L);
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(f, o_row(x, at_row)[c0 + k], v[k]);
     }
@@ -815,9 +820,9 @@ __device__ __forceinline__ void wide_weights(v16_t& c, const float* ks, const fl
   if (__ballot(top > z.m + kSlack)) {
     // a row's own scores alone move it
     const float mn = top > z.m + kSlack ? top : z.m;
-    const float alpha = __builtin_amdgcn_exp2f(z.m - (mn == -__builtin_inff() ? 0.0f : mn));
+    const float root = half_move(z.m - (mn == -__builtin_inff() ? 0.0f : mn)), alpha = root * root;
     z.m = mn;
-    z.l *= alpha;
+    z.l = z.l * root * root;
 #pragma unroll
     for (int d = 0; d < 4; ++d) z.acc[d] *= alpha;
   }
@@ -1040,8 +1045,8 @@ __global__ __launch_bounds__(256) void hq_cache_tree_join_kernel(hq_cache_attn_a
   const float ref = M == -__builtin_inff() ? 0.0f : M;
   float L = 0.0f, v[8] = {};
   auto add = [&](float mx, float lx, const float* ax) {
-    const float f = __builtin_amdgcn_exp2f(mx - ref);
-    L = __builtin_fmaf(f, lx, L);
+    const float root = half_move(mx - ref), f = root * root;
+    L = __builtin_fmaf(root, root * lx, L);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(f, ax[e], v[e]);
   };
