@@ -643,8 +643,9 @@ hq_status hq_cache_window_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan
  * queries (in the stored coordinates) enter the products with 22 bits of the row's largest
  * value, a weight times its token's value scale with 22 bits or 2^-21 of the row's largest such
  * product, whichever is coarser.  Results repeat bit for bit.  Infinities or NaN come out where a
- * score passes 3.4e38 or an attended key's |y| 2^95; value scales below 2^-96 lose low bits and
- * below 2^-118 all.  An E4M3 code that is a NaN (hq_cache_write stores none) makes every row of
+ * score passes 3.4e38 or an attended key's |y| 2^95; a value scale below 2^-92 beside larger ones
+ * loses low bits and one below 2^-114 all.  Value scales above 2^103, and sequences with none from
+ * 2^-80 on, take twice the time.  An E4M3 code that is a NaN (hq_cache_write stores none) makes every row of
  * its sequence NaN; a NaN scale the
  * rows that see its token.
  * Device-side, in k->stats (HQ_ERR_INVALID_ARG): lengths and block ids as hq_cache_attention;

@@ -28,6 +28,8 @@
 // rate, the two terms' products 116 at that of a large matrix product.)
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "hq_cache_device.h"
 #include "hq_lds.h"
 
@@ -60,7 +62,7 @@ __device__ __forceinline__ void two_terms(float x, float y, uint32_t& hi, uint32
 }
 
 // Int8 codes c + 128 as bytes 0 and 2 of a word, which are the fp16 numbers (c + 128) 2^-24:
-// c 2^-9.  The scales take the 2^9 (kCodeUnit).
+// c 2^-9.  A row's scores and its values' sum take the 2^9 (kCodeUnit).
 __device__ __forceinline__ uint32_t halves_of_bytes(uint32_t w) {
   const v2h_t x = __builtin_bit_cast(v2h_t, w);
   const v2h_t up = {(_Float16)32768.0f, (_Float16)32768.0f}, off = {(_Float16)-0.25f, (_Float16)-0.25f};
@@ -151,11 +153,7 @@ __device__ __forceinline__ void tree_take(uint8_t* step, int lane, TreeStep<FMT>
     } else {
       s.kf[h] = 1.0f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s.vf[h][r] = 1.0f;
-        s.ks[h][r] *= kCodeUnit<FMT>;
-        s.vs[h][r] *= kCodeUnit<FMT>;
-      }
+      for (int r = 0; r < 4; ++r) s.vf[h][r] = 1.0f;
     }
   }
 }
@@ -210,16 +208,64 @@ struct TreeState {
 // product down to 2^-2, and 2^-24 below.
 constexpr float kSlack = 7.0f;
 
-// A scale below 2^-87 stays where it is: products with it are small, and sums of the weights
-// alone fit.
+// A scale below 2^-83 stays where it is: products with it are small, and the sum of 2^30 tokens'
+// weights of up to 2^97 fits.
 __device__ __forceinline__ float lift_of(uint32_t scale_bits) {
-  return max((float)((int32_t)((scale_bits >> 23) & 0xFFu) - (126 + 8)), -94.0f);
+  return max((float)((int32_t)((scale_bits >> 23) & 0xFFu) - (126 + 8)), -90.0f);
 }
 
 // 2^x of a reference's move, x <= 0, as its root: a sum of weights takes it in two steps.  Zero vectors
-// have weights of up to 2^94 under their references, beside a value scale of 2^k others of 2^-k:
-// in one step what is left of the first would be 0 from k = 33 on.
+// have weights of up to 2^97 under their references, beside a value scale of 2^k others of 2^(7 - k):
+// in one step what is left of the first would be 0 from k = 44 on.
 __device__ __forceinline__ float half_move(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
+
+// ---- value scales and scores that one reference does not hold
+// It holds value scales from 2^-80 to 2^104: above, weights of 2^-20 of the largest would pass below
+// 2^-126, and below, products lose their 22 bits.  A wave (of tiles of 128 rows, a workgroup) that met
+// a step whose largest scale lies outside goes over its tokens again with two references a row
+// (`apart`): the largest score for the weights, and 2^unit beside it for the products, the largest
+// of which lies between 2^7 and 2^8 when it is set.  A product takes an exponential of its own there:
+// mantissa(scale) * 2^(score - reference + exponent - unit).  (8 sequences of 8192 tokens and 64
+// rows with scales of 2^104: 411 us, 175 with others.)
+__device__ __forceinline__ bool scales_apart(uint32_t most) {
+  return most >> 23 > 127 + 103 || (most != 0 && most >> 23 < 127 - 80);
+}
+
+// A value scale's exponent, and its other factor; of a zero vector none.
+__device__ __forceinline__ float scale_exp(float s) { return s == 0.0f ? -1000.0f : (float)__builtin_amdgcn_frexp_expf(s); }
+__device__ __forceinline__ float scale_mant(float s) { return __builtin_amdgcn_frexp_mantf(s); }
+
+// A row's move: the root of the factor of its sum of weights, and the factor of its values' sum.
+struct Move {
+  float root, values;
+};
+// To the largest score `top` and the largest score and exponent `most`(reference) beside it.
+template <typename MOST>
+__device__ __forceinline__ Move move_apart(float top, float& m, float& unit, MOST most) {
+  const float mn = __builtin_fmaxf(m, top), ref = mn == -__builtin_inff() ? 0.0f : mn, by = m - ref;
+  const float u = __builtin_fmaxf(__builtin_ceilf(__builtin_fmaxf(unit + by, most(ref) - 8.0f)), -140.0f);
+  const Move x = {half_move(by), __builtin_amdgcn_exp2f(by + (unit - u))};
+  m = mn;
+  unit = u;
+  return x;
+}
+
+// A weight, which `sum` takes, and its product with a value scale.  x: score - reference, -inf where
+// the row does not see the token, whose scale may be a NaN.
+__device__ __forceinline__ float product_apart(float x, float scale, float unit, float& sum) {
+  sum += __builtin_amdgcn_exp2f(x);
+  const float p = scale_mant(scale) * __builtin_amdgcn_exp2f(x + (scale_exp(scale) - unit));
+  return x == -__builtin_inff() ? 0.0f : p;
+}
+
+// A row's sums with two references as those of one, both within fp32.  Returns the factor of the
+// values' sum.
+__device__ __forceinline__ float join_apart(float unit, float& m, float& l) {
+  const float left = __builtin_fminf(__builtin_fmaxf(unit, -48.0f), 48.0f);
+  m += unit - left;
+  l *= __builtin_amdgcn_exp2f(left - unit);
+  return __builtin_amdgcn_exp2f(left);
+}
 
 // Whether one lift, the largest scale's, does for tokens whose scales lie between these: the
 // largest product of a row is then at least 2^1.
@@ -317,11 +363,55 @@ __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)
   }
 }
 
-// One step: the 32 tokens from t on, of which `seen` is what SpanWalk::fetch returned.
-template <int FMT, int RT>
+// The same with two references.
+template <int RT>
+__device__ __forceinline__ void tree_weights_apart(v4_t (&c)[RT][2], const float (&ks)[2][4], const float (&vs)[2][4],
+                                                   bool each, const SpanWalk& w, int32_t t, uint32_t seen,
+                                                   const TreeRow* rows, const float (&back)[RT], int lane, float (&unit)[RT],
+                                                   TreeState (&z)[RT], uint32_t (&pt)[RT][2][4]) {
+  const int g = lane >> 4;
+  int32_t live[2], at[2];
+  w.about(t, seen, live, at);
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const TreeRow row = rows[16 * i + (lane & 15)];
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t sees = each ? (row.sees(at[h], w.ctx, w.sinks) & (uint32_t)live[h]) >> (4 * g) : 15u;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        c[i][h][r] = (sees >> r) & 1 ? c[i][h][r] * ks[h][r] * back[i] : -__builtin_inff();
+        top = __builtin_fmaxf(top, c[i][h][r]);
+      }
+    }
+    const Move by = move_apart(groups_max(top), z[i].m, unit[i], [&](float ref) {
+      float most = -__builtin_inff();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) most = __builtin_fmaxf(most, c[i][k >> 2][k & 3] - ref + scale_exp(vs[k >> 2][k & 3]));
+      return groups_max(most);
+    });
+    z[i].l = z[i].l * by.root * by.root;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[i].acc[j] *= by.values;
+    const float ref = z[i].m == -__builtin_inff() ? 0.0f : z[i].m;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float p[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[r] = product_apart(c[i][h][r] - ref, vs[h][r], unit[i], z[i].l);
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) two_terms(p[r], p[r + 1], pt[i][0][2 * h + r / 2], pt[i][1][2 * h + r / 2]);
+    }
+  }
+}
+
+// One step: the 32 tokens from t on, of which `seen` is what SpanWalk::fetch returned.  odd: the
+// wave has met value scales that one reference does not hold.  unit: of APART.
+template <int FMT, int RT, bool APART>
 __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const SpanWalk& w, int32_t t, uint32_t seen,
                                           const uint32_t (&q)[RT][2][4][4], const TreeRow* rows, const float (&back)[RT],
-                                          int lane, TreeState (&z)[RT]) {
+                                          int lane, bool& odd, float (&unit)[RT], TreeState (&z)[RT]) {
   const int g = lane >> 4;
   bool each = !(seen & 1);  // some row does not see some token
   if (each) {
@@ -345,7 +435,10 @@ __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const SpanWalk& w,
     least = __builtin_fminf(least, cur.vs[i >> 2][i & 3]);
   }
   const uint32_t hi = readfirst(__float_as_uint(groups_max(most))), lo = readfirst(__float_as_uint(-groups_max(-least)));
-  each |= !one_lift(lo, hi);
+  if (!APART) {
+    each |= !one_lift(lo, hi);
+    odd |= scales_apart(hi);
+  }
   v4_t c[RT][2];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
@@ -371,7 +464,10 @@ __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const SpanWalk& w,
         for (int i = 0; i < RT; ++i) c[i][h] = mfma_f16(a[h], q[i][t][s], c[i][h]);
   }
   uint32_t pt[RT][2][4];
-  tree_weights<RT>(c, cur.ks, cur.vs, each, lift_of(hi), w, t, seen, rows, back, lane, z, pt);
+  if constexpr (APART)
+    tree_weights_apart<RT>(c, cur.ks, cur.vs, each, w, t, seen, rows, back, lane, unit, z, pt);
+  else
+    tree_weights<RT>(c, cur.ks, cur.vs, each, lift_of(hi), w, t, seen, rows, back, lane, z, pt);
   // value codes: per word the tokens' pairs of each of its dims
 #pragma unroll
   for (int w = 0; w < CacheStep<FMT>::VW; ++w) {
@@ -526,7 +622,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   // step s of the contraction takes dims 32 (l / 16) + 8 s + j in lane l (the codes
   // that the lane's one run of 32 holds)
   uint32_t q[RT][2][4][4];
-  float back[RT];  // 1 / the power of two that a row was moved by
+  float back[RT];  // 1 / the power of two that a row was moved by, times the codes' unit
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
 #pragma unroll
@@ -536,44 +632,61 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
         const uint4 x = *(const uint4*)(q_row(16 * i + n, t) + 32 * g + 8 * s);
         q[i][t][s][0] = x.x; q[i][t][s][1] = x.y; q[i][t][s][2] = x.z; q[i][t][s][3] = x.w;
       }
-    back[i] = s_f[16 * i + n];
+    back[i] = s_f[16 * i + n] * kCodeUnit<FMT>;
   }
   __syncthreads();  // the queries' place is loaded over
 
   TreeState z[RT];
+  bool odd = false;
+  float unit[RT] = {};
+  auto way = [&](auto apart) {
+    constexpr bool APART = decltype(apart)::value;
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    z[i].m = -__builtin_inff();
-    z[i].l = 0.0f;
+    for (int i = 0; i < RT; ++i) {
+      z[i].m = -__builtin_inff();
+      z[i].l = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z[i].acc[k] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  if (begin + 32 < end) next = w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP);
-  int32_t slot = 0;
-  Behind first;
-  first.start(begin, (end - begin) / 128 * 32);
-  for (int32_t t = begin; t < end; t += 32) {
-    first.at(t, end);
-    // the loads of this step are done when at most the next step's are not
-    if (t + 32 < end)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    TreeStep<FMT> cur;
-    tree_take<FMT>(ring + slot * R::STEP, lane, cur);
-    const uint32_t here = sees;
-    sees = next;
-    if (t + 64 < end) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
-      next = w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP);
+      for (int k = 0; k < 8; ++k) z[i].acc[k] = (v4_t){0.0f, 0.0f, 0.0f, 0.0f};
     }
-    slot ^= 1;
-    tree_step<FMT, RT>(cur, w, t, here, q, s_row, back, lane, z);
+    if (begin + 32 < end) next = w.template fetch<FMT>(A, begin + 32, end, lane, ring + R::STEP);
+    int32_t slot = 0;
+    Behind first;
+    first.start(begin, (end - begin) / 128 * 32);
+    for (int32_t t = begin; t < end; t += 32) {
+      first.at(t, end);
+      // the loads of this step are done when at most the next step's are not
+      if (t + 32 < end)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      TreeStep<FMT> cur;
+      tree_take<FMT>(ring + slot * R::STEP, lane, cur);
+      const uint32_t here = sees;
+      sees = next;
+      if (t + 64 < end) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
+        next = w.template fetch<FMT>(A, t + 64, end, lane, ring + slot * R::STEP);
+      }
+      slot ^= 1;
+      tree_step<FMT, RT, APART>(cur, w, t, here, q, s_row, back, lane, odd, unit, z);
+    }
+  };
+  way(std::false_type());
+  if (__builtin_expect(odd, 0)) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
+    w.ask(A, begin, lane);
+    w.got();
+    sees = w.template fetch<FMT>(A, begin, end, lane, ring);
+    way(std::true_type());
   }
   // ---- the waves' sums under one reference, one row per 16 lanes
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     z[i].l = groups_sum(z[i].l);
+    float by = kCodeUnit<FMT>;
+    if (odd) by *= join_apart(unit[i], z[i].m, z[i].l);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[i].acc[k] *= by;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float* o = o_row(wave, 16 * i + n) + (4 * g + r) * 8;
@@ -692,7 +805,7 @@ __device__ __forceinline__ uint32_t token_scale(uint32_t w) {
     const uint32_t x = largest_byte(w);
     return x == 255u ? 0x7FC00000u : x << 23;
   } else {
-    return __float_as_uint(__uint_as_float(w) * kCodeUnit<FMT>);
+    return w;
   }
 }
 
@@ -847,6 +960,45 @@ __device__ __forceinline__ void wide_weights(v16_t& c, const float* ks, const fl
   }
 }
 
+// The same with two references.
+__device__ __forceinline__ void wide_weights_apart(v16_t& c, const float* ks, const float* vs, bool each,
+                                                   const int32_t (&live)[2], const int32_t (&at)[2], int32_t ctx,
+                                                   int32_t sinks, const TreeRow* rows, float back, int lane, float& unit,
+                                                   WideState& z, uint32_t (&pt)[2][2][4]) {
+  const int u = lane >> 5;
+  auto both = [](float x) {
+    const v2u_t t = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __builtin_fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+  };
+  const TreeRow row = rows[lane & 31];
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int h = k >> 3, token = 8 * (k >> 2) + 4 * u + (k & 3);
+    const uint32_t sees = each ? row.sees(at[h], ctx, sinks) & (uint32_t)live[h] : 0xFFFFu;
+    c[k] = (sees >> (token & 15)) & 1 ? c[k] * ks[token] * back : -__builtin_inff();
+    top = __builtin_fmaxf(top, c[k]);
+  }
+  const Move by = move_apart(both(top), z.m, unit, [&](float ref) {
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) most = __builtin_fmaxf(most, c[k] - ref + scale_exp(vs[8 * (k >> 2) + 4 * u + (k & 3)]));
+    return both(most);
+  });
+  z.l = z.l * by.root * by.root;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) z.acc[d] *= by.values;
+  const float ref = z.m == -__builtin_inff() ? 0.0f : z.m;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = product_apart(c[4 * q + r] - ref, vs[8 * q + 4 * u + r], unit, z.l);
+    two_terms(p[0], p[1], pt[0][q / 2][2 * (q & 1)], pt[1][q / 2][2 * (q & 1)]);
+    two_terms(p[2], p[3], pt[0][q / 2][2 * (q & 1) + 1], pt[1][q / 2][2 * (q & 1) + 1]);
+  }
+}
+
 template <int FMT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_wide_kernel(hq_cache_attn_args A) {
   using T = TreeTile<FMT>;
@@ -854,6 +1006,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   extern __shared__ __attribute__((aligned(16))) uint8_t s_tile[];  // two tiles
   __shared__ float s_m[ROWS], s_l[ROWS], s_f[ROWS];
   __shared__ TreeRow s_row[ROWS];
+  __shared__ uint32_t s_odd;  // some wave has met value scales that one reference does not hold
   static_assert(ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
   auto o_row = [&](int row) { return (float*)s_tile + row * kOPitch; };
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4;
@@ -881,6 +1034,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   way.template load<FMT>(A, begin + 16 * wave, end, lane, loads);
   const int32_t ctx = it.span.len - rows;
   if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
+  if (tid == 0) s_odd = 0u;
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each,
   // [32 rows][term][contraction step][lane] 16 bytes; the next ones are on their way meanwhile
   const uint4 qd = sign_words(A.k_dsign16, head * HQ_TILE + c0);
@@ -914,74 +1068,94 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       const uint4 x = *(const uint4*)(s_tile + ((wave * 2 + t) * 8 + s) * 1024 + lane * 16);
       q[t][s][0] = x.x; q[t][s][1] = x.y; q[t][s][2] = x.z; q[t][s][3] = x.w;
     }
-  const float back = s_f[32 * wave + (lane & 31)];  // 1 / the power of two that the row was moved by
+  // 1 / the power of two that the row was moved by, times the codes' unit
+  const float back = s_f[32 * wave + (lane & 31)] * kCodeUnit<FMT>;
   __syncthreads();  // the queries' place is written over
   WideState z;
-  z.m = -__builtin_inff();
-  z.l = 0.0f;
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int k = 0; k < 16; ++k) z.acc[d][k] = 0.0f;
   // from here on every row's window has begun
   const int32_t open = A.window ? ctx + rows - A.window : 0;
   const bool idle = tile * ROWS + 32 * wave >= rows * A.group;  // the wave has no rows
-  turn<FMT>(loads, s_tile, wave, lane);
-  if (begin + kTreeTile < end) way.template load<FMT>(A, begin + kTreeTile + 16 * wave, end, lane, loads);
-  tile_barrier();
-  uint8_t* at_tile = s_tile;
-  uint8_t* to_tile = s_tile + T::BYTES;
-  Behind first;
-  first.start(begin, (end - begin) / (4 * kTreeTile) * kTreeTile);
-  for (int32_t t = begin; t < end; t += kTreeTile) {
-    first.at(t, end);
-    if (t + kTreeTile < end) {
-      turn<FMT>(loads, to_tile, wave, lane);
-      if (t + 2 * kTreeTile < end) way.template load<FMT>(A, t + 2 * kTreeTile + 16 * wave, end, lane, loads);
-    }
-#pragma unroll 1
-    for (int step = 0; step < 2; ++step) {
-      const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32);
-      const uint4 about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
-      const int32_t live[2] = {(int32_t)readfirst(about0.z), (int32_t)readfirst(about1.z)};
-      if ((live[0] | live[1]) == 0 || idle) continue;
-      // the largest and least value scale: not negative, so ordered as their bits are
-      const uint32_t most = max(readfirst(about0.x), readfirst(about1.x));
-      const uint32_t least = min(readfirst(about0.y), readfirst(about1.y));
-      const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
-      bool each = (live[0] & live[1]) != 0xFFFF || !one_lift(least, most);
+  float unit = 0.0f;
+  auto tokens = [&](auto apart) {
+    constexpr bool APART = decltype(apart)::value;
+    z.m = -__builtin_inff();
+    z.l = 0.0f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
-      v16_t c;
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int k = 0; k < 16; ++k) c[k] = 0.0f;
-#pragma unroll
-      for (int s = 0; s < 8; ++s) {
-        const uint4 a = *(const uint4*)(at_tile + ((step * 8 + s) * 64 + lane) * 16);
-#pragma unroll
-        for (int t1 = 1; t1 >= 0; --t1) c = mfma_f16(a, q[t1][s], c);
-      }
-      uint32_t pt[2][2][4];
-      wide_weights(c, (const float*)(at_tile + T::KS) + step * 32, (const float*)(at_tile + T::VS) + step * 32, each,
-                   lift_of(most), live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, z, pt);
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const uint4 v = *(const uint4*)(at_tile + T::V + (((step * 4 + d) * 2 + k) * 64 + lane) * 16);
-#pragma unroll
-          for (int t1 = 1; t1 >= 0; --t1) z.acc[d] = mfma_f16(v, pt[t1][k], z.acc[d]);
-        }
-    }
+      for (int k = 0; k < 16; ++k) z.acc[d][k] = 0.0f;
+    turn<FMT>(loads, s_tile, wave, lane);
+    if (begin + kTreeTile < end) way.template load<FMT>(A, begin + kTreeTile + 16 * wave, end, lane, loads);
     tile_barrier();
-    uint8_t* const x = at_tile;
-    at_tile = to_tile;
-    to_tile = x;
+    uint8_t* at_tile = s_tile;
+    uint8_t* to_tile = s_tile + T::BYTES;
+    Behind first;
+    first.start(begin, (end - begin) / (4 * kTreeTile) * kTreeTile);
+    for (int32_t t = begin; t < end; t += kTreeTile) {
+      first.at(t, end);
+      if (t + kTreeTile < end) {
+        turn<FMT>(loads, to_tile, wave, lane);
+        if (t + 2 * kTreeTile < end) way.template load<FMT>(A, t + 2 * kTreeTile + 16 * wave, end, lane, loads);
+      }
+#pragma unroll 1
+      for (int step = 0; step < 2; ++step) {
+        const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32);
+        const uint4 about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
+        const int32_t live[2] = {(int32_t)readfirst(about0.z), (int32_t)readfirst(about1.z)};
+        if ((live[0] | live[1]) == 0 || idle) continue;
+        // the largest and least value scale: not negative, so ordered as their bits are
+        const uint32_t most = max(readfirst(about0.x), readfirst(about1.x));
+        const uint32_t least = min(readfirst(about0.y), readfirst(about1.y));
+        const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
+        bool each = (live[0] & live[1]) != 0xFFFF || (!APART && !one_lift(least, most));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
+        if (!APART && __builtin_expect(scales_apart(most), 0)) s_odd = 1u;
+        v16_t c;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) c[k] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          const uint4 a = *(const uint4*)(at_tile + ((step * 8 + s) * 64 + lane) * 16);
+#pragma unroll
+          for (int t1 = 1; t1 >= 0; --t1) c = mfma_f16(a, q[t1][s], c);
+        }
+        uint32_t pt[2][2][4];
+        const float *ks = (const float*)(at_tile + T::KS) + step * 32, *vs = (const float*)(at_tile + T::VS) + step * 32;
+        if constexpr (APART)
+          wide_weights_apart(c, ks, vs, each, live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, unit, z, pt);
+        else
+          wide_weights(c, ks, vs, each, lift_of(most), live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, z, pt);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint4 v = *(const uint4*)(at_tile + T::V + (((step * 4 + d) * 2 + k) * 64 + lane) * 16);
+#pragma unroll
+            for (int t1 = 1; t1 >= 0; --t1) z.acc[d] = mfma_f16(v, pt[t1][k], z.acc[d]);
+          }
+      }
+      tile_barrier();
+      uint8_t* const x = at_tile;
+      at_tile = to_tile;
+      to_tile = x;
+    }
+  };
+  tokens(std::false_type());
+  const bool odd = readfirst(s_odd) != 0u;
+  if (__builtin_expect(odd, 0)) {
+    way.ask(A, begin + 16 * wave);
+    way.template load<FMT>(A, begin + 16 * wave, end, lane, loads);
+    tokens(std::true_type());
   }
   // ---- the sums, one row per 16 lanes
   {
     const v2u_t l = __builtin_amdgcn_permlane32_swap(__float_as_uint(z.l), __float_as_uint(z.l), false, false);
     const int u = lane >> 5, at_row = 32 * wave + (lane & 31);
+    float sum = __uint_as_float(l[0]) + __uint_as_float(l[1]), by = kCodeUnit<FMT>;
+    if (odd) by *= join_apart(unit, z.m, sum);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) z.acc[d] *= by;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {  // i / 4 % 2 = k / 4, i % 4 = k % 4
       const int i = 4 * (k >> 2) + (k & 3);
@@ -991,7 +1165,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     }
     if (u == 0) {
       s_m[at_row] = z.m;
-      s_l[at_row] = __uint_as_float(l[0]) + __uint_as_float(l[1]);
+      s_l[at_row] = sum;
     }
   }
   __syncthreads();

@@ -1,17 +1,19 @@
 """The tree attention at both ends of fp32's range, in tiles of 16, 32 and 128 rows, against the
-definitions in 64 bits (tests/rows64.py)."""
+definitions in 64 bits (tests/rows64.py): value scales of any size, zero vectors among them."""
 import numpy as np
 import pytest
 import torch
 
 from tests import cache64 as R
 from tests import rows64 as W
+from tests import test_gpu_cache_long_ways as L
 from tests.test_gpu_cache_tree import FMTS, Case, hq  # noqa: F401  (hq: the fixture)
 from tests.test_gpu_cache_tree_full_tiles import FILL, MOST, Full
 
 pytestmark = pytest.mark.gpu
-U = R.U
+N, U = R.N, R.U
 TILES = ["16", "32", "128"]
+TOP = {"int8": 127.0, "e4m3": 448.0, "mxfp4": 6.0}
 
 
 def case(hq, fmt, tile, lens, trees, **kw):
@@ -25,7 +27,7 @@ def case(hq, fmt, tile, lens, trees, **kw):
     return Full(hq, fmt, list(lens) + [3] * FILL, list(trees) + [1] * FILL, heads, group, bt, pool=pool, max_tree=MOST, **kw)
 
 
-def set_scales(c, cache, exponents):
+def set_scales(cache, exponents):
     """Value or key scales 2^exponents, [blocks, block_tokens]."""
     e = exponents[:, None, :].expand(cache.scales.shape[:3])
     if R.name(cache) == "mxfp4":
@@ -44,14 +46,85 @@ def compare(c, out):
     assert torch.equal(c.run(), out) and c.kc.read_stats()["status"] == 0
 
 
+# the largest scale's exponent whose vectors, as random_cache draws them, stay below 3.4e38
+LARGEST = {"int8": 120, "e4m3": 119, "mxfp4": 124}
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("tile", TILES)
-@pytest.mark.parametrize("exponent", [38, 90])
+@pytest.mark.parametrize("low,high", [(95, 108), (110, None), (-40, None), (-120, -100), (-100, -20), (-90, 30)])
+def test_value_scales(hq, fmt, tile, low, high):
+    """All scales large, all small, or from small to large; a score's weight does not depend on them."""
+    print(f"[tree] range {fmt} {tile} {low} .. {high}", flush=True)
+    c = case(hq, fmt, tile, [400, 90, 1500], [9, 20, 30], seed=40)
+    c.vc.codes.copy_(R.random_cache(hq, c.vp, fmt, c.vc.blocks, 2, 32, 41).codes.cpu())
+    g = torch.Generator().manual_seed(low + 200)
+    set_scales(c.vc, torch.randint(low, LARGEST[fmt] + 1 if high is None else high, (60, 32), generator=g))
+    compare(c, c.run())
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("exponent", [38, 90, 118])
 def test_zero_vectors_beside_large_values(hq, fmt, tile, exponent):
     """Half of the tokens are zero vectors, whole steps of them: they keep their part of the weights."""
     print(f"[tree] range zeros {fmt} {tile} {exponent}", flush=True)
     c = case(hq, fmt, tile, [400, 90, 1500], [9, 20, 30], seed=42)
-    set_scales(c, c.vc, torch.full((60, 32), exponent))
+    set_scales(c.vc, torch.full((60, 32), exponent))
     c.vc.codes[::2] = 0
     c.vc.scales[::2] = 0
     compare(c, c.run())
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("exponent", [0, 100, 112, 118])
+def test_many_tokens_of_small_weight(hq, fmt, tile, exponent):
+    """One token has the largest weight, each of 16000 others 2^-17 of it: an eighth in all."""
+    print(f"[tree] range weights {fmt} {tile} {exponent}", flush=True)
+    c = case(hq, fmt, tile, [16000], [4], seed=43, pool=500)
+    c.table[0] = torch.randperm(500, generator=torch.Generator().manual_seed(2))
+    code = {"int8": 64, "e4m3": 0x38, "mxfp4": 0x22}[fmt]  # 64, 1 and 1
+    unit = {"int8": 64.0, "e4m3": 1.0, "mxfp4": 1.0}[fmt]
+    # queries whose transform is 128 in the first value alone, keys of one code: scores go by the key's scale
+    c.kc.codes.copy_(torch.full(c.kc.codes.shape, code, dtype=c.kc.codes.dtype))
+    d = torch.from_numpy(R.signs(R.SEED_K, 2 * N)).float().view(2, 1, N).expand(2, 4, N).reshape(1, 8, N)
+    c.q = d.expand(c.q.shape).contiguous()
+    # 17 bits: scale * 128 * unit * (2^0 - 2^-20 of the key) / 128 = 17 ln 2, nearly
+    c.scale = 17 * np.log(2.0) / unit
+    set_scales(c.kc, torch.full((c.kc.blocks, 32), -20))
+    blk, at = int(c.table[0, 40]), 7
+    c.kc.scales[blk, :, at] = 1.0 if fmt != "mxfp4" else 127
+    set_scales(c.vc, torch.full((c.vc.blocks, 32), exponent))
+    out = c.run()
+    ref, _ = c.reference()
+    # 16000 tokens: sums of the weights and of the products, and 60 roundings more; scores of 17 bits move a weight by 2 * 150 U * 17
+    big = 2.0 ** exponent * TOP[fmt]
+    rows = slice(0, 4)
+    assert (np.abs(out[rows].cpu().numpy() - ref[rows]) <= (16060 + 2 * 150 * 17) * U * big).all()
+    assert np.linalg.norm(out[rows].cpu().numpy() - ref[rows]) <= 64 * U * 17 * np.linalg.norm(ref[rows])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("window,sinks,group,tree", [(0, 0, 1, 2), (2000, 1500, 4, 7), (0, 0, 8, 16)])
+def test_large_values_on_long_ways(hq, fmt, window, sinks, group, tree):
+    """Ways of more blocks than a wave asks for at once, gone over twice; the largest scales come late."""
+    print(f"[tree] range long ways {fmt} {window} {sinks} {group} x {tree}", flush=True)
+    lens = L.lengths()
+    kp, vp, kc, vc, table, g = L.cache(hq, fmt, lens)
+    exponents = torch.randint(-10, 90, (200, L.BT), generator=g)
+    exponents[150:] += 25
+    table[:, :-150] %= 150
+    set_scales(vc, exponents)
+    trees = np.full(L.B, tree)
+    masks = [m for n in trees for m in W.random_tree(np.random.default_rng(5), int(n))]
+    starts = np.concatenate(([0], np.cumsum(trees))).astype(np.int32)
+    q = torch.randn((int(starts[-1]), L.HEADS * group, N), generator=g)
+    out = hq.hq_cache_tree_attention(kp, kc, vp, vc, q.cuda(), W.mask_tensor(masks).cuda(), torch.from_numpy(starts).cuda(), tree,
+                                     table.cuda(), torch.from_numpy(lens).to(torch.int32).cuda(), window=window, sinks=sinks).cpu().numpy()
+    kv, vv = R.values(kc), R.values(vc)
+    for b in L.LOOKED_AT:
+        r = slice(starts[b], starts[b + 1])
+        live = W.tree_visible(int(lens[b]), masks[r], window, sinks)
+        want, tol = W.attend(q[r].numpy(), kv, vv, table[b].numpy(), live, L.BT, N ** -0.5, L.HEADS, group)
+        W.check(out[r], want, tol, scale=N ** -0.5)
