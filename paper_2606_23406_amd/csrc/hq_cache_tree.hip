@@ -221,8 +221,10 @@ __device__ __forceinline__ float half_move(float x) { return __builtin_amdgcn_ex
 
 // ---- value scales and scores that one reference does not hold
 // It holds value scales from 2^-80 to 2^104: above, weights of 2^-20 of the largest would pass below
-// 2^-126, and below, products lose their 22 bits.  A wave (of tiles of 128 rows, a workgroup) that met
-// a step whose largest scale lies outside goes over its tokens again with two references a row
+// 2^-126, and below, products lose their 22 bits.  And it holds scores (of base 2) up to 2^24, above
+// which the lift is lost in a score's rounding.  A wave (of tiles of 128 rows, a workgroup) that met
+// a step whose largest scale lies outside, or such a reference, goes over its tokens again with two
+// references a row
 // (`apart`): the largest score for the weights, and 2^unit beside it for the products, the largest
 // of which lies between 2^7 and 2^8 when it is set.  A product takes an exponential of its own there:
 // mantissa(scale) * 2^(score - reference + exponent - unit).  (8 sequences of 8192 tokens and 64
@@ -230,6 +232,8 @@ __device__ __forceinline__ float half_move(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ bool scales_apart(uint32_t most) {
   return most >> 23 > 127 + 103 || (most != 0 && most >> 23 < 127 - 80);
 }
+
+__device__ __forceinline__ bool score_apart(float m) { return __builtin_fabsf(m) > 0x1p24f && m != -__builtin_inff(); }
 
 // A value scale's exponent, and its other factor; of a zero vector none.
 __device__ __forceinline__ float scale_exp(float s) { return s == 0.0f ? -1000.0f : (float)__builtin_amdgcn_frexp_expf(s); }
@@ -278,7 +282,7 @@ __device__ __forceinline__ bool one_lift(uint32_t least, uint32_t most) { return
 template <int RT>
 __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)[2][4], const float (&vs)[2][4], bool each,
                                              float lift, const SpanWalk& w, int32_t t, uint32_t seen, const TreeRow* rows,
-                                             const float (&back)[RT], int lane, TreeState (&z)[RT],
+                                             const float (&back)[RT], int lane, bool& odd, TreeState (&z)[RT],
                                              uint32_t (&pt)[RT][2][4]) {
   const int g = lane >> 4;
   float top[RT];
@@ -328,6 +332,7 @@ __device__ __forceinline__ void tree_weights(v4_t (&c)[RT][2], const float (&ks)
       const float mn = top[i] > z[i].m + kSlack ? top[i] : z[i].m;
       const float root = half_move(z[i].m - (mn == -__builtin_inff() ? 0.0f : mn)), alpha = root * root;
       z[i].m = mn;
+      odd |= __ballot(score_apart(mn)) != 0;
       z[i].l = z[i].l * root * root;
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[i].acc[j] *= alpha;
@@ -407,7 +412,7 @@ __device__ __forceinline__ void tree_weights_apart(v4_t (&c)[RT][2], const float
 }
 
 // One step: the 32 tokens from t on, of which `seen` is what SpanWalk::fetch returned.  odd: the
-// wave has met value scales that one reference does not hold.  unit: of APART.
+// wave has met what one reference does not hold.  unit: of APART.
 template <int FMT, int RT, bool APART>
 __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const SpanWalk& w, int32_t t, uint32_t seen,
                                           const uint32_t (&q)[RT][2][4][4], const TreeRow* rows, const float (&back)[RT],
@@ -467,7 +472,7 @@ __device__ __forceinline__ void tree_step(TreeStep<FMT>& cur, const SpanWalk& w,
   if constexpr (APART)
     tree_weights_apart<RT>(c, cur.ks, cur.vs, each, w, t, seen, rows, back, lane, unit, z, pt);
   else
-    tree_weights<RT>(c, cur.ks, cur.vs, each, lift_of(hi), w, t, seen, rows, back, lane, z, pt);
+    tree_weights<RT>(c, cur.ks, cur.vs, each, lift_of(hi), w, t, seen, rows, back, lane, odd, z, pt);
   // value codes: per word the tokens' pairs of each of its dims
 #pragma unroll
   for (int w = 0; w < CacheStep<FMT>::VW; ++w) {
@@ -897,7 +902,8 @@ struct WideState {
 // two products' operands.
 __device__ __forceinline__ void wide_weights(v16_t& c, const float* ks, const float* vs, bool each, float lift,
                                              const int32_t (&live)[2], const int32_t (&at)[2], int32_t ctx, int32_t sinks,
-                                             const TreeRow* rows, float back, int lane, WideState& z, uint32_t (&pt)[2][2][4]) {
+                                             const TreeRow* rows, float back, int lane, uint32_t& odd, WideState& z,
+                                             uint32_t (&pt)[2][2][4]) {
   const int u = lane >> 5;
   float top;
 #pragma unroll
@@ -935,6 +941,7 @@ __device__ __forceinline__ void wide_weights(v16_t& c, const float* ks, const fl
     const float mn = top > z.m + kSlack ? top : z.m;
     const float root = half_move(z.m - (mn == -__builtin_inff() ? 0.0f : mn)), alpha = root * root;
     z.m = mn;
+    if (score_apart(mn)) odd = 1u;
     z.l = z.l * root * root;
 #pragma unroll
     for (int d = 0; d < 4; ++d) z.acc[d] *= alpha;
@@ -1006,7 +1013,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   extern __shared__ __attribute__((aligned(16))) uint8_t s_tile[];  // two tiles
   __shared__ float s_m[ROWS], s_l[ROWS], s_f[ROWS];
   __shared__ TreeRow s_row[ROWS];
-  __shared__ uint32_t s_odd;  // some wave has met value scales that one reference does not hold
+  __shared__ uint32_t s_odd;  // some wave has met what one reference does not hold
   static_assert(ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
   auto o_row = [&](int row) { return (float*)s_tile + row * kOPitch; };
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4;
@@ -1125,7 +1132,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
         if constexpr (APART)
           wide_weights_apart(c, ks, vs, each, live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, unit, z, pt);
         else
-          wide_weights(c, ks, vs, each, lift_of(most), live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, z, pt);
+          wide_weights(c, ks, vs, each, lift_of(most), live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, s_odd, z, pt);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll

@@ -1,5 +1,6 @@
 """The tree attention at both ends of fp32's range, in tiles of 16, 32 and 128 rows, against the
-definitions in 64 bits (tests/rows64.py): value scales of any size, zero vectors among them."""
+definitions in 64 bits (tests/rows64.py): value scales of any size, zero vectors among them,
+and scores of any size."""
 import numpy as np
 import pytest
 import torch
@@ -128,3 +129,76 @@ def test_large_values_on_long_ways(hq, fmt, window, sinks, group, tree):
         live = W.tree_visible(int(lens[b]), masks[r], window, sinks)
         want, tol = W.attend(q[r].numpy(), kv, vv, table[b].numpy(), live, L.BT, N ** -0.5, L.HEADS, group)
         W.check(out[r], want, tol, scale=N ** -0.5)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("exponent", [-9, 40])
+@pytest.mark.parametrize("size", [3e8, 1e30, -1e12])
+def test_scores_of_any_size(hq, fmt, tile, exponent, size):
+    """Every third token has the same largest score, exactly; the others are half of it below: the
+    result is the mean of those tokens' values."""
+    print(f"[tree] range scores {fmt} {tile} 2^{exponent} {size}", flush=True)
+    c = case(hq, fmt, tile, [400, 90, 1500], [9, 20, 30], seed=44)
+    code = {"int8": 64, "e4m3": 0x38, "mxfp4": 0x22}[fmt]
+    unit = {"int8": 64.0, "e4m3": 1.0, "mxfp4": 1.0}[fmt]
+    c.kc.codes.copy_(torch.full(c.kc.codes.shape, code, dtype=c.kc.codes.dtype))
+    d = torch.from_numpy(R.signs(R.SEED_K, 2 * N)).float().view(2, 1, N).expand(2, 4, N).reshape(1, 8, N)
+    c.q = d.expand(c.q.shape).contiguous()
+    c.scale = abs(size) / unit  # of a key of scale 1
+    top = torch.arange(32).expand(60, 32) % 3 == 1
+    # scores size and size / 2, or -size / 2 and -size: every row sees a token before the tree
+    if size < 0:
+        c.q = -c.q
+        set_scales(c.kc, torch.where(top, -1, 0))
+    else:
+        set_scales(c.kc, torch.where(top, 0, -1))
+    c.vc.codes.copy_(R.random_cache(hq, c.vp, fmt, c.vc.blocks, 2, 32, 45).codes.cpu())
+    set_scales(c.vc, exponent + torch.randint(-3, 4, (60, 32), generator=torch.Generator().manual_seed(1)))
+    out = c.run().cpu().numpy()
+    vv = R.values(c.vc)
+    for b, n in enumerate(c.lens[:3]):
+        r = range(c.starts[b], c.starts[b + 1])
+        live = W.tree_visible(n, c.masks[r.start:r.stop])
+        t = np.arange(n)
+        blk = c.table[b].numpy()[t // 32]
+        for i, row in enumerate(r):
+            at = live[i] & (t % 32 % 3 == 1)
+            mean = vv[blk[at], :, t[at] % 32].mean(0)  # [heads, 128]
+            want = np.repeat((mean @ R.hadamard()) / N * R.signs(R.SEED_V, 2 * N).reshape(2, N), 4, 0)
+            # weights are alike; their sum, the products' and the transform: (tokens + 60) U of the largest value
+            big = np.sqrt((vv[blk[at], :, t[at] % 32] ** 2).sum(-1).max() / N)
+            assert (np.abs(out[row] - want) <= (at.sum() + 60) * U * big).all(), (b, i)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("exponent", [-9, 60, 110])
+def test_scores_far_below_before_others(hq, fmt, tile, exponent):
+    """A sequence's first tokens have scores of -1e12, the later ones of size one."""
+    print(f"[tree] range rising {fmt} {tile} 2^{exponent}", flush=True)
+    c = case(hq, fmt, tile, [400, 90, 1500], [9, 20, 30], seed=46, pool=120)
+    blocks = [-(-n // 32) for n in c.lens[:3]]
+    for b, n in enumerate(blocks):  # blocks of their own
+        c.table[b, :n] = torch.arange(n) + sum(blocks[:b])
+    assert sum(blocks) <= 120
+    g = torch.Generator().manual_seed(5)
+    scale = torch.full((120, 32), 0.2)
+    for b, n in enumerate(blocks):
+        scale[sum(blocks[:b]):sum(blocks[:b]) + n // 2] = 1e12
+    code = {"int8": -1, "e4m3": 0xB8, "mxfp4": 0xAA}[fmt]  # -1
+    c.kc.codes.copy_(torch.full(c.kc.codes.shape, code, dtype=torch.int32).to(c.kc.codes.dtype))
+    if fmt == "mxfp4":
+        c.kc.scales.copy_(torch.where(scale > 1, 167, 125).to(torch.uint8)[:, None, :, None].expand(c.kc.scales.shape))
+    else:
+        c.kc.scales.copy_((scale * (0.5 + torch.rand(scale.shape, generator=g)))[:, None].expand(c.kc.scales.shape))
+    d = torch.from_numpy(R.signs(R.SEED_K, 2 * N)).float().view(2, 1, N).expand(2, 4, N).reshape(1, 8, N)
+    c.q, c.scale = d.expand(c.q.shape).contiguous(), 1.0
+    set_scales(c.vc, exponent + torch.randint(-3, 4, (120, 32), generator=g))
+    out = c.run().cpu().numpy()
+    ref, _ = c.reference()
+    for b in range(3):
+        r = slice(c.starts[b], c.starts[b + 1])
+        # scores of the tokens that count are below one: 2 * 150 U of it in a weight
+        big = np.abs(R.values(c.vc)[c.table[b, :blocks[b]].numpy()]).max()
+        assert (np.abs(out[r] - ref[r]) <= (c.lens[b] + 60 + 300) * U * big).all() and np.abs(ref[r]).max() > 1e-3 * big
