@@ -224,11 +224,10 @@ __device__ __forceinline__ float half_move(float x) { return __builtin_amdgcn_ex
 // 2^-126, and below, products lose their 22 bits.  And it holds scores (of base 2) up to 2^24, above
 // which the lift is lost in a score's rounding.  A wave (of tiles of 128 rows, a workgroup) that met
 // a step whose largest scale lies outside, or such a reference, goes over its tokens again with two
-// references a row
-// (`apart`): the largest score for the weights, and 2^unit beside it for the products, the largest
-// of which lies between 2^7 and 2^8 when it is set.  A product takes an exponential of its own there:
-// mantissa(scale) * 2^(score - reference + exponent - unit).  (8 sequences of 8192 tokens and 64
-// rows with scales of 2^104: 411 us, 175 with others.)
+// references a row (`apart`): the largest score for the weights, and 2^unit beside it for the
+// products, the largest of which lies between 2^7 and 2^8 when it is set.  A product takes an
+// exponential of its own there, mantissa(scale) * 2^(score - reference + exponent - unit).  (8
+// sequences of 8192 tokens and 64 rows with scales of 2^104: 411 us, 175 with others.)
 __device__ __forceinline__ bool scales_apart(uint32_t most) {
   return most >> 23 > 127 + 103 || (most != 0 && most >> 23 < 127 - 80);
 }
@@ -262,10 +261,12 @@ __device__ __forceinline__ float product_apart(float x, float scale, float unit,
   return x == -__builtin_inff() ? 0.0f : p;
 }
 
-// A row's sums with two references as those of one, both within fp32.  Returns the factor of the
-// values' sum.
+// A row's sums with two references as those of one, both within fp32: products of up to 2^8, 2^30
+// tokens of them with codes of up to 2^9, have room for 2^80, and what is left goes into the
+// reference (which a score above 2^24 rounds away: parts of a row whose value scales lie above 2^87
+// then meet with weights that are off by the scales' ratio).  Returns the factor of the values' sum.
 __device__ __forceinline__ float join_apart(float unit, float& m, float& l) {
-  const float left = __builtin_fminf(__builtin_fmaxf(unit, -48.0f), 48.0f);
+  const float left = __builtin_fminf(__builtin_fmaxf(unit, -80.0f), 80.0f);
   m += unit - left;
   l *= __builtin_amdgcn_exp2f(left - unit);
   return __builtin_amdgcn_exp2f(left);

@@ -133,7 +133,7 @@ def test_large_values_on_long_ways(hq, fmt, window, sinks, group, tree):
 
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("tile", TILES)
-@pytest.mark.parametrize("exponent", [-9, 40])
+@pytest.mark.parametrize("exponent", [-9, 40, 70])
 @pytest.mark.parametrize("size", [3e8, 1e30, -1e12])
 def test_scores_of_any_size(hq, fmt, tile, exponent, size):
     """Every third token has the same largest score, exactly; the others are half of it below: the
