@@ -642,7 +642,8 @@ hq_status hq_cache_window_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan
  * k, v, block_table, scale and the rest as hq_cache_attention.  Scores and sums are fp32; the
  * queries (in the stored coordinates) enter the products with 22 bits of the row's largest
  * value, a weight times its token's value scale with 22 bits or 2^-21 of the row's largest such
- * product, whichever is coarser.  Results repeat bit for bit.  Infinities or NaN come out where a
+ * product, whichever is coarser; MXFP4 codes as multiples of 2^-24 of their vector's largest block
+ * scale.  Results repeat bit for bit.  Infinities or NaN come out where a
  * score passes 3.4e38 or an attended key's |y| 2^95; a value scale below 2^-92 beside larger ones
  * loses low bits and one below 2^-114 all.  Value scales above 2^103, sequences with none from 2^-80
  * on and scores above 10^7 take twice the time; such scores and value scales above 2^86 together

@@ -9,8 +9,9 @@
 //   values   O^T[dim, row] += V^T (16 dims x 32 tokens) P^T
 // with the same numbering of a step's tokens, so that no weight moves between lanes.
 //
-// Both products run on the matrix cores in fp16, which holds every code of the three formats
-// exactly (MXFP4's with its block's scale relative to the token's largest).  A query row is
+// Both products run on the matrix cores in fp16, which holds every int8 and E4M3 code exactly, and an
+// MXFP4 code with its block's scale relative to the token's largest as a multiple of 2^-24: of blocks
+// 2^-24 of the largest and less it loses codes, 2^-25 of the largest at most.  A query row is
 // moved to [2^14, 2^15) by a power of two and enters as two fp16 terms, cut off: 11 + 11 bits
 // of the row's largest value.  So do a weight times its token's value scale: a row's reference
 // (TreeState, kSlack) keeps that product below 2^15 and its row's largest at 2^1 or more, so

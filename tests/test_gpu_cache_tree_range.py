@@ -202,3 +202,44 @@ def test_scores_far_below_before_others(hq, fmt, tile, exponent):
         # scores of the tokens that count are below one: 2 * 150 U of it in a weight
         big = np.abs(R.values(c.vc)[c.table[b, :blocks[b]].numpy()]).max()
         assert (np.abs(out[r] - ref[r]) <= (c.lens[b] + 60 + 300) * U * big).all() and np.abs(ref[r]).max() > 1e-3 * big
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("low", [96, 0])
+@pytest.mark.parametrize("side", ["k", "v", "both"])
+def test_mxfp4_blocks_far_apart(hq, tile, low, side):
+    """Block scales of a vector from 2^(low - 127) to 2^2: a code enters as a multiple of 2^-24 of the vector's
+    largest block scale, half a step of which, 2^-25 of it, is a fourth of the U of the largest value
+    that the bound allows for each token."""
+    print(f"[tree] range blocks {tile} {low} {side}", flush=True)
+    c = case(hq, "mxfp4", tile, [400, 90, 1500], [9, 20, 30], seed=47)
+    g = torch.Generator().manual_seed(low)
+    for x, of in ((c.kc, "k"), (c.vc, "v")):
+        if side in (of, "both"):
+            x.scales.copy_(torch.randint(low, 130, x.scales.shape, generator=g, dtype=torch.uint8))
+            x.scales[::3, :, ::2, 1:] = 0  # one block alone counts
+    c.vc.scales[:, :, ::7] = 0 if side != "k" else c.vc.scales[:, :, ::7]  # vectors of the least scale
+    out = c.run()
+    W.check(out.cpu().numpy(), *c.reference())
+    assert torch.equal(c.run(), out) and c.kc.read_stats()["status"] == 0
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("below", [10, 14, 16, 20, 23, 25, 30])
+def test_mxfp4_codes_of_a_block_far_below(hq, tile, below):
+    """A sequence of one token, whose weight is 1: what comes out are its codes, in a block 2^-below of the
+    largest one (which holds zeros) rounded to multiples of 2^-24."""
+    c = case(hq, "mxfp4", tile, [1], [1], seed=48)
+    blk = int(c.table[0, 0])
+    g = torch.Generator().manual_seed(below)
+    codes = torch.randint(0, 256, (2, 64), generator=g, dtype=torch.uint8)
+    codes[:, :16] = 0
+    c.vc.codes[blk, :, 0] = codes.cuda()
+    c.vc.scales[blk, :, 0] = torch.tensor([127, 127 - below, 127 - below, 0], dtype=torch.uint8).cuda()
+    out = c.run()[0].cpu().numpy().astype(np.float64).reshape(2, 4, N)
+    y = (out * R.signs(R.SEED_V, 2 * N).reshape(2, 1, N)) @ R.hadamard()
+    want = R.values(c.vc)[blk, :, 0]
+    # half a step, and a handful of roundings of what came through the transform, sqrt(128) of its norm at most
+    room = 2.0 ** -25 + 16 * U * np.linalg.norm(want, axis=-1).max() * np.sqrt(N)
+    assert (np.abs(y - want[:, None]) <= room).all()
+    assert below > 24 or np.abs(y).max() > 2.0 ** -below
