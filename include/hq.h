@@ -636,6 +636,8 @@ hq_status hq_cache_window_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan
  *   window       0: all tokens before the tree; else a row whose mask has d bits looks at those of
  *                the last window - d of them and at the first `sinks` tokens.  At least max_tree
  *                (HQ_ERR_UNSUPPORTED below).
+ *   block_table  entries of blocks that end before the last `window` tokens before the tree and hold
+ *                none of the first `sinks`, and of those behind the sequence, are not used.
  *   out          device [rows, heads_q, 128], HQ_FP32 or HQ_BF16, 16-byte aligned
  *   workspace    >= hq_cache_tree_workspace_bytes(k, batch, heads_q, max_blocks, max_tree, window,
  *                sinks); may be null where that is 0.  Overlapping calls need one each.
