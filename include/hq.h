@@ -648,8 +648,9 @@ hq_status hq_cache_window_attention(hq_plan_t k_plan, const hq_cache* k, hq_plan
  * scale.  Results repeat bit for bit.  Infinities or NaN come out where a
  * score passes 3.4e38 or an attended key's |y| 2^95; a value scale below 2^-92 beside larger ones
  * loses low bits and one below 2^-114 all.  Value scales above 2^103, sequences with none from 2^-80
- * on and scores above 10^7 take twice the time; such scores and value scales above 2^86 together
- * weigh tokens of one score by up to the ratio of their value scales.  An E4M3 code that is a NaN
+ * on and scores above 10^7 take two to two and a half times as long (and, unlike elsewhere, the rows
+ * beside them in a tile may round otherwise); such scores and value scales above 2^86 together weigh
+ * tokens of one score by up to the ratio of their value scales.  An E4M3 code that is a NaN
  * (hq_cache_write stores none) makes every row of its sequence NaN; a NaN scale the rows that see
  * its token.
  * Device-side, in k->stats (HQ_ERR_INVALID_ARG): lengths and block ids as hq_cache_attention;

@@ -63,7 +63,8 @@ __device__ __forceinline__ void two_terms(float x, float y, uint32_t& hi, uint32
 }
 
 // Int8 codes c + 128 as bytes 0 and 2 of a word, which are the fp16 numbers (c + 128) 2^-24:
-// c 2^-9.  A row's scores and its values' sum take the 2^9 (kCodeUnit).
+// c 2^-9.  The scales take the 2^9 (kCodeUnit), of which one of 2^119 or more becomes infinite; with
+// two references (below) a row's scores and its values' sum take it.
 __device__ __forceinline__ uint32_t halves_of_bytes(uint32_t w) {
   const v2h_t x = __builtin_bit_cast(v2h_t, w);
   const v2h_t up = {(_Float16)32768.0f, (_Float16)32768.0f}, off = {(_Float16)-0.25f, (_Float16)-0.25f};
@@ -124,7 +125,7 @@ __device__ __forceinline__ float below_scale(uint32_t byte, float scale) {
   return __uint_as_float((uint32_t)max(e, 0) << 23);
 }
 
-template <int FMT>
+template <int FMT, bool APART>
 __device__ __forceinline__ void tree_take(uint8_t* step, int lane, TreeStep<FMT>& s) {
   using R = CacheRing<FMT>;
   const uint32_t n = lane & 15, g = lane >> 4;
@@ -154,7 +155,11 @@ __device__ __forceinline__ void tree_take(uint8_t* step, int lane, TreeStep<FMT>
     } else {
       s.kf[h] = 1.0f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s.vf[h][r] = 1.0f;
+      for (int r = 0; r < 4; ++r) {
+        s.vf[h][r] = 1.0f;
+        if (!APART) s.ks[h][r] *= kCodeUnit<FMT>;
+        if (!APART) s.vs[h][r] *= kCodeUnit<FMT>;
+      }
     }
   }
 }
@@ -228,9 +233,10 @@ __device__ __forceinline__ float half_move(float x) { return __builtin_amdgcn_ex
 // references a row (`apart`): the largest score for the weights, and 2^unit beside it for the
 // products, the largest of which lies between 2^7 and 2^8 when it is set.  A product takes an
 // exponential of its own there, mantissa(scale) * 2^(score - reference + exponent - unit).  (8
-// sequences of 8192 tokens and 64 rows with scales of 2^104: 411 us, 175 with others.)
+// sequences of 8192 tokens and 64 rows with scales of 2^104: 410 us, 166 with others.)
 __device__ __forceinline__ bool scales_apart(uint32_t most) {
-  return most >> 23 > 127 + 103 || (most != 0 && most >> 23 < 127 - 80);
+  // one comparison for both ends; a zero passes the second
+  return most - (47u << 23) > (183u << 23 | 0x7FFFFFu) && most != 0u;
 }
 
 __device__ __forceinline__ bool score_apart(float m) { return __builtin_fabsf(m) > 0x1p24f && m != -__builtin_inff(); }
@@ -629,7 +635,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   // step s of the contraction takes dims 32 (l / 16) + 8 s + j in lane l (the codes
   // that the lane's one run of 32 holds)
   uint32_t q[RT][2][4][4];
-  float back[RT];  // 1 / the power of two that a row was moved by, times the codes' unit
+  float back[RT];  // 1 / the power of two that a row was moved by
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
 #pragma unroll
@@ -639,7 +645,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
         const uint4 x = *(const uint4*)(q_row(16 * i + n, t) + 32 * g + 8 * s);
         q[i][t][s][0] = x.x; q[i][t][s][1] = x.y; q[i][t][s][2] = x.z; q[i][t][s][3] = x.w;
       }
-    back[i] = s_f[16 * i + n] * kCodeUnit<FMT>;
+    back[i] = s_f[16 * i + n];
   }
   __syncthreads();  // the queries' place is loaded over
 
@@ -667,7 +673,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
       else
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       TreeStep<FMT> cur;
-      tree_take<FMT>(ring + slot * R::STEP, lane, cur);
+      tree_take<FMT, APART>(ring + slot * R::STEP, lane, cur);
       const uint32_t here = sees;
       sees = next;
       if (t + 64 < end) {
@@ -680,6 +686,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   };
   way(std::false_type());
   if (__builtin_expect(odd, 0)) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) back[i] *= kCodeUnit<FMT>;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what the ring held is in registers
     w.ask(A, begin, lane);
     w.got();
@@ -690,10 +698,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     z[i].l = groups_sum(z[i].l);
-    float by = kCodeUnit<FMT>;
-    if (odd) by *= join_apart(unit[i], z[i].m, z[i].l);
+    if (odd) {
+      const float by = kCodeUnit<FMT> * join_apart(unit[i], z[i].m, z[i].l);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z[i].acc[k] *= by;
+      for (int k = 0; k < 8; ++k) z[i].acc[k] *= by;
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float* o = o_row(wave, 16 * i + n) + (4 * g + r) * 8;
@@ -806,13 +815,13 @@ __device__ __forceinline__ uint32_t largest_byte(uint32_t w) {
   return max(max(w & 0xFFu, (w >> 8) & 0xFFu), max((w >> 16) & 0xFFu, w >> 24));
 }
 // Bits of a token's scale: MXFP4's is its largest block's.
-template <int FMT>
+template <int FMT, bool APART>
 __device__ __forceinline__ uint32_t token_scale(uint32_t w) {
   if constexpr (FMT == kMx) {
     const uint32_t x = largest_byte(w);
     return x == 255u ? 0x7FC00000u : x << 23;
   } else {
-    return w;
+    return APART ? w : __float_as_uint(__uint_as_float(w) * kCodeUnit<FMT>);
   }
 }
 
@@ -826,13 +835,13 @@ __device__ __forceinline__ float row_max(float x) {
 
 // The 16 tokens as fp16 into a tile, where they are its `group`-th, with their scales and what
 // the products go by: the value scales' largest and least, and the tokens that anybody sees.
-template <int FMT>
+template <int FMT, bool APART>
 __device__ __forceinline__ void turn(TreeLoads<FMT>& x, uint8_t* tile, int group, int lane) {
   using T = TreeTile<FMT>;
   constexpr int VW = TreeLoads<FMT>::VW, D = 8 / VW;
   const int n = lane & 15, g = lane >> 4, step = group >> 1, h = group & 1;
-  const uint32_t ks = token_scale<FMT>(x.ks);
-  uint32_t vs = token_scale<FMT>(x.vs);
+  const uint32_t ks = token_scale<FMT, APART>(x.ks);
+  uint32_t vs = token_scale<FMT, APART>(x.vs);
   const float kf = FMT == kMx ? below_scale((x.ks >> (8 * g)) & 0xFFu, __uint_as_float(ks)) : 1.0f;
   float vf[4] = {1.0f, 1.0f, 1.0f, 1.0f};
   if constexpr (FMT == kMx) {
@@ -1008,27 +1017,34 @@ __device__ __forceinline__ void wide_weights_apart(v16_t& c, const float* ks, co
   }
 }
 
-template <int FMT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_wide_kernel(hq_cache_attn_args A) {
+// What a workgroup keeps in LDS beside its tiles.
+struct WideShared {
+  float m[kWideRows], l[kWideRows], f[kWideRows];
+  TreeRow row[kWideRows];
+  uint32_t odd;  // some wave has met what one reference does not hold
+};
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+typedef __attribute__((address_space(3))) WideShared lds_wide;
+typedef __attribute__((address_space(4))) const hq_cache_attn_args kernel_args;
+
+// Workgroup `block` of the grid.  Returns whether it has to be done over again with two references.
+template <int FMT, bool APART>
+__device__ __forceinline__ bool wide_workgroup(const hq_cache_attn_args& A, uint32_t block, int tid, uint8_t* s_tile, WideShared& S) {
   using T = TreeTile<FMT>;
   constexpr int ROWS = kWideRows;
-  extern __shared__ __attribute__((aligned(16))) uint8_t s_tile[];  // two tiles
-  __shared__ float s_m[ROWS], s_l[ROWS], s_f[ROWS];
-  __shared__ TreeRow s_row[ROWS];
-  __shared__ uint32_t s_odd;  // some wave has met what one reference does not hold
   static_assert(ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
   auto o_row = [&](int row) { return (float*)s_tile + row * kOPitch; };
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, grp = tid >> 4;
+  const int lane = tid & 63, n = lane & 15, grp = tid >> 4;
   const int wave = (int)readfirst((uint32_t)(tid >> 6));
-  const int32_t j = (int32_t)(blockIdx.x / (uint32_t)A.heads_kv), c0 = n * 8;
-  const int32_t head = (int32_t)(blockIdx.x - (uint32_t)j * (uint32_t)A.heads_kv);
-  const CacheItem it = cache_item<kTree>(A, j, lane, blockIdx.x == 0 && wave == 0);
-  if (it.b < 0) return;
+  const int32_t j = (int32_t)(block / (uint32_t)A.heads_kv), c0 = n * 8;
+  const int32_t head = (int32_t)(block - (uint32_t)j * (uint32_t)A.heads_kv);
+  const CacheItem it = cache_item<kTree>(A, j, lane, block == 0 && wave == 0);
+  if (it.b < 0) return false;
   // what the join goes by
   if (A.join && A.batch <= HQ_CACHE_UNPLANNED && j == it.first && head == 0 && tid == 0)
     A.parts[it.b] = {it.first, it.n};
   const int32_t rows = it.span.rows, seen = it.span.seen(), tile = it.tile;
-  if (tile * ROWS >= rows * A.group) return;  // none of this sequence's, or it has none at all
+  if (tile * ROWS >= rows * A.group) return false;  // none of this sequence's, or it has none at all
   const int32_t from = it.span.from;
   const int32_t begin = (int32_t)(it.at * it.chunk), end = begin + min(it.chunk, seen - begin);
   TreeWay way;
@@ -1042,8 +1058,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   way.ask(A, begin + 16 * wave);
   way.template load<FMT>(A, begin + 16 * wave, end, lane, loads);
   const int32_t ctx = it.span.len - rows;
-  if (tid < ROWS) s_row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
-  if (tid == 0) s_odd = 0u;
+  if (tid < ROWS) S.row[tid] = tree_row(A, tile * ROWS + tid, rows, from, ctx);
+  if (tid == 0) S.odd = 0u;
   // ---- the queries into the cache's coordinates, as two fp16 terms of a power of two times each,
   // [32 rows][term][contraction step][lane] 16 bytes; the next ones are on their way meanwhile
   const uint4 qd = sign_words(A.k_dsign16, head * HQ_TILE + c0);
@@ -1066,7 +1082,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     uint8_t* to = s_tile + (i >> 1) * 16384 + (n >> 1) * 1024 + ((n & 1) * 32 + (i & 1) * 16 + grp) * 16;
     *(uint4*)to = hi;
     *(uint4*)(to + 8192) = lo;
-    if (n == 0) s_f[16 * i + grp] = f;
+    if (n == 0) S.f[16 * i + grp] = f;
   }
   __syncthreads();
   uint32_t q[2][8][4];
@@ -1077,94 +1093,92 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       const uint4 x = *(const uint4*)(s_tile + ((wave * 2 + t) * 8 + s) * 1024 + lane * 16);
       q[t][s][0] = x.x; q[t][s][1] = x.y; q[t][s][2] = x.z; q[t][s][3] = x.w;
     }
-  // 1 / the power of two that the row was moved by, times the codes' unit
-  const float back = s_f[32 * wave + (lane & 31)] * kCodeUnit<FMT>;
+  // 1 / the power of two that the row was moved by
+  const float back = S.f[32 * wave + (lane & 31)] * (APART ? kCodeUnit<FMT> : 1.0f);
   __syncthreads();  // the queries' place is written over
   WideState z;
   // from here on every row's window has begun
   const int32_t open = A.window ? ctx + rows - A.window : 0;
   const bool idle = tile * ROWS + 32 * wave >= rows * A.group;  // the wave has no rows
   float unit = 0.0f;
-  auto tokens = [&](auto apart) {
-    constexpr bool APART = decltype(apart)::value;
-    z.m = -__builtin_inff();
-    z.l = 0.0f;
+  z.m = -__builtin_inff();
+  z.l = 0.0f;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int k = 0; k < 16; ++k) z.acc[d][k] = 0.0f;
-    turn<FMT>(loads, s_tile, wave, lane);
-    if (begin + kTreeTile < end) way.template load<FMT>(A, begin + kTreeTile + 16 * wave, end, lane, loads);
-    tile_barrier();
-    uint8_t* at_tile = s_tile;
-    uint8_t* to_tile = s_tile + T::BYTES;
-    Behind first;
-    first.start(begin, (end - begin) / (4 * kTreeTile) * kTreeTile);
-    for (int32_t t = begin; t < end; t += kTreeTile) {
-      first.at(t, end);
-      if (t + kTreeTile < end) {
-        turn<FMT>(loads, to_tile, wave, lane);
-        if (t + 2 * kTreeTile < end) way.template load<FMT>(A, t + 2 * kTreeTile + 16 * wave, end, lane, loads);
-      }
-#pragma unroll 1
-      for (int step = 0; step < 2; ++step) {
-        const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32);
-        const uint4 about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
-        const int32_t live[2] = {(int32_t)readfirst(about0.z), (int32_t)readfirst(about1.z)};
-        if ((live[0] | live[1]) == 0 || idle) continue;
-        // the largest and least value scale: not negative, so ordered as their bits are
-        const uint32_t most = max(readfirst(about0.x), readfirst(about1.x));
-        const uint32_t least = min(readfirst(about0.y), readfirst(about1.y));
-        const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
-        bool each = (live[0] & live[1]) != 0xFFFF || (!APART && !one_lift(least, most));
-#pragma unroll
-        for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
-        if (!APART && __builtin_expect(scales_apart(most), 0)) s_odd = 1u;
-        v16_t c;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) c[k] = 0.0f;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          const uint4 a = *(const uint4*)(at_tile + ((step * 8 + s) * 64 + lane) * 16);
-#pragma unroll
-          for (int t1 = 1; t1 >= 0; --t1) c = mfma_f16(a, q[t1][s], c);
-        }
-        uint32_t pt[2][2][4];
-        const float *ks = (const float*)(at_tile + T::KS) + step * 32, *vs = (const float*)(at_tile + T::VS) + step * 32;
-        if constexpr (APART)
-          wide_weights_apart(c, ks, vs, each, live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, unit, z, pt);
-        else
-          wide_weights(c, ks, vs, each, lift_of(most), live, at, ctx, A.sinks, s_row + 32 * wave, back, lane, s_odd, z, pt);
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const uint4 v = *(const uint4*)(at_tile + T::V + (((step * 4 + d) * 2 + k) * 64 + lane) * 16);
-#pragma unroll
-            for (int t1 = 1; t1 >= 0; --t1) z.acc[d] = mfma_f16(v, pt[t1][k], z.acc[d]);
-          }
-      }
-      tile_barrier();
-      uint8_t* const x = at_tile;
-      at_tile = to_tile;
-      to_tile = x;
+    for (int k = 0; k < 16; ++k) z.acc[d][k] = 0.0f;
+  turn<FMT, APART>(loads, s_tile, wave, lane);
+  if (begin + kTreeTile < end) way.template load<FMT>(A, begin + kTreeTile + 16 * wave, end, lane, loads);
+  tile_barrier();
+  uint8_t* at_tile = s_tile;
+  uint8_t* to_tile = s_tile + T::BYTES;
+  Behind first;
+  first.start(begin, (end - begin) / (4 * kTreeTile) * kTreeTile);
+  for (int32_t t = begin; t < end; t += kTreeTile) {
+    first.at(t, end);
+    if (t + kTreeTile < end) {
+      turn<FMT, APART>(loads, to_tile, wave, lane);
+      if (t + 2 * kTreeTile < end) way.template load<FMT>(A, t + 2 * kTreeTile + 16 * wave, end, lane, loads);
     }
-  };
-  tokens(std::false_type());
-  const bool odd = readfirst(s_odd) != 0u;
-  if (__builtin_expect(odd, 0)) {
-    way.ask(A, begin + 16 * wave);
-    way.template load<FMT>(A, begin + 16 * wave, end, lane, loads);
-    tokens(std::true_type());
+#pragma unroll 1
+    for (int step = 0; step < 2; ++step) {
+      const uint4 about0 = *(const uint4*)(at_tile + T::SEEN + step * 32);
+      const uint4 about1 = *(const uint4*)(at_tile + T::SEEN + step * 32 + 16);
+      const int32_t live[2] = {(int32_t)readfirst(about0.z), (int32_t)readfirst(about1.z)};
+      if ((live[0] | live[1]) == 0 || idle) continue;
+      // the largest and least value scale: not negative, so ordered as their bits are
+      const uint32_t most = max(readfirst(about0.x), readfirst(about1.x));
+      const uint32_t least = min(readfirst(about0.y), readfirst(about1.y));
+      const int32_t at[2] = {way.real(t + 32 * step), way.real(t + 32 * step + 16)};
+      bool each = (live[0] & live[1]) != 0xFFFF || (!APART && !one_lift(least, most));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) each |= at[h] + 16 > ctx || (at[h] < open && at[h] + 16 > A.sinks);
+      if (!APART && __builtin_expect(scales_apart(most), 0)) S.odd = 1u;
+      v16_t c;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) c[k] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const uint4 a = *(const uint4*)(at_tile + ((step * 8 + s) * 64 + lane) * 16);
+#pragma unroll
+        for (int t1 = 1; t1 >= 0; --t1) c = mfma_f16(a, q[t1][s], c);
+      }
+      uint32_t pt[2][2][4];
+      const float *ks = (const float*)(at_tile + T::KS) + step * 32, *vs = (const float*)(at_tile + T::VS) + step * 32;
+      if constexpr (APART)
+        wide_weights_apart(c, ks, vs, each, live, at, ctx, A.sinks, S.row + 32 * wave, back, lane, unit, z, pt);
+      else
+        wide_weights(c, ks, vs, each, lift_of(most), live, at, ctx, A.sinks, S.row + 32 * wave, back, lane, S.odd, z, pt);
+      // the next fragments are read before a product waits for its own
+      uint4 v[3];
+      auto read = [&](int i) {
+        v[i % 3] = *(const uint4*)(at_tile + T::V + (((step * 4 + (i & 3)) * 2 + (i >> 2)) * 64 + lane) * 16);
+      };
+#pragma unroll
+      for (int i = 0; i < 3; ++i) read(i);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int t1 = 1; t1 >= 0; --t1) z.acc[i & 3] = mfma_f16(v[i % 3], pt[t1][i >> 2], z.acc[i & 3]);
+        if (i + 3 < 8) read(i + 3);
+      }
+    }
+    tile_barrier();
+    uint8_t* const x = at_tile;
+    at_tile = to_tile;
+    to_tile = x;
   }
+  const bool odd = !APART && readfirst(S.odd) != 0u;
   // ---- the sums, one row per 16 lanes
   {
     const v2u_t l = __builtin_amdgcn_permlane32_swap(__float_as_uint(z.l), __float_as_uint(z.l), false, false);
     const int u = lane >> 5, at_row = 32 * wave + (lane & 31);
-    float sum = __uint_as_float(l[0]) + __uint_as_float(l[1]), by = kCodeUnit<FMT>;
-    if (odd) by *= join_apart(unit, z.m, sum);
+    float sum = __uint_as_float(l[0]) + __uint_as_float(l[1]);
+    if constexpr (APART) {
+      const float by = kCodeUnit<FMT> * join_apart(unit, z.m, sum);
 #pragma unroll
-    for (int d = 0; d < 4; ++d) z.acc[d] *= by;
+      for (int d = 0; d < 4; ++d) z.acc[d] *= by;
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {  // i / 4 % 2 = k / 4, i % 4 = k % 4
       const int i = 4 * (k >> 2) + (k & 3);
@@ -1173,8 +1187,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       *(float4*)(o + 4) = make_float4(z.acc[2][i], z.acc[2][i + 8], z.acc[3][i], z.acc[3][i + 8]);
     }
     if (u == 0) {
-      s_m[at_row] = z.m;
-      s_l[at_row] = sum;
+      S.m[at_row] = z.m;
+      S.l[at_row] = sum;
     }
   }
   __syncthreads();
@@ -1184,7 +1198,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     const TreePlace p(A, tile * ROWS + at_row);
     float v[8];
     load8(o_row(at_row), c0, false, v);
-    tree_result(A, it.n > 1, (int64_t)blockIdx.x * ROWS + at_row, s_m[at_row], s_l[at_row], v, p, rows, from, head, lane);
+    tree_result(A, it.n > 1, (int64_t)block * ROWS + at_row, S.m[at_row], S.l[at_row], v, p, rows, from, head, lane);
+  }
+  return odd;
+}
+
+// A function of its own: as part of the kernel it would cost its loop registers, 2 to 4 % of every call's
+// time.  The registers that it saves are the kernel's scratch memory, which other calls do not touch.
+template <int FMT>
+__device__ __attribute__((noinline)) void wide_again(kernel_args* A, uint32_t block, int tid, lds_byte* tile, lds_wide* S) {
+  const uint64_t at = (uint64_t)A;  // what is the same in every lane, told so
+  const auto* args = (kernel_args*)((uint64_t)readfirst((uint32_t)(at >> 32)) << 32 | readfirst((uint32_t)at));
+  auto* t = (lds_byte*)(uintptr_t)readfirst((uint32_t)(uintptr_t)tile);
+  auto* s = (lds_wide*)(uintptr_t)readfirst((uint32_t)(uintptr_t)S);
+  wide_workgroup<FMT, true>(*(const hq_cache_attn_args*)args, readfirst(block), tid, (uint8_t*)t, *(WideShared*)s);
+}
+
+template <int FMT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_wide_kernel(hq_cache_attn_args A) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t s_tile[];  // two tiles
+  __shared__ WideShared S;
+  if (__builtin_expect((wide_workgroup<FMT, false>(A, blockIdx.x, threadIdx.x, s_tile, S)), 0)) {
+    __syncthreads();  // the sums have been read
+    wide_again<FMT>((kernel_args*)__builtin_amdgcn_kernarg_segment_ptr(), blockIdx.x, threadIdx.x, (lds_byte*)s_tile, (lds_wide*)&S);
   }
 }
 
