@@ -20,13 +20,13 @@
 // 24 bits, for half as many products again and twice the instructions of cutting.)
 //
 // What bounds it: a row and token take 2 x 2 x 2 x 128 operations of the matrix cores, and a
-// lane's 16 of them some 8 instructions each for their softmax, two terms included.  Of two waves
-// on a SIMD the products of one hide a seventh of the other's vector instructions (4 products of
-// 16 x 16 x 32 beside 16 fma: 97 ns for both waves, 64 and 49 alone), so the time is nearly their
-// sum: of 198 us for 8 sequences of 8192 tokens, 64 rows, 8 KV heads of 4, int8 (182 since), 39 lay
-// before, behind and between the loops (11 the join); without the loads 150 were left, without
-// the softmax 123, without the second product 129.  (The codes' bytes take 29 us at a copy's
-// rate, the two terms' products 116 at that of a large matrix product.)
+// lane's 16 of them some 8 instructions each for their softmax, two terms included.  8 sequences of
+// 8192 tokens, 64 rows, 8 KV heads of 4, int8: 167 us in tiles of 128 rows and the join's 11.  In 40 %
+// of the kernel's cycles the matrix units are busy, in 48 % the vector units.  A wave's products wait
+// for its softmax and its softmax for its products, so they overlap with another wave's only, of
+// which a SIMD has two.  (The codes' bytes take 29 us at a copy's rate, the two terms' products 116
+// at that of a large matrix product.  24 uneven trees in MXFP4, groups of 7, in tiles of 32: 66 us,
+// matrix units busy in 23 %, vector units in 52.)
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -572,8 +572,8 @@ constexpr int tree_wave_bytes() {
 }
 
 // Tiles of 16 RT rows: every wave has all of them and its own tokens.  (24 uneven trees in MXFP4,
-// groups of 7: 70 us; the longest wave goes through 22 steps, some 5400 cycles each with two waves
-// a SIMD.  1 x 777 tokens 11.7 us: four steps and the chain around them.)
+// groups of 7: 69.6 us a call; the longest wave goes through 22 steps, some 5400 cycles each with two
+// waves a SIMD.  1 x 777 tokens 11.8 us: four steps and the chain around them.)
 template <int FMT, int RT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void hq_cache_tree_kernel(
     hq_cache_attn_args A) {
@@ -741,8 +741,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 // steps of 32; each wave turns the keys and values of 16 of them into LDS in the order that the
 // products' operands are read in, a tile ahead of the products; the codes of the tile after it
 // are on their way in registers meanwhile.  (8 sequences of 8192 tokens and 64 rows, groups of 4:
-// 181 us, and 195 in tiles of 32 rows, whose waves each turn what they read.  Tiles of 256 rows,
-// eight waves of one workgroup a CU, took 177, but uneven trees 299 where these took 221.)
+// 172 us a call, and 181 in tiles of 32 rows, whose waves each turn what they read.  Tiles of 256 rows,
+// eight waves of one workgroup a CU, were 3 % faster there, but took 299 for uneven trees where these
+// took 221.)
 //
 // The products are 32 x 32 x 16: a step's scores are one tile C[token, row], in which lane l
 // holds tokens 8 q + 4 (l / 32) + r of row l % 32; with product t of the values contracting
@@ -1029,7 +1030,8 @@ typedef __attribute__((address_space(4))) const hq_cache_attn_args kernel_args;
 
 // Workgroup `block` of the grid.  Returns whether it has to be done over again with two references.
 template <int FMT, bool APART>
-__device__ __forceinline__ bool wide_workgroup(const hq_cache_attn_args& A, uint32_t block, int tid, uint8_t* s_tile, WideShared& S) {
+__device__ __forceinline__ bool wide_workgroup(const hq_cache_attn_args& A, uint32_t block, int tid, uint8_t* s_tile,
+                                               WideShared& S) {
   using T = TreeTile<FMT>;
   constexpr int ROWS = kWideRows;
   static_assert(ROWS * kOPitch * (int)sizeof(float) <= 2 * T::BYTES && ROWS * 2 * HQ_TILE * 2 <= 2 * T::BYTES, "");
@@ -1220,7 +1222,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   __shared__ WideShared S;
   if (__builtin_expect((wide_workgroup<FMT, false>(A, blockIdx.x, threadIdx.x, s_tile, S)), 0)) {
     __syncthreads();  // the sums have been read
-    wide_again<FMT>((kernel_args*)__builtin_amdgcn_kernarg_segment_ptr(), blockIdx.x, threadIdx.x, (lds_byte*)s_tile, (lds_wide*)&S);
+    wide_again<FMT>((kernel_args*)__builtin_amdgcn_kernarg_segment_ptr(), blockIdx.x, threadIdx.x, (lds_byte*)s_tile,
+                    (lds_wide*)&S);
   }
 }
 

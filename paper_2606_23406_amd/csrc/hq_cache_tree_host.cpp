@@ -5,7 +5,7 @@
 
 namespace {
 
-// What a workspace size goes by; 0 rows: one token per sequence.
+// What a workspace size goes by.
 bool sizes_ok(const hq_cache* k, int64_t batch, int32_t heads_q, int32_t max_blocks, int32_t window, int32_t sinks) {
   return k && batch > 0 && heads_q > 0 && max_blocks > 0 && k->heads > 0 && k->block_tokens > 0 &&
          heads_q % k->heads == 0 && window >= 0 && sinks >= 0;

@@ -435,10 +435,10 @@ static inline int64_t hq_cache_joins(int64_t batch, int64_t heads_kv) {
 //   128  the codes turned into fp16 once for all of a workgroup's waves: where the tiles are
 //        three quarters full and fill the chip, which chunks do for split sequences
 //   32   else
-// 8 KV heads of 4, int8, us: 16 sequences of 500 tokens and 8 rows each 12.1 in tiles of 16, 15.7 of
-// 32; 4 of 1000 and 32 14.5 and 23.4; 16 of 8192 and 8 86 and 69.  8 of 8192 tokens and 64 rows
-// 181 in tiles of 128, 195 of 32; 64 of 1000 and 16, groups of 8, 102 and 122; but 8 of 1000 and
-// 25 (256 workgroups of 128 rows) 65 and 23, and 24 of up to 6001 and up to 48, groups of 16, which
+// 8 KV heads of 4, int8, us a call: 16 sequences of 500 tokens and 8 rows each 12.3 in tiles of 16,
+// 16.0 of 32; 4 of 1000 and 32 14.5 and 23.8; 16 of 8192 and 8 83 and 69.  8 of 8192 tokens and 64
+// rows 172 in tiles of 128, 181 of 32; 64 of 1000 and 16, groups of 8, 94 and 121; but 8 of 1000 and
+// 25 (256 workgroups of 128 rows) 65 and 25, and 24 of up to 6001 and up to 48, groups of 16, which
 // fill tiles of 128 by half, 227 and 199.
 #define HQ_TREE_SMALL 256
 #define HQ_TREE_WIDE 512

@@ -119,6 +119,8 @@ __device__ __forceinline__ void apply_turn(const hq_turns& T, const Turn& t, int
   for (int j = 0; j < 8; ++j) v[j] = t.in ? v[j] * t.c[j] + o[j] * t.s[j] : v[j];
 }
 
+// Bound by its 64-bit arithmetic (sine, cosine, a division): 131072 positions of 64 pairs, 67 MB, take
+// 34.9 us, at a large copy's rate 13.1; 4096 of them 5.7, a launch and little else.
 __global__ __launch_bounds__(256) void hq_rope_table_kernel(hq_rope_table_args A) {
   const int64_t n = A.count * A.pairs;
   for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
