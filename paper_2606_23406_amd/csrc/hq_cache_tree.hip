@@ -1206,7 +1206,8 @@ __device__ __forceinline__ bool wide_workgroup(const hq_cache_attn_args& A, uint
 }
 
 // A function of its own: as part of the kernel it would cost its loop registers, 2 to 4 % of every call's
-// time.  The registers that it saves are the kernel's scratch memory, which other calls do not touch.
+// time.  The registers that it saves are the kernel's scratch memory, which other calls do not touch:
+// 476 bytes a lane, of which the runtime sets 240 MB aside for a hardware queue.
 template <int FMT>
 __device__ __attribute__((noinline)) void wide_again(kernel_args* A, uint32_t block, int tid, lds_byte* tile, lds_wide* S) {
   const uint64_t at = (uint64_t)A;  // what is the same in every lane, told so
